@@ -303,6 +303,45 @@ pvf_status pvf_gemm_swiglu(void *stream, int32_t dtype, const void *A, const voi
 pvf_status pvf_rmsnorm(void *stream, int32_t dtype, const void *x, const void *gain, void *out,
                        int32_t M, int32_t d, float eps);
 
+/* ---- block-scaled rows ------------------------------------------------------------------
+ * Rows in 8 or 4 bits for the projections around a layer's norms: 32 consecutive elements of a row share a scale 2^(b - 127), b a
+ * byte; the elements are
+ *   PVF_MX_E4M3  8 bits, sign, 4 exponent bits, 3 mantissa bits, at most 448, no infinities;
+ *   PVF_MX_E2M1  4 bits, 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0-7) and their negatives (8-15); two in a byte, the even element low.
+ * Kp = K rounded up to a multiple of 128.  Codes are [rows, Kp] bytes (PVF_MX_E2M1: [rows, Kp / 2]), scales [Kp / 128, rows, 4] bytes:
+ * scales[k / 128][row][k / 32 % 4] belongs to elements k .. k + 31.  Elements behind K are zero codes; a product multiplies them like
+ * others, so a caller who makes codes of its own must clear them and give their scales a value below 255.
+ * Scales are the smallest powers of two, from 2^-127 on, that bring a block's largest magnitude to 448 (6) at most, so nothing
+ * saturates; elements are rounded to the nearest code, ties to even.  A block that holds a NaN or an infinity has scale byte 255, which
+ * stands for NaN, and zero codes: every result that reads it is NaN.
+ * codes, scales and rows of bf16 / float32 may begin at any element but for this: codes at multiples of 16 bytes, scales of 4.  Sizes are at most
+ * 2^28, K at most 2^24.  The calls use no workspace: those on different streams may overlap, and all may be captured into a graph. */
+enum { PVF_MX_E4M3 = 0, PVF_MX_E2M1 = 1 };
+
+/* codes, scales = x [M, K] (dtype PVF_F32 / PVF_BF16) in format fmt. */
+pvf_status pvf_quant_mx(void *stream, int32_t dtype, const void *x, int32_t fmt, void *codes, void *scales, int32_t M, int32_t K);
+
+/* h = x + residual (residual NULL: h = x), rounded to dtype; sum[M, d] = h (NULL: not stored; may alias x or residual);
+ * codes, scales (PVF_MX_E4M3) = (h / sqrt(mean(h^2) + eps)) * gain, evaluated in float32 with 1 / sqrt(...) taken in float64 and rounded. */
+pvf_status pvf_add_rmsnorm_mx(void *stream, int32_t dtype, const void *x, const void *residual, const void *gain, void *sum,
+                              void *codes, void *scales, int32_t M, int32_t d, float eps);
+
+/* C[M,N] = A[M,K] * W[N,K]^T (+ residual[M,N]); A in PVF_MX_E4M3, W in w_fmt, C and residual in dtype.  residual may be NULL and may
+ * alias C.  Sums are kept in float32, but for PVF_BF16 results (and pvf_gemm_mx_swiglu) the scaled matrix instruction first adds groups of 8
+ * neighbouring k, whose products it cuts off 13 bits below the group's largest (1.5e-5 of a result on random operands). */
+pvf_status pvf_gemm_mx(void *stream, int32_t w_fmt, int32_t dtype, const void *A, const void *a_scales, const void *W,
+                       const void *w_scales, void *C, const void *residual, int32_t M, int32_t N, int32_t K);
+
+/* act[M, ff] = silu(A W_gate^T) * (A W_up^T) in PVF_MX_E4M3, the operand of the down projection; W [2*ff, K] (rows gate | up) in w_fmt.
+ * The float32 products are quantised without a rounding in between. */
+pvf_status pvf_gemm_mx_swiglu(void *stream, int32_t w_fmt, const void *A, const void *a_scales, const void *W, const void *w_scales,
+                              void *act, void *act_scales, int32_t M, int32_t ff, int32_t K);
+
+/* C[M,N] = x[M,K] * W[N,K]^T (+ residual[M,N]); x, C and residual in dtype, W in PVF_MX_E2M1: rows as they are against 4-bit weights,
+ * for single tokens and few rows.  residual may be NULL and may alias C.  Sums are kept in float32 for both types. */
+pvf_status pvf_gemm_w4(void *stream, int32_t dtype, const void *x, const void *W, const void *w_scales, void *C,
+                       const void *residual, int32_t M, int32_t N, int32_t K);
+
 /* In-place rotary embedding of the q and k thirds of qkv [S*T, 3*d] (row m is canvas
  * position m % T), then out[S*T, d] = softmax(q k^T / sqrt(d_head)) v per canvas and head,
  * over all T keys.

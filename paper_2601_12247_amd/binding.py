@@ -17,6 +17,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libpvf.so")
 
 PVF_F32, PVF_BF16 = 0, 1
+MX_E4M3, MX_E2M1 = 0, 1   # PVF_MX_E4M3, PVF_MX_E2M1
 PVF_ROUTES_PLAN, PVF_ROUTES_AR, PVF_ROUTES_CAL, PVF_ROUTES_XRANDOM, PVF_ROUTES_XPLANNING = 1, 2, 4, 8, 16
 PVF_ROUTE_NONE, PVF_ROUTE_PLAN, PVF_ROUTE_AR, PVF_ROUTE_CAL = 0, 1, 2, 3
 ROUTE_NONE, ROUTE_PLAN, ROUTE_AR = 0, 1, 2
@@ -30,7 +31,7 @@ EXPORTS = ["pvf_create", "pvf_destroy", "pvf_last_error", "pvf_workspace_bytes",
            "pvf_epilogue", "pvf_round", "pvf_state_init", "pvf_decode", "pvf_stage1", "pvf_gemm",
            "pvf_gemm_swiglu", "pvf_rmsnorm", "pvf_rope_attention", "pvf_fill_normal", "pvf_entropy",
            "pvf_plan_vocab_select", "pvf_qkv_attention", "pvf_rope_attention_noalloc", "pvf_round_sync", "pvf_ctx_gemm",
-           "pvf_ctx_gemm_swiglu"]
+           "pvf_ctx_gemm_swiglu", "pvf_quant_mx", "pvf_add_rmsnorm_mx", "pvf_gemm_mx", "pvf_gemm_mx_swiglu", "pvf_gemm_w4"]
 
 
 class PvfError(RuntimeError):
@@ -137,6 +138,15 @@ def lib() -> C.CDLL:
         L.pvf_rope_attention_noalloc.argtypes = L.pvf_rope_attention.argtypes
         L.pvf_qkv_attention.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                         C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_float]
+        L.pvf_quant_mx.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32]
+        L.pvf_add_rmsnorm_mx.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                         C.c_void_p, C.c_int32, C.c_int32, C.c_float]
+        L.pvf_gemm_mx.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                  C.c_void_p, C.c_int32, C.c_int32, C.c_int32]
+        L.pvf_gemm_mx_swiglu.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                         C.c_void_p, C.c_int32, C.c_int32, C.c_int32]
+        L.pvf_gemm_w4.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                  C.c_int32, C.c_int32, C.c_int32]
         L.pvf_fill_normal.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_uint64,
                                       C.c_float, C.c_float]
         for name in EXPORTS:
@@ -415,6 +425,112 @@ def rmsnorm(x: torch.Tensor, gain: torch.Tensor, eps: float) -> torch.Tensor:
     M, d = x.shape
     out = torch.empty_like(x)
     _check(lib().pvf_rmsnorm(_stream(), _dtype_code(x.dtype), _ptr(x), _ptr(gain), _ptr(out), M, d, eps))
+    return out
+
+
+# ---- block-scaled rows -------------------------------------------------------------------
+# Codes are float8_e4m3fn tensors [rows, Kp], or uint8 [rows, Kp / 2] with two e2m1 codes a byte (even element low); scales are
+# float8_e8m0fnu tensors [Kp / 128, rows, 4]; Kp = mx_width(K).
+def mx_width(K: int) -> int:
+    return (K + 127) // 128 * 128
+
+
+def mx_empty(rows: int, K: int, fmt: int = MX_E4M3, device="cuda"):
+    """Uninitialised codes and scales for rows of K elements."""
+    Kp = mx_width(K)
+    codes = (torch.empty(rows, Kp, dtype=torch.float8_e4m3fn, device=device) if fmt == MX_E4M3 else
+             torch.empty(rows, Kp // 2, dtype=torch.uint8, device=device))
+    return codes, torch.empty(Kp // 128, rows, 4, dtype=torch.float8_e8m0fnu, device=device)
+
+
+def _mx_format(codes: torch.Tensor, scales: torch.Tensor, rows: int, Kp: int) -> int:
+    """The format of checked codes and scales."""
+    fmt = MX_E4M3 if codes.dtype == torch.float8_e4m3fn else MX_E2M1
+    assert fmt == MX_E4M3 or codes.dtype == torch.uint8, f"codes are float8_e4m3fn or uint8, not {codes.dtype}"
+    assert codes.shape == (rows, Kp if fmt == MX_E4M3 else Kp // 2), f"codes of {rows} rows of {Kp}: {tuple(codes.shape)}"
+    assert scales.dtype == torch.float8_e8m0fnu and scales.shape == (Kp // 128, rows, 4), \
+        f"scales of {rows} rows of {Kp}: {scales.dtype} {tuple(scales.shape)}"
+    return fmt
+
+
+def _mx_call(fn, tensors, *args) -> None:
+    """fn(stream, *args) on the device that the tensors are on."""
+    dev = tensors[0].device
+    for t in tensors:
+        assert t is None or (t.device == dev and t.is_contiguous()), "contiguous tensors on one device required"
+    assert dev.type == "cuda", "device-resident tensors required"
+    if dev.index != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            return _check(fn(_stream(), *args))
+    _check(fn(_stream(), *args))
+
+
+def _p(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def quant_mx(x: torch.Tensor, fmt: int = MX_E4M3, out=None):
+    """(codes, scales) of rows x [M, K] in MX_E4M3 or MX_E2M1; out = (codes, scales) to write into (mx_empty)."""
+    M, K = x.shape
+    codes, scales = mx_empty(M, K, fmt, x.device) if out is None else out
+    assert _mx_format(codes, scales, M, mx_width(K)) == fmt, "out is of the other format"
+    _mx_call(lib().pvf_quant_mx, (x, codes, scales), _dtype_code(x.dtype), x.data_ptr(), fmt, codes.data_ptr(), scales.data_ptr(), M, K)
+    return codes, scales
+
+
+def add_rmsnorm_mx(x: torch.Tensor, gain: torch.Tensor, eps: float, residual: Optional[torch.Tensor] = None,
+                   sum_out: Optional[torch.Tensor] = None, out=None):
+    """(h, codes, scales): h = x + residual (x itself without a residual), codes and scales (MX_E4M3) of RMSNorm(h) * gain.
+    sum_out (may be x or residual) receives h; out = (codes, scales)."""
+    M, d = x.shape
+    codes, scales = mx_empty(M, d, MX_E4M3, x.device) if out is None else out
+    assert _mx_format(codes, scales, M, mx_width(d)) == MX_E4M3, "the norm writes MX_E4M3"
+    if residual is not None and sum_out is None:
+        sum_out = torch.empty_like(x)
+    assert gain.shape == (d,) and gain.dtype == x.dtype
+    assert all(t is None or (t.shape == x.shape and t.dtype == x.dtype) for t in (residual, sum_out))
+    _mx_call(lib().pvf_add_rmsnorm_mx, (x, residual, gain, sum_out, codes, scales), _dtype_code(x.dtype), x.data_ptr(), _p(residual),
+             gain.data_ptr(), _p(sum_out), codes.data_ptr(), scales.data_ptr(), M, d, eps)
+    return x if sum_out is None else sum_out, codes, scales
+
+
+def gemm_mx(A: torch.Tensor, a_scales: torch.Tensor, W: torch.Tensor, w_scales: torch.Tensor,
+            residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """A W^T (+ residual) of MX_E4M3 rows A and weights W in either format; `dtype` where neither out nor residual has one."""
+    (M, Kp), N = A.shape, W.shape[0]
+    assert _mx_format(A, a_scales, M, Kp) == MX_E4M3 and Kp % 128 == 0, "A is MX_E4M3"
+    fmt = _mx_format(W, w_scales, N, Kp)
+    if out is None:
+        out = torch.empty(M, N, dtype=dtype if residual is None else residual.dtype, device=A.device)
+    assert out.shape == (M, N) and (residual is None or (residual.shape == (M, N) and residual.dtype == out.dtype))
+    _mx_call(lib().pvf_gemm_mx, (A, a_scales, W, w_scales, out, residual), fmt, _dtype_code(out.dtype), A.data_ptr(), a_scales.data_ptr(),
+             W.data_ptr(), w_scales.data_ptr(), out.data_ptr(), _p(residual), M, N, Kp)
+    return out
+
+
+def gemm_mx_swiglu(A: torch.Tensor, a_scales: torch.Tensor, W: torch.Tensor, w_scales: torch.Tensor, out=None):
+    """(codes, scales), MX_E4M3, of silu(A W_gate^T) * (A W_up^T), W [2 * ff, Kp] (rows gate | up); out = (codes, scales)."""
+    (M, Kp), ff = A.shape, W.shape[0] // 2
+    assert _mx_format(A, a_scales, M, Kp) == MX_E4M3 and Kp % 128 == 0, "A is MX_E4M3"
+    assert W.shape[0] == 2 * ff, "rows gate | up"
+    fmt = _mx_format(W, w_scales, 2 * ff, Kp)
+    codes, scales = mx_empty(M, ff, MX_E4M3, A.device) if out is None else out
+    assert _mx_format(codes, scales, M, mx_width(ff)) == MX_E4M3, "the activation is MX_E4M3"
+    _mx_call(lib().pvf_gemm_mx_swiglu, (A, a_scales, W, w_scales, codes, scales), fmt, A.data_ptr(), a_scales.data_ptr(), W.data_ptr(),
+             w_scales.data_ptr(), codes.data_ptr(), scales.data_ptr(), M, ff, Kp)
+    return codes, scales
+
+
+def gemm_w4(x: torch.Tensor, W: torch.Tensor, w_scales: torch.Tensor, residual: Optional[torch.Tensor] = None,
+            out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x W^T (+ residual) of rows x [M, K] (float32 / bfloat16) and MX_E2M1 weights."""
+    (M, K), N = x.shape, W.shape[0]
+    assert _mx_format(W, w_scales, N, mx_width(K)) == MX_E2M1, "W is MX_E2M1"
+    if out is None:
+        out = torch.empty(M, N, dtype=x.dtype, device=x.device)
+    assert all(t is None or (t.shape == (M, N) and t.dtype == x.dtype) for t in (out, residual))
+    _mx_call(lib().pvf_gemm_w4, (x, W, w_scales, out, residual), _dtype_code(x.dtype), x.data_ptr(), W.data_ptr(), w_scales.data_ptr(),
+             out.data_ptr(), _p(residual), M, N, K)
     return out
 
 

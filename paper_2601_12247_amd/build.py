@@ -22,6 +22,8 @@ SOURCES = [
     "gemm_simple.hip",
     "gemm_f32.hip",
     "gemm_mfma.hip",
+    "gemm_mx.hip",
+    "mx_rows.hip",
     "attention_simple.hip",
     "attention_f32.hip",
     "attention_mfma.hip",

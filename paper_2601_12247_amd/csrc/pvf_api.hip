@@ -1,6 +1,7 @@
 // C-ABI entry points of libpvf: argument validation, workspace, and the order of launches of
 // one PVF round (Algorithm 1 with one batched forward per round) and of the decode loop.
 #include "common.h"
+#include "mx.h"
 
 #include <chrono>
 #include <cmath>
@@ -1045,6 +1046,84 @@ extern "C" pvf_status pvf_rmsnorm(void *stream, int32_t dtype, const void *x, co
   if (check_dtype(dtype) != PVF_OK) return PVF_EINVAL;
   PVF_REQUIRE(nullptr, x && gain && out && M >= 0 && d > 0, PVF_EINVAL, "pvf_rmsnorm: bad argument");
   return launch_rmsnorm(nullptr, (hipStream_t)stream, dtype, x, gain, out, M, d, eps);
+}
+
+static pvf_status check_mx(const char *call, const void *codes, const void *scales) {
+  PVF_REQUIRE(nullptr, codes && scales, PVF_EINVAL, "%s: codes or scales are NULL", call);
+  PVF_REQUIRE(nullptr, (uintptr_t)codes % 16 == 0 && (uintptr_t)scales % 4 == 0, PVF_EINVAL, "%s: codes begin at multiples of 16 bytes, scales of 4", call);
+  return PVF_OK;
+}
+static pvf_status check_mx_sizes(const char *call, int32_t M, int32_t N, int32_t K) {
+  PVF_REQUIRE(nullptr, M >= 0 && N >= 0 && K > 0, PVF_EINVAL, "%s: bad size (%d, %d, %d)", call, M, N, K);
+  PVF_REQUIRE(nullptr, M <= 1 << 28 && N <= 1 << 28 && K <= 1 << 24, PVF_ESHAPE, "%s: size (%d, %d, %d) beyond 2^28 rows or 2^24 elements", call, M, N, K);
+  return PVF_OK;
+}
+static bool at_element(int dtype, const void *p) { return (uintptr_t)p % (dtype == PVF_F32 ? 4 : 2) == 0; }
+
+extern "C" pvf_status pvf_quant_mx(void *stream, int32_t dtype, const void *x, int32_t fmt, void *codes, void *scales, int32_t M, int32_t K) {
+  if (check_dtype(dtype) != PVF_OK) return PVF_EINVAL;
+  PVF_REQUIRE(nullptr, fmt == PVF_MX_E4M3 || fmt == PVF_MX_E2M1, PVF_EINVAL, "pvf_quant_mx: fmt=%d", fmt);
+  if (const pvf_status st = check_mx_sizes("pvf_quant_mx", M, 0, K)) return st;
+  if (M == 0) return PVF_OK;
+  PVF_REQUIRE(nullptr, x && at_element(dtype, x), PVF_EINVAL, "pvf_quant_mx: x is NULL or between elements");
+  if (const pvf_status st = check_mx("pvf_quant_mx", codes, scales)) return st;
+  return launch_quant_mx((hipStream_t)stream, dtype, x, fmt, codes, scales, M, K);
+}
+
+extern "C" pvf_status pvf_add_rmsnorm_mx(void *stream, int32_t dtype, const void *x, const void *residual, const void *gain, void *sum,
+                                         void *codes, void *scales, int32_t M, int32_t d, float eps) {
+  if (check_dtype(dtype) != PVF_OK) return PVF_EINVAL;
+  if (const pvf_status st = check_mx_sizes("pvf_add_rmsnorm_mx", M, 0, d)) return st;
+  PVF_REQUIRE(nullptr, eps >= 0.f, PVF_EINVAL, "pvf_add_rmsnorm_mx: eps=%g", eps);
+  if (M == 0) return PVF_OK;
+  PVF_REQUIRE(nullptr, x && gain && at_element(dtype, x) && at_element(dtype, residual) && at_element(dtype, gain) && at_element(dtype, sum),
+              PVF_EINVAL, "pvf_add_rmsnorm_mx: a tensor is NULL or between elements");
+  if (const pvf_status st = check_mx("pvf_add_rmsnorm_mx", codes, scales)) return st;
+  return launch_add_rmsnorm_mx((hipStream_t)stream, dtype, x, residual, gain, sum, codes, scales, M, d, eps);
+}
+
+extern "C" pvf_status pvf_gemm_mx(void *stream, int32_t w_fmt, int32_t dtype, const void *A, const void *a_scales, const void *W,
+                                  const void *w_scales, void *C, const void *residual, int32_t M, int32_t N, int32_t K) {
+  if (check_dtype(dtype) != PVF_OK) return PVF_EINVAL;
+  PVF_REQUIRE(nullptr, w_fmt == PVF_MX_E4M3 || w_fmt == PVF_MX_E2M1, PVF_EINVAL, "pvf_gemm_mx: w_fmt=%d", w_fmt);
+  if (const pvf_status st = check_mx_sizes("pvf_gemm_mx", M, N, K)) return st;
+  if (M == 0 || N == 0) return PVF_OK;
+  if (const pvf_status st = check_mx("pvf_gemm_mx (A)", A, a_scales)) return st;
+  if (const pvf_status st = check_mx("pvf_gemm_mx (W)", W, w_scales)) return st;
+  PVF_REQUIRE(nullptr, C && at_element(dtype, C) && at_element(dtype, residual), PVF_EINVAL, "pvf_gemm_mx: C is NULL or C or residual between elements");
+  MxGemm g;
+  g.A = A; g.a_scales = (const uint8_t *)a_scales; g.W = W; g.w_scales = (const uint8_t *)w_scales;
+  g.C = C; g.residual = residual; g.M = M; g.N = N; g.K = K; g.w_fmt = w_fmt; g.dtype = dtype;
+  return launch_gemm_mx((hipStream_t)stream, g);
+}
+
+extern "C" pvf_status pvf_gemm_mx_swiglu(void *stream, int32_t w_fmt, const void *A, const void *a_scales, const void *W, const void *w_scales,
+                                         void *act, void *act_scales, int32_t M, int32_t ff, int32_t K) {
+  PVF_REQUIRE(nullptr, w_fmt == PVF_MX_E4M3 || w_fmt == PVF_MX_E2M1, PVF_EINVAL, "pvf_gemm_mx_swiglu: w_fmt=%d", w_fmt);
+  if (const pvf_status st = check_mx_sizes("pvf_gemm_mx_swiglu", M, ff, K)) return st;
+  PVF_REQUIRE(nullptr, ff <= 1 << 24, PVF_ESHAPE, "pvf_gemm_mx_swiglu: ff=%d beyond 2^24", ff);
+  if (M == 0 || ff == 0) return PVF_OK;
+  if (const pvf_status st = check_mx("pvf_gemm_mx_swiglu (A)", A, a_scales)) return st;
+  if (const pvf_status st = check_mx("pvf_gemm_mx_swiglu (W)", W, w_scales)) return st;
+  if (const pvf_status st = check_mx("pvf_gemm_mx_swiglu (act)", act, act_scales)) return st;
+  MxGemm g;
+  g.A = A; g.a_scales = (const uint8_t *)a_scales; g.W = W; g.w_scales = (const uint8_t *)w_scales;
+  g.C = act; g.c_scales = (uint8_t *)act_scales; g.M = M; g.N = ff; g.K = K; g.w_fmt = w_fmt; g.dtype = PVF_BF16;
+  return launch_gemm_mx((hipStream_t)stream, g);
+}
+
+extern "C" pvf_status pvf_gemm_w4(void *stream, int32_t dtype, const void *x, const void *W, const void *w_scales, void *C,
+                                  const void *residual, int32_t M, int32_t N, int32_t K) {
+  if (check_dtype(dtype) != PVF_OK) return PVF_EINVAL;
+  if (const pvf_status st = check_mx_sizes("pvf_gemm_w4", M, N, K)) return st;
+  if (M == 0 || N == 0) return PVF_OK;
+  PVF_REQUIRE(nullptr, x && at_element(dtype, x), PVF_EINVAL, "pvf_gemm_w4: x is NULL or between elements");
+  if (const pvf_status st = check_mx("pvf_gemm_w4 (W)", W, w_scales)) return st;
+  PVF_REQUIRE(nullptr, C && at_element(dtype, C) && at_element(dtype, residual), PVF_EINVAL, "pvf_gemm_w4: C is NULL or C or residual between elements");
+  MxGemm g;
+  g.A = x; g.W = W; g.w_scales = (const uint8_t *)w_scales;
+  g.C = C; g.residual = residual; g.M = M; g.N = N; g.K = K; g.w_fmt = PVF_MX_E2M1; g.dtype = dtype;
+  return launch_gemm_mx((hipStream_t)stream, g);
 }
 
 // Builds the rotary table on the host for this call, so it synchronises the stream and
