@@ -454,15 +454,19 @@ def _mx_format(codes: torch.Tensor, scales: torch.Tensor, rows: int, Kp: int) ->
 
 
 def _mx_call(fn, tensors, *args) -> None:
-    """fn(stream, *args) on the device that the tensors are on."""
-    dev = tensors[0].device
+    """fn(stream, *args) on the device that the tensors are on.  Costs a microsecond beside the launch, so the stream is asked for as a
+    number: torch.cuda.current_stream() takes three."""
+    dev = tensors[0].get_device()
     for t in tensors:
-        assert t is None or (t.device == dev and t.is_contiguous()), "contiguous tensors on one device required"
-    assert dev.type == "cuda", "device-resident tensors required"
-    if dev.index != torch.cuda.current_device():
+        assert t is None or (t.get_device() == dev and t.is_contiguous()), "contiguous tensors on one device required"
+    assert dev >= 0, "device-resident tensors required"
+    if dev != torch.cuda.current_device():
         with torch.cuda.device(dev):
-            return _check(fn(_stream(), *args))
-    _check(fn(_stream(), *args))
+            status = fn(torch._C._cuda_getCurrentRawStream(dev), *args)
+    else:
+        status = fn(torch._C._cuda_getCurrentRawStream(dev), *args)
+    if status:
+        _check(status)
 
 
 def _p(t: Optional[torch.Tensor]) -> Optional[int]:

@@ -31,7 +31,7 @@ typedef int intx8 __attribute__((ext_vector_type(8)));
 enum Rows { kRowsMx, kRowsMxExact, kRowsBf16, kRowsF32 };   // what multiplies what (table above)
 enum Out { kOutBf16, kOutF32, kOutSwiglu };
 
-template <int WF> constexpr int code_bytes(int elements) { return WF == PVF_MX_E4M3 ? elements : elements / 2; }
+constexpr bool codes_in(int rows) { return rows == kRowsMx || rows == kRowsMxExact; }
 
 __device__ __forceinline__ float silu_f(float g) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
 
@@ -134,163 +134,7 @@ __device__ __forceinline__ void store_act(floatx4 g0, floatx4 g1, floatx4 u0, fl
   if (g == 0) p.c_scales[((int64_t)(c0 / kMxStage) * p.M + m) * 4 + c0 / kMxBlock % 4] = (uint8_t)b;
 }
 
-// ---- few rows -----------------------------------------------------------------------------------------------------
-// A workgroup computes 16 MT rows x 16 NT columns; its KW waves take the stages of 128 k in turn, operands straight from memory into the
-// registers of the instruction, and add their sums through LDS.  Weights are read once for all rows of a workgroup.
-template <int ROWS, int WF, int OUT, int MT, int NT, int KW>
-__global__ void __launch_bounds__(64 * KW)
-gemm_mx_rows_kernel(MxGemm p, uint32_t n_tiles) {
-  constexpr bool kSwiglu = OUT == kOutSwiglu;
-  constexpr int kPlanes = ROWS == kRowsF32 ? 3 : 1;
-  static_assert(!kSwiglu || NT == 4, "SwiGLU: two column tiles of gate, two of up, a block of 32 outputs");
-  __shared__ floatx4 sums[KW][NT * MT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-  const int M = p.M, N = p.N, K = p.K, Kp = (K + kMxStage - 1) / kMxStage * kMxStage, nk = Kp / kMxStage;
-  const int w_rows = kSwiglu ? 2 * N : N;
-  const int n0 = (int)(blockIdx.x % n_tiles) * (kSwiglu ? 32 : 16 * NT), m0 = (int)(blockIdx.x / n_tiles) * (16 * MT);
-  const uint8_t *w_ptr[NT], *a_ptr[MT];
-  uint32_t w_s[NT], a_s[MT];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int n = kSwiglu ? min(n0 + (nt & 1) * 16 + r, N - 1) + (nt >= 2 ? N : 0) : min(n0 + nt * 16 + r, N - 1);
-    w_ptr[nt] = (const uint8_t *)p.W + (int64_t)n * code_bytes<WF>(Kp);
-    w_s[nt] = n * 4 + g;
-  }
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    const int m = min(m0 + mt * 16 + r, M - 1);
-    a_ptr[mt] = (const uint8_t *)p.A + (ROWS == kRowsBf16 ? (int64_t)m * K * 2 : ROWS == kRowsF32 ? (int64_t)m * K * 4 : (int64_t)m * Kp);
-    a_s[mt] = m * 4 + g;
-  }
-  floatx4 acc[NT][MT];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) acc[nt][mt] = floatx4{0.f, 0.f, 0.f, 0.f};
-
-  for (int kt = wave; kt < nk; kt += KW) {
-    if constexpr (ROWS == kRowsMx) {
-      intx8 w[NT], a[MT];
-      int ws[NT], as[MT];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        if (WF == PVF_MX_E4M3) {
-          const intx4 *q = reinterpret_cast<const intx4 *>(w_ptr[nt] + kt * 128 + 16 * g);
-          w[nt] = join(q[0], q[4]);
-        } else {
-          const intx4 q = *reinterpret_cast<const intx4 *>(w_ptr[nt] + kt * 64 + 16 * g);
-          w[nt] = join(q, intx4{0, 0, 0, 0});
-        }
-        ws[nt] = p.w_scales[(int64_t)kt * w_rows * 4 + w_s[nt]];
-      }
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        const intx4 *q = reinterpret_cast<const intx4 *>(a_ptr[mt] + kt * 128 + 16 * g);
-        a[mt] = join(q[0], q[4]);
-        as[mt] = p.a_scales[(int64_t)kt * M * 4 + a_s[mt]];
-      }
-#ifdef __HIP_DEVICE_COMPILE__
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-          acc[nt][mt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w[nt], a[mt], acc[nt][mt], WF == PVF_MX_E4M3 ? 0 : 4, 0, 0, ws[nt], 0, as[mt]);
-#endif
-    } else {
-      // four instructions of 32 k: lane g has elements 32 g + 8 j .. + 7 of the stage in the j-th, all of one block
-      intx4 w[NT][WF == PVF_MX_E4M3 ? 2 : 1];
-      float ws[NT];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const intx4 *q = reinterpret_cast<const intx4 *>(w_ptr[nt] + code_bytes<WF>(kt * 128 + 32 * g));
-        w[nt][0] = q[0];
-        if (WF == PVF_MX_E4M3) w[nt][WF == PVF_MX_E4M3 ? 1 : 0] = q[1];
-        ws[nt] = byte_scale(p.w_scales[(int64_t)kt * w_rows * 4 + w_s[nt]]);
-      }
-      bf16x8 a[MT][4][kPlanes];
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        const int k = kt * 128 + 32 * g;
-        if constexpr (ROWS == kRowsMxExact) {
-          const intx4 *q = reinterpret_cast<const intx4 *>(a_ptr[mt] + k);
-          const intx4 q0 = q[0], q1 = q[1];
-          const float as = byte_scale(p.a_scales[(int64_t)kt * M * 4 + a_s[mt]]);
-          a[mt][0][0] = decode_e4m3(q0[0], q0[1], as); a[mt][1][0] = decode_e4m3(q0[2], q0[3], as);
-          a[mt][2][0] = decode_e4m3(q1[0], q1[1], as); a[mt][3][0] = decode_e4m3(q1[2], q1[3], as);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int kj = k + 8 * j;
-            if constexpr (ROWS == kRowsBf16) {
-              a[mt][j][0] = __builtin_bit_cast(bf16x8, load8_raw((const bf16_t *)a_ptr[mt] + min(kj, K), K - kj));
-            } else {
-              float x[8];
-              load8((const float *)a_ptr[mt] + min(kj, K), K - kj, x);
-              split3(x, a[mt][j]);
-            }
-          }
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const bf16x8 wf = WF == PVF_MX_E4M3 ? decode_e4m3(w[nt][WF == PVF_MX_E4M3 ? j >> 1 : 0][j * 2 & 3], w[nt][WF == PVF_MX_E4M3 ? j >> 1 : 0][(j * 2 & 3) + 1], ws[nt])
-                                              : decode_e2m1(w[nt][0][j], ws[nt]);
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int q = kPlanes - 1; q >= 0; --q)
-              acc[nt][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, a[mt][j][q], acc[nt][mt], 0, 0, 0);
-        }
-    }
-  }
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) sums[wave][nt * MT + mt][lane] = acc[nt][mt];
-  __syncthreads();
-  auto total = [&](int t, int l) {                           // in the order of the waves
-    floatx4 s = sums[0][t][l];
-#pragma unroll
-    for (int w = 1; w < KW; ++w) s += sums[w][t][l];
-    return s;
-  };
-  if constexpr (kSwiglu) {
-    const int Np = (N + kMxStage - 1) / kMxStage * kMxStage;
-    for (int mt = wave; mt < MT; mt += KW) {
-      const int m = m0 + mt * 16 + r;
-      store_act(total(mt, lane), total(MT + mt, lane), total(2 * MT + mt, lane), total(3 * MT + mt, lane), m < M, m, n0, g, p, Np);
-    }
-  } else {
-    using T = std::conditional_t<OUT == kOutF32, float, bf16_t>;
-    for (int t = wave; t < NT * MT; t += KW) {
-      const int m = m0 + t % MT * 16 + r;
-      const floatx4 s = total(t, lane);
-      if (m < M) store_row4<T>(s, m, n0 + t / MT * 16 + 4 * g, p);
-    }
-  }
-}
-
-template <int ROWS, int WF, int OUT>
-pvf_status run_rows(hipStream_t s, const MxGemm &p) {
-  constexpr int NT = OUT == kOutSwiglu ? 4 : 1, KW = 4;
-  const uint32_t n_tiles = OUT == kOutSwiglu ? (uint32_t)(mx_width(p.N) / 32) : (p.N + 16 * NT - 1) / (16 * NT);
-  auto go = [&](auto mt) -> pvf_status {
-    constexpr int MT = decltype(mt)::value;
-    const int64_t grid = (int64_t)n_tiles * ((p.M + 16 * MT - 1) / (16 * MT));
-    PVF_REQUIRE(nullptr, grid <= INT32_MAX, PVF_ESHAPE, "%d x %d results are too many for a launch", p.M, p.N);
-    gemm_mx_rows_kernel<ROWS, WF, OUT, MT, NT, KW><<<(uint32_t)grid, 64 * KW, 0, s>>>(p, n_tiles);
-    PVF_LAUNCH_CHECK(nullptr, "gemm_mx");
-    return PVF_OK;
-  };
-  if (p.M <= 16) return go(std::integral_constant<int, 1>{});
-  if (p.M <= 32 || ROWS == kRowsF32) return go(std::integral_constant<int, 2>{});
-  return go(std::integral_constant<int, 4>{});
-}
-
-
-// ---- many rows ----------------------------------------------------------------------------------------------------
+// ---- the kernel ---------------------------------------------------------------------------------------------------
 typedef __attribute__((address_space(1))) const void gptr_t;
 typedef __attribute__((address_space(3))) void lptr_t;
 
@@ -302,38 +146,47 @@ template <int N> __device__ __forceinline__ void wait_vmcnt() {
 
 struct TileMap { int tiles_m, tiles_n, group_m; };
 
-// Bytes of LDS that a stage of 128 k takes: operand rows, then their scale dwords.
-template <int ROWS> constexpr int a_stage_bytes(int BM) { return ROWS == kRowsBf16 ? BM * 256 : ROWS == kRowsF32 ? BM * 768 : BM * 128; }
-constexpr bool codes_in(int ROWS) { return ROWS == kRowsMx || ROWS == kRowsMxExact; }
+// Where 16-byte chunk c of a row lies in LDS rows of R bytes: the reads of an operand (16 rows, one chunk each) touch every bank once.
+template <int R> __device__ __forceinline__ int swizzle(int row) { return R >= 256 ? row & 15 : R == 128 ? row >> 1 & 7 : row >> 2 & 3; }
 
-// A workgroup computes BM x BN results, a wave BM / WM x BN / WN of them.  Stages of 128 k go through a ring of kStages slots of LDS: codes and scales
-// straight from memory (a 16-byte chunk of a row sits at chunk position ^ swizzle(row), chosen by the lane's source address, so that the
-// reads of 16 rows touch every bank once), rows of bf16 / float32 through registers, where float32 is split into its three parts.
-template <int ROWS, int WF, int OUT, int BM, int BN, int WM, int WN, int kStages>
-__global__ void __launch_bounds__(64 * WM * WN)
-gemm_mx_tile_kernel(MxGemm p, TileMap tm) {
+// Sizes of an instance.
+template <int ROWS, int WF, int BM, int BN, int WM, int WN, int WK, int kStages, int AR = BM> struct Shape {
+  static constexpr int kASize = codes_in(ROWS) ? 1 : ROWS == kRowsBf16 ? 2 : 4;
+  static constexpr int kThreads = 64 * WM * WN * WK, kWaves = WM * WN * WK, MT = BM / WM / 16, NT = BN / WN / 16;
+  static constexpr int kARow = 128 * WK * kASize, kWRow = (WF == PVF_MX_E4M3 ? 128 : 64) * WK;           // LDS bytes of a row and stage
+  static constexpr int kABytes = AR * kARow, kWBytes = BN * kWRow;
+  static constexpr int kAUnits = codes_in(ROWS) ? (AR * WK + 63) / 64 : 0, kWUnits = (BN * WK + 63) / 64;   // scale dwords, 64 at a time
+  static constexpr int kSBytes = (kAUnits + kWUnits) * 256, kStage = kABytes + kWBytes + kSBytes;
+  static constexpr int kRing = kStages * kStage, kSums = WK > 1 ? WK * BM * BN * 4 : 0, kLds = kRing > kSums ? kRing : kSums;
+};
+
+// A workgroup computes BM x BN results.  A stage is 128 WK elements of k: wave (wm, wn, wk) multiplies the wk-th 128 of them for its
+// BM / WM x BN / WN results, and with WK > 1 the waves' sums are added through LDS at the end.  Stages go through a ring of kStages slots of LDS, straight
+// from memory (whole 128-byte lines per request: loads of 64-byte pieces straight into registers reached half the rate), one barrier
+// a stage.  Rows of bf16 / float32 that do not begin at 16-byte chunks go through registers (kDirect = false).
+template <int ROWS, int WF, int OUT, int BM, int BN, int WM, int WN, int WK, int kStages, int AR, bool kDirect>
+__global__ void __launch_bounds__(64 * WM * WN * WK)
+gemm_mx_kernel(MxGemm p, TileMap tm) {
+  using S = Shape<ROWS, WF, BM, BN, WM, WN, WK, kStages, AR>;
   constexpr bool kSwiglu = OUT == kOutSwiglu, kCodes = codes_in(ROWS), kW8 = WF == PVF_MX_E4M3;
-  constexpr int kThreads = 64 * WM * WN, kWaves = WM * WN, WTM = BM / WM, WTN = BN / WN, MT = WTM / 16, NT = WTN / 16;
+  constexpr int kThreads = S::kThreads, kWaves = S::kWaves, MT = S::MT, NT = S::NT, kASize = S::kASize;
+  constexpr int kACpr = S::kARow / 16, kWCpr = S::kWRow / 16;                // chunks of a row
+  constexpr int kAChunks = AR * kACpr, kWChunks = BN * kWCpr, LA = (kAChunks + kThreads - 1) / kThreads, LW = (kWChunks + kThreads - 1) / kThreads;
+  constexpr int LS = (S::kAUnits + S::kWUnits + kWaves - 1) / kWaves;
+  constexpr int kLoads = (kDirect ? LA : 0) + LW + LS;       // load instructions of a thread and stage that go straight to LDS
   constexpr int kPlanes = ROWS == kRowsF32 ? 3 : 1;
-  constexpr int kABytes = a_stage_bytes<ROWS>(BM), kWRow = kW8 ? 128 : 64, kWBytes = BN * kWRow;
-  constexpr int kASlots = kCodes ? kStages : 2;
-  constexpr int kAScale = 0, kWScale = kCodes ? BM * 4 : 0, kScaleBytes = kWScale + BN * 4;
-  constexpr int kWBase = kASlots * kABytes, kSBase = kWBase + kStages * kWBytes;
-  // load instructions of a thread and stage
-  constexpr int LA = kCodes ? BM * 8 / kThreads : 0, LW = kWBytes / 16 / kThreads;
-  constexpr int kScaleUnits = kScaleBytes / 256, LS = (kScaleUnits + kWaves - 1) / kWaves, kLoads = LA + LW + LS;
-  constexpr int LX = kCodes ? 0 : BM * 16 / kThreads;       // 8-element chunks of rows that a thread stages
-  static_assert(BM % (16 * WM) == 0 && BN % (16 * WN) == 0 && (kCodes ? BM * 8 : BM * 16) % kThreads == 0 && kWBytes / 16 % kThreads == 0, "tile shape");
-  static_assert(BM % 64 == 0 && BN % 64 == 0 && (!kSwiglu || WTN == 64), "scale dwords are loaded 64 at a time; a wave has a block of gate and of up");
+  static_assert(BM % (16 * WM) == 0 && BN % (16 * WN) == 0 && kAChunks % 64 == 0 && kWChunks % 64 == 0, "tile shape");
+  static_assert(kDirect || !kCodes, "codes always go straight");
+  static_assert(!kSwiglu || BN / WN == 64, "a wave has a block of gate and the same block of up");
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave / WN, wn = wave % WN, r = lane & 15, g = lane >> 4;
-  const int M = p.M, N = p.N, K = p.K, Kp = (K + kMxStage - 1) / kMxStage * kMxStage, nk = Kp / kMxStage;
+  const int wk = wave / (WM * WN), wm = wave / WN % WM, wn = wave % WN, r = lane & 15, g = lane >> 4;
+  const int M = p.M, N = p.N, K = p.K, Kp = (K + kMxStage - 1) / kMxStage * kMxStage, nk = Kp / kMxStage, ns = (nk + WK - 1) / WK;
 
   // the 32 workgroups that an XCD runs at a time cover a patch of tiles and share operands through its L2
-  const int total = tm.tiles_m * tm.tiles_n, chunk = (total + 7) >> 3;
-  const int L = (int)(blockIdx.x & 7) * chunk + (int)(blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= chunk || L >= total) return;
+  const int total = tm.tiles_m * tm.tiles_n, per_xcd = (total + 7) >> 3;
+  const int L = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= per_xcd || L >= total) return;
   const int band = L / (tm.group_m * tm.tiles_n), within = L - band * (tm.group_m * tm.tiles_n);
   const int band_rows = min(tm.group_m, tm.tiles_m - band * tm.group_m);
   const int tile_n = within / band_rows, tile_m = band * tm.group_m + (within - tile_n * band_rows);
@@ -346,72 +199,64 @@ gemm_mx_tile_kernel(MxGemm p, TileMap tm) {
     const int n = min(n0 + (t >> 6) * 32 + (t & 31), N - 1);
     return (t & 32) ? (int64_t)N + n : n;
   };
-  // ---- sources of this thread's direct loads ----
-  const uint8_t *a_src = nullptr, *w_src[LW], *s_src[LS];
-  int64_t a_step[LA > 0 ? LA : 1] = {};
-  if (kCodes) {
-    const int row = tid / 8, c = (tid % 8) ^ ((row >> 1) & 7);
-    const int64_t first = min(m0 + row, M - 1);
-    a_src = (const uint8_t *)p.A + first * Kp + c * 16;
+  // ---- loads: chunk i * kThreads + tid of an operand tile; behind the end of a row its last chunk again, which is not read.  Every wave has
+  //      as many loads as the others: some repeat one, into the same place ----
+  const uint32_t a_bytes = (uint32_t)((kCodes ? Kp : K) * kASize), w_bytes = kW8 ? Kp : Kp / 2;
+  const uint8_t *a_src[LA], *w_src[LW], *s_src[LS];
+  uint32_t a_at[LA], w_at[LW], s_rows[LS];
+  int s_sub[LS], s_slot[LS];
 #pragma unroll
-    for (int i = 0; i < LA; ++i) a_step[i] = (min(m0 + i * (kThreads / 8) + row, M - 1) - first) * Kp;
+  for (int i = 0; i < LA; ++i) {
+    const int f = (i * kThreads + tid) % kAChunks, row = f / kACpr;
+    a_at[i] = ((f % kACpr) ^ swizzle<S::kARow>(row)) * 16;
+    a_src[i] = (const uint8_t *)p.A + (int64_t)min(m0 + row, M - 1) * a_bytes;
   }
 #pragma unroll
   for (int i = 0; i < LW; ++i) {
-    constexpr int CPR = kWRow / 16;
-    const int row = (i * kThreads + tid) / CPR, c = (tid % CPR) ^ (kW8 ? (row >> 1) & 7 : (row >> 2) & 3);
-    w_src[i] = (const uint8_t *)p.W + w_row(row) * (Kp / (kW8 ? 1 : 2)) + c * 16;
+    const int f = (i * kThreads + tid) % kWChunks, row = f / kWCpr;
+    w_at[i] = ((f % kWCpr) ^ swizzle<S::kWRow>(row)) * 16;
+    w_src[i] = (const uint8_t *)p.W + w_row(row) * w_bytes;
   }
-  int s_slot[LS];
-  int64_t s_step[LS];
 #pragma unroll
-  for (int i = 0; i < LS; ++i) {                             // every wave has as many loads as the others: some repeat a unit
-    const int u = (i * kWaves + wave) % kScaleUnits;
+  for (int i = 0; i < LS; ++i) {
+    const int u = (i * kWaves + wave) % (S::kAUnits + S::kWUnits);
+    const bool of_a = u < S::kAUnits;
+    const int f = (of_a ? u : u - S::kAUnits) * 64 + lane;
+    const int row = of_a ? f % AR : f % BN;
     s_slot[i] = u * 256;
-    const bool of_a = kCodes && u < BM / 64;
-    const int t = (of_a ? u : u - kWScale / 256) * 64 + lane;
-    s_src[i] = of_a ? p.a_scales + (int64_t)min(m0 + t, M - 1) * 4 : p.w_scales + w_row(t) * 4;
-    s_step[i] = (int64_t)(of_a ? M : w_rows) * 4;
+    s_sub[i] = of_a ? f / AR : f / BN;
+    s_rows[i] = of_a ? M : w_rows;
+    s_src[i] = of_a ? p.a_scales + (int64_t)min(m0 + row, M - 1) * 4 : p.w_scales + w_row(row) * 4;
   }
-  auto issue = [&](int kt) {
-    const int slot = kt % kStages;
+  auto issue = [&](int st) {
+    unsigned char *slot = lds + st % kStages * S::kStage;
+    if constexpr (kDirect)
 #pragma unroll
-    for (int i = 0; i < LA; ++i)
-      __builtin_amdgcn_global_load_lds((gptr_t *)(a_src + a_step[i] + (int64_t)kt * 128), (lptr_t *)(lds + slot * kABytes + (i * kThreads + wave * 64) * 16), 16, 0, 0);
+      for (int i = 0; i < LA; ++i)
+        __builtin_amdgcn_global_load_lds((gptr_t *)(a_src[i] + min(a_at[i] + (uint32_t)st * S::kARow, a_bytes - 16)), (lptr_t *)(slot + (i * kThreads + (wave << 6)) % kAChunks * 16), 16, 0, 0);
 #pragma unroll
     for (int i = 0; i < LW; ++i)
-      __builtin_amdgcn_global_load_lds((gptr_t *)(w_src[i] + (int64_t)kt * kWRow), (lptr_t *)(lds + kWBase + slot * kWBytes + (i * kThreads + wave * 64) * 16), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((gptr_t *)(w_src[i] + min(w_at[i] + (uint32_t)st * S::kWRow, w_bytes - 16)), (lptr_t *)(slot + S::kABytes + (i * kThreads + (wave << 6)) % kWChunks * 16), 16, 0, 0);
 #pragma unroll
     for (int i = 0; i < LS; ++i)
-      __builtin_amdgcn_global_load_lds((gptr_t *)(s_src[i] + kt * s_step[i]), (lptr_t *)(lds + kSBase + slot * kScaleBytes + s_slot[i]), 4, 0, 0);
+      __builtin_amdgcn_global_load_lds((gptr_t *)(s_src[i] + (uint64_t)min(st * WK + s_sub[i], nk - 1) * s_rows[i] * 4), (lptr_t *)(slot + S::kABytes + S::kWBytes + s_slot[i]), 4, 0, 0);
   };
-  // ---- rows of bf16 / float32: chunk tid % 16 of rows tid / 16 + i * kThreads / 16 ----
-  constexpr int kXRegs = LX > 0 ? LX : 1;
-  uint4 xb[ROWS == kRowsBf16 ? kXRegs : 1];
-  float xf[ROWS == kRowsF32 ? kXRegs : 1][8];
-  auto fetch = [&](int kt) {
-    const int k = kt * 128 + (tid & 15) * 8;
+  // ---- rows through registers ----
+  constexpr int LX = kDirect ? 1 : LA;
+  uint4 x[LX];
+  auto fetch = [&](int st) {
+    if constexpr (!kDirect)
 #pragma unroll
-    for (int i = 0; i < LX; ++i) {
-      const int64_t at = (int64_t)min(m0 + i * (kThreads / 16) + (tid >> 4), M - 1) * K + min(k, K);
-      if constexpr (ROWS == kRowsBf16) xb[i] = load8_raw((const bf16_t *)p.A + at, K - k);
-      if constexpr (ROWS == kRowsF32) load8((const float *)p.A + at, K - k, xf[i]);
-    }
-  };
-  auto stash = [&](int kt) {                                 // plane, half of 64 k, row, chunk
-    unsigned char *dst = lds + (kt & 1) * kABytes + (tid >> 3 & 1) * (BM * 128);
-#pragma unroll
-    for (int i = 0; i < LX; ++i) {
-      const int row = i * (kThreads / 16) + (tid >> 4);
-      unsigned char *q = dst + row * 128 + (((tid & 7) ^ (row >> 1 & 7)) << 4);
-      if constexpr (ROWS == kRowsBf16) *reinterpret_cast<uint4 *>(q) = xb[i];
-      if constexpr (ROWS == kRowsF32) {
-        bf16x8 part[3];
-        split3(xf[i], part);
-#pragma unroll
-        for (int e = 0; e < 3; ++e) *reinterpret_cast<bf16x8 *>(q + e * (BM * 256)) = part[e];
+      for (int i = 0; i < LX; ++i) {
+        const int k = (int)(a_at[i] + st * S::kARow) / kASize;
+        if constexpr (ROWS == kRowsBf16) x[i] = load8_raw((const bf16_t *)a_src[i] + min(k, K), K - k);
+        else x[i] = load4_raw((const float *)a_src[i] + min(k, K), K - k);
       }
-    }
+  };
+  auto stash = [&](int st) {
+    if constexpr (!kDirect)
+#pragma unroll
+      for (int i = 0; i < LX; ++i) *reinterpret_cast<uint4 *>(lds + st % kStages * S::kStage + (i * kThreads + tid) % kAChunks * 16) = x[i];
   };
 
   floatx4 acc[NT][MT];
@@ -420,144 +265,213 @@ gemm_mx_tile_kernel(MxGemm p, TileMap tm) {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) acc[nt][mt] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  if (!kCodes) { fetch(0); stash(0); }
+  // ---- operands of a stage in registers ----
+  const int am = wm * (BM / WM) + r, an = wn * (BN / WN) + r;               // rows of the lane's operands in the tiles (but for 16 mt, 16 nt)
+  const int ar = AR < 16 ? r % AR : am;                      // behind AR rows the first ones again, for columns of the instruction that are not stored
+  const int a_swz = swizzle<S::kARow>(ar), w_swz = swizzle<S::kWRow>(r);
+  constexpr int kFA = kCodes ? 2 : ROWS == kRowsBf16 ? 4 : 8, kFW = kW8 ? 2 : 1;
+  struct Operands { intx4 a[MT][kFA], w[NT][kFW]; int as[kCodes ? MT : 1], ws[NT]; };
+  auto read = [&](Operands &o, int st) {
+    const unsigned char *slot = lds + st % kStages * S::kStage;
+    const unsigned char *la = slot + ar * S::kARow, *lw = slot + S::kABytes + an * S::kWRow;
+    const unsigned char *sa = slot + S::kABytes + S::kWBytes + (wk * AR + ar) * 4 + g, *sw = slot + S::kABytes + S::kWBytes + S::kAUnits * 256 + (wk * BN + an) * 4 + g;
+    // chunks of the lane: scaled instruction g and 4 + g; else kFA from kFA g on
 #pragma unroll
-  for (int s = 0; s < kStages - 1; ++s)
-    if (s < nk) issue(s);
-
-  const int swz = (r >> 1) & 7, am = wm * WTM + r, an = wn * WTN + r;       // rows of the lane's operands in the tiles
-  auto compute = [&](int kt) {
-    const int slot = kt % kStages;
-    const unsigned char *la = lds + (kCodes ? slot : kt & 1) * kABytes + am * 128, *lw = lds + kWBase + slot * kWBytes + an * kWRow;
-    const unsigned char *sa = lds + kSBase + slot * kScaleBytes + am * 4 + g, *sw = lds + kSBase + slot * kScaleBytes + kWScale + an * 4 + g;
-    auto chunk_of = [&](const unsigned char *row, int c) { return *reinterpret_cast<const intx4 *>(row + ((c ^ swz) << 4)); };
-    auto w4_chunk = [&](int nt) { return *reinterpret_cast<const intx4 *>(lw + nt * 16 * 64 + ((g ^ (r >> 2 & 3)) << 4)); };
+    for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+      for (int c = 0; c < kFA; ++c)
+        o.a[mt][c] = *reinterpret_cast<const intx4 *>(la + mt * 16 * S::kARow + (((wk * (kACpr / WK) + (ROWS == kRowsMx ? 4 * c + g : kFA * g + c)) ^ a_swz) << 4));
+      if (kCodes) o.as[kCodes ? mt : 0] = sa[mt * 64];
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int c = 0; c < kFW; ++c)
+        o.w[nt][c] = *reinterpret_cast<const intx4 *>(lw + nt * 16 * S::kWRow + (((wk * (kWCpr / WK) + (ROWS == kRowsMx ? 4 * c + g : kFW * g + c)) ^ w_swz) << 4));
+      o.ws[nt] = sw[nt * 64];
+    }
+  };
+  auto multiply = [&](const Operands &o, int st) {
     if constexpr (ROWS == kRowsMx) {
-      intx8 a[MT];
-      int as[MT];
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        a[mt] = join(chunk_of(la + mt * 16 * 128, g), chunk_of(la + mt * 16 * 128, 4 + g));
-        as[mt] = sa[mt * 64];
-      }
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const intx8 w = kW8 ? join(chunk_of(lw + nt * 16 * 128, g), chunk_of(lw + nt * 16 * 128, 4 + g)) : join(w4_chunk(nt), intx4{0, 0, 0, 0});
-        const int ws = sw[nt * 64];
 #ifdef __HIP_DEVICE_COMPILE__
 #pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
         for (int mt = 0; mt < MT; ++mt)
-          acc[nt][mt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, a[mt], acc[nt][mt], kW8 ? 0 : 4, 0, 0, ws, 0, as[mt]);
+          acc[nt][mt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kW8 ? join(o.w[nt][0], o.w[nt][kFW - 1]) : join(o.w[nt][0], intx4{0, 0, 0, 0}),
+                                                                         join(o.a[mt][0], o.a[mt][1]), acc[nt][mt], kW8 ? 0 : 4, 0, 0, o.ws[nt], 0, o.as[kCodes ? mt : 0]);
 #endif
-      }
     } else {
-      float as[kCodes ? MT : 1];
-      if (kCodes)
+      // four instructions of 32 k: lane g has elements 32 g + 8 j .. + 7 of its 128 in the j-th, all of one block
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) as[mt] = byte_scale(sa[mt * 64]);
-      float ws[NT];
+      for (int j = 0; j < 4; ++j) {
+        bf16x8 w[NT];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) ws[nt] = byte_scale(sw[nt * 64]);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {                          // elements 32 g + 16 h .. + 15: two instructions
-        bf16x8 a[MT][2][kPlanes];
+        for (int nt = 0; nt < NT; ++nt)
+          w[nt] = kW8 ? decode_e4m3(o.w[nt][(j >> 1) % kFW][j * 2 & 3], o.w[nt][(j >> 1) % kFW][(j * 2 & 3) + 1], byte_scale(o.ws[nt]))
+                      : decode_e2m1(o.w[nt][0][j], byte_scale(o.ws[nt]));
+        const int k = (st * WK + wk) * 128 + 32 * g + 8 * j;                 // rows of bf16 / float32: what lies behind K is another chunk's
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
+          bf16x8 a[3];
           if constexpr (kCodes) {
-            const intx4 c = chunk_of(la + mt * 16 * 128, 2 * g + h);
-            a[mt][0][0] = decode_e4m3(c[0], c[1], as[mt]);
-            a[mt][1][0] = decode_e4m3(c[2], c[3], as[mt]);
+            const float as = byte_scale(o.as[kCodes ? mt : 0]);
+            a[0] = decode_e4m3(o.a[mt][j >> 1][j * 2 & 3], o.a[mt][j >> 1][(j * 2 & 3) + 1], as);
+          } else if constexpr (ROWS == kRowsBf16) {
+            a[0] = __builtin_bit_cast(bf16x8, k >= K ? intx4{0, 0, 0, 0} : o.a[mt][j]);
           } else {
+            float v[8];
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-              for (int q = 0; q < kPlanes; ++q)
-                a[mt][j][q] = __builtin_bit_cast(bf16x8, chunk_of(la + mt * 16 * 128 + (g >> 1) * (BM * 128) + q * (BM * 256), (g & 1) * 4 + 2 * h + j));
-          }
-        }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          bf16x8 w[2];
-          if (kW8) {
-            const intx4 c = chunk_of(lw + nt * 16 * 128, 2 * g + h);
-            w[0] = decode_e4m3(c[0], c[1], ws[nt]);
-            w[1] = decode_e4m3(c[2], c[3], ws[nt]);
-          } else {
-            const intx4 c = w4_chunk(nt);
-            w[0] = decode_e2m1(c[2 * h], ws[nt]);
-            w[1] = decode_e2m1(c[2 * h + 1], ws[nt]);
+            for (int e = 0; e < 8; ++e) v[e] = k + (e & 4) >= K ? 0.f : __int_as_float(o.a[mt][(2 * j + e / 4) % kFA][e % 4]);
+            split3(v, a);
           }
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-              for (int q = kPlanes - 1; q >= 0; --q)
-                acc[nt][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[j], a[mt][j][q], acc[nt][mt], 0, 0, 0);
+            for (int q = kPlanes - 1; q >= 0; --q) acc[nt][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[nt], a[q], acc[nt][mt], 0, 0, 0);
         }
       }
     }
   };
-  for (int kt = 0; kt < nk; ++kt) {
-    if (kt + kStages - 2 < nk) wait_vmcnt<(kStages - 2) * kLoads>(); else wait_vmcnt<0>();    // my loads of stage kt have landed
-    __builtin_amdgcn_s_waitcnt(0xc07f);                      // lgkmcnt(0): my reads of stage kt - 1 and my rows of stage kt are done
+
+  // ---- the ring ----
+  fetch(0);
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s)
+    if (s < ns) issue(s);
+  stash(0);
+  for (int st = 0; st < ns; ++st) {
+    if (st + kStages - 2 < ns) wait_vmcnt<(kStages - 2) * kLoads>(); else wait_vmcnt<0>();    // my loads of this stage have landed
+    __builtin_amdgcn_s_waitcnt(0xc07f);                      // lgkmcnt(0): my reads of the last stage and my rows of this one are done
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    if (!kCodes && kt + 1 < nk) fetch(kt + 1);
-    if (kt + kStages - 1 < nk) issue(kt + kStages - 1);
-    compute(kt);
-    if (!kCodes && kt + 1 < nk) stash(kt + 1);
+    if (!kDirect && st + 1 < ns) fetch(st + 1);
+    if (st + kStages - 1 < ns) issue(st + kStages - 1);
+    if (WK == 1 || st * WK + wk < nk) {
+      Operands o;
+      read(o, st);
+      multiply(o, st);
+    }
+    if (!kDirect && st + 1 < ns) stash(st + 1);
   }
 
   // ---- results: lane has columns 4 g .. 4 g + 3 of row r of each 16 x 16 tile ----
+  if constexpr (WK > 1) {
+    floatx4 *sums = reinterpret_cast<floatx4 *>(lds);        // [wk][wm, wn][tile][lane]
+    __syncthreads();                                         // every wave is done with the ring
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) sums[(wave * NT * MT + nt * MT + mt) * 64 + lane] = acc[nt][mt];
+    __syncthreads();
+  }
+  auto result = [&](int nt, int mt) {                        // in the order of k
+    if constexpr (WK == 1) return acc[nt][mt];
+    const floatx4 *sums = reinterpret_cast<const floatx4 *>(lds) + ((wave % (WM * WN)) * NT * MT + nt * MT + mt) * 64 + lane;
+    floatx4 s = sums[0];
+#pragma unroll
+    for (int k = 1; k < WK; ++k) s += sums[k * WM * WN * NT * MT * 64];
+    return s;
+  };
   if constexpr (kSwiglu) {
     const int Np = (N + kMxStage - 1) / kMxStage * kMxStage, c0 = n0 + wn * 32;
     if (c0 >= Np) return;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      const int m = m0 + wm * WTM + mt * 16 + r;
-      store_act(acc[0][mt], acc[NT / 4][mt], acc[NT / 2][mt], acc[NT / 2 + NT / 4][mt], m < M, m, c0, g, p, Np);
+      if (WK > 1 && mt % WK != wk) continue;
+      const int m = m0 + am + mt * 16;
+      store_act(result(0, mt), result(1, mt), result(2, mt), result(3, mt), m < M, m, c0, g, p, Np);
     }
   } else {
     using T = std::conditional_t<OUT == kOutF32, float, bf16_t>;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-      const int m = m0 + wm * WTM + mt * 16 + r;
-      if (m >= M) continue;
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) store_row4<T>(acc[nt][mt], m, n0 + wn * WTN + nt * 16 + 4 * g, p);
-    }
+      for (int nt = 0; nt < NT; ++nt) {
+        if (WK > 1 && (mt * NT + nt) % WK != wk) continue;
+        const int m = m0 + am + mt * 16;
+        if (m < M) store_row4<T>(result(nt, mt), m, n0 + wn * (BN / WN) + nt * 16 + 4 * g, p);
+      }
   }
 }
 
-template <int ROWS, int WF, int OUT, int BM, int BN, int WM, int WN, int kStages>
-pvf_status run_tile(hipStream_t s, const MxGemm &p) {
-  constexpr int kLds = (codes_in(ROWS) ? kStages : 2) * a_stage_bytes<ROWS>(BM) + kStages * (BN * (WF == PVF_MX_E4M3 ? 128 : 64) + (codes_in(ROWS) ? BM * 4 : 0) + BN * 4);
-  static_assert(kLds <= 160 * 1024, "LDS");
+template <int ROWS, int WF, int OUT, int BM, int BN, int WM, int WN, int WK, int kStages, int AR = BM, bool kDirect = true>
+pvf_status run_as(hipStream_t s, const MxGemm &p) {
+  using S = Shape<ROWS, WF, BM, BN, WM, WN, WK, kStages, AR>;
+  static_assert(S::kLds <= 160 * 1024, "LDS");
   TileMap tm;
   const int64_t tiles_n = OUT == kOutSwiglu ? (mx_width(p.N) + BN / 2 - 1) / (BN / 2) : (p.N + BN - 1) / BN, tiles_m = (p.M + BM - 1) / BM;
   PVF_REQUIRE(nullptr, tiles_m * tiles_n < 1 << 28, PVF_ESHAPE, "%d x %d results are too many for a launch", p.M, p.N);
   tm.tiles_m = (int)tiles_m; tm.tiles_n = (int)tiles_n; tm.group_m = (int)std::min<int64_t>(tiles_m, 8);
-  const int chunk = (int)((tiles_m * tiles_n + 7) / 8);
-  auto kernel = gemm_mx_tile_kernel<ROWS, WF, OUT, BM, BN, WM, WN, kStages>;
-  static const hipError_t allowed = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+  auto kernel = gemm_mx_kernel<ROWS, WF, OUT, BM, BN, WM, WN, WK, kStages, AR, kDirect>;
+  // once per kernel instance; a function-local static is initialised exactly once even with concurrent callers
+  static const hipError_t allowed = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
   PVF_HIP_CHECK(nullptr, allowed);
-  kernel<<<chunk * 8, 64 * WM * WN, kLds, s>>>(p, tm);
+  kernel<<<(uint32_t)((tiles_m * tiles_n + 7) / 8 * 8), S::kThreads, S::kLds, s>>>(p, tm);
   PVF_LAUNCH_CHECK(nullptr, "gemm_mx");
   return PVF_OK;
 }
 
-template <int ROWS, int WF, int OUT> pvf_status run(hipStream_t s, const MxGemm &p) {
-  if (p.M <= 64) return run_rows<ROWS, WF, OUT>(s, p);
-  if constexpr (ROWS == kRowsMx) {
-    if ((int64_t)p.M * p.N >= 256 * 256 * 192) return run_tile<ROWS, WF, OUT, 256, 256, 2, 4, 2>(s, p);
+// ---- which instance -------------------------------------------------------------------------------------------------
+// What a tile costs for 128 k, in microseconds, measured at K = 4096 (launch time less 3 us, over 32 and the tiles of the fullest CU):
+// where a CU has one tile, and per tile where it has several (those that fit its LDS run at a time and hide each other's barriers and
+// latencies).  The launch takes the instance whose fullest CU is done first.  What bounds small tiles is a CU's loads on the way: some 60
+// bytes a nanosecond, so a tile's rows count, not its area.
+struct Candidate {
+  int BM, BN, most_rows;                                     // most_rows: rows of A that the instance loads (0: any number)
+  float alone, among;
+  pvf_status (*run)(hipStream_t, const MxGemm &);
+};
+
+template <int ROWS, int WF, int OUT, bool kDirect> struct Candidates;
+#define PVF_MX_TILE(BM, BN, WM, WN, WK, ST, AR, alone, among) \
+  {BM, OUT == kOutSwiglu ? BN / 2 : BN, AR < BM ? AR : 0, alone, among, run_as<ROWS, WF, OUT, BM, BN, WM, WN, WK, ST, AR, kDirect>}
+
+template <int WF, bool kDirect> struct Candidates<kRowsMx, WF, kOutBf16, kDirect> {
+  static constexpr int ROWS = kRowsMx, OUT = kOutBf16;
+  static constexpr Candidate list[] = {
+      PVF_MX_TILE(16, 16, 1, 1, 4, 3, 16, .08f, .075f),   PVF_MX_TILE(32, 32, 1, 1, 4, 3, 32, .1375f, .153f), PVF_MX_TILE(64, 64, 2, 2, 2, 3, 64, .275f, .28f),
+      PVF_MX_TILE(64, 64, 2, 2, 2, 2, 64, .38f, .217f),   PVF_MX_TILE(80, 64, 1, 2, 4, 2, 80, .29f, .33f),   PVF_MX_TILE(96, 64, 2, 2, 1, 3, 96, .39f, .28f),
+      PVF_MX_TILE(64, 128, 2, 4, 1, 3, 64, .415f, .375f), PVF_MX_TILE(128, 128, 2, 2, 1, 2, 128, .78f, .51f), PVF_MX_TILE(160, 128, 2, 4, 1, 2, 160, .83f, .72f),
+      PVF_MX_TILE(192, 256, 2, 4, 1, 2, 192, 1.49f, 1.44f), PVF_MX_TILE(256, 256, 2, 4, 1, 2, 256, 1.8f, 1.84f)};
+};
+template <int WF, bool kDirect> struct Candidates<kRowsMxExact, WF, kOutF32, kDirect> {
+  static constexpr int ROWS = kRowsMxExact, OUT = kOutF32;
+  static constexpr Candidate list[] = {
+      PVF_MX_TILE(16, 16, 1, 1, 4, 3, 16, .10f, .10f),   PVF_MX_TILE(32, 32, 1, 1, 4, 3, 32, .19f, .20f),    PVF_MX_TILE(64, 64, 2, 2, 2, 2, 64, .42f, .36f),
+      PVF_MX_TILE(64, 128, 2, 4, 1, 3, 64, .74f, .61f),  PVF_MX_TILE(128, 128, 2, 2, 1, 2, 128, 1.2f, .91f), PVF_MX_TILE(160, 128, 2, 4, 1, 2, 160, 1.43f, 1.22f)};
+};
+template <int WF, bool kDirect> struct Candidates<kRowsMxExact, WF, kOutSwiglu, kDirect> {
+  static constexpr int ROWS = kRowsMxExact, OUT = kOutSwiglu;
+  static constexpr Candidate list[] = {
+      PVF_MX_TILE(16, 64, 1, 1, 4, 2, 16, .18f, .14f),   PVF_MX_TILE(32, 64, 1, 1, 4, 2, 32, .25f, .20f),    PVF_MX_TILE(64, 128, 2, 2, 2, 2, 64, .53f, .65f),
+      PVF_MX_TILE(64, 128, 2, 2, 1, 2, 64, .67f, .55f),  PVF_MX_TILE(128, 128, 2, 2, 1, 2, 128, 1.2f, .90f)};
+};
+template <bool kDirect> struct Candidates<kRowsBf16, PVF_MX_E2M1, kOutBf16, kDirect> {
+  static constexpr int ROWS = kRowsBf16, WF = PVF_MX_E2M1, OUT = kOutBf16;
+  static constexpr Candidate list[] = {
+      PVF_MX_TILE(16, 16, 1, 1, 8, 2, 1, .04f, .047f),   PVF_MX_TILE(16, 16, 1, 1, 8, 2, 4, .06f, .05f),     PVF_MX_TILE(16, 16, 1, 1, 4, 2, 16, .095f, .058f),
+      PVF_MX_TILE(32, 32, 2, 1, 4, 2, 32, .19f, .20f),   PVF_MX_TILE(32, 64, 2, 1, 2, 2, 32, .35f, .215f),   PVF_MX_TILE(64, 64, 2, 2, 2, 2, 64, .41f, .42f),
+      PVF_MX_TILE(64, 128, 2, 2, 1, 2, 64, .75f, .58f)};
+};
+template <bool kDirect> struct Candidates<kRowsF32, PVF_MX_E2M1, kOutF32, kDirect> {
+  static constexpr int ROWS = kRowsF32, WF = PVF_MX_E2M1, OUT = kOutF32;
+  static constexpr Candidate list[] = {
+      PVF_MX_TILE(16, 16, 1, 1, 8, 2, 1, .07f, .10f),    PVF_MX_TILE(16, 16, 1, 1, 8, 2, 16, .27f, .30f),    PVF_MX_TILE(16, 32, 1, 1, 4, 2, 16, .35f, .37f),
+      PVF_MX_TILE(32, 32, 2, 1, 4, 2, 32, .59f, .70f),   PVF_MX_TILE(32, 64, 2, 1, 2, 2, 32, .82f, .84f),    PVF_MX_TILE(64, 128, 4, 1, 1, 2, 64, 2.1f, 2.1f)};
+};
+
+template <int ROWS, int WF, int OUT, bool kDirect = true> pvf_status run(hipStream_t s, const MxGemm &p) {
+  const int64_t columns = OUT == kOutSwiglu ? mx_width(p.N) : p.N;
+  const Candidate *best = nullptr;
+  float least = 0.f;
+  for (const Candidate &c : Candidates<ROWS, WF, OUT, kDirect>::list) {
+    if (c.most_rows && p.M > c.most_rows) continue;
+    const int64_t tiles = ((p.M + c.BM - 1) / c.BM) * ((columns + c.BN - 1) / c.BN), fullest = (tiles + 255) / 256;
+    const float cost = fullest == 1 ? c.alone : c.among * (float)fullest;
+    if (!best || cost < least) { best = &c; least = cost; }
   }
-  if constexpr (codes_in(ROWS)) {
-    if ((int64_t)p.M * p.N * (OUT == kOutSwiglu ? 2 : 1) >= 128 * 128 * 192) return run_tile<ROWS, WF, OUT, 128, 128, 2, 2, 3>(s, p);
-    return run_tile<ROWS, WF, OUT, 64, 64, 4, 1, 4>(s, p);
-  } else {
-    return run_tile<ROWS, WF, OUT, 64, 64, 2, 2, 3>(s, p);
-  }
+  return best->run(s, p);
 }
 
 template <int WF> pvf_status run_mx(hipStream_t s, const MxGemm &p) {
@@ -570,8 +484,11 @@ template <int WF> pvf_status run_mx(hipStream_t s, const MxGemm &p) {
 
 pvf_status launch_gemm_mx(hipStream_t s, const MxGemm &p) {
   if (p.M == 0 || p.N == 0) return PVF_OK;
-  if (!p.a_scales)
-    return p.dtype == PVF_F32 ? run<kRowsF32, PVF_MX_E2M1, kOutF32>(s, p) : run<kRowsBf16, PVF_MX_E2M1, kOutBf16>(s, p);
+  if (!p.a_scales) {                                         // rows that begin at 16-byte chunks go straight to LDS
+    const bool f32 = p.dtype == PVF_F32, direct = (uintptr_t)p.A % 16 == 0 && p.K % (f32 ? 4 : 8) == 0;
+    if (f32) return direct ? run<kRowsF32, PVF_MX_E2M1, kOutF32>(s, p) : run<kRowsF32, PVF_MX_E2M1, kOutF32, false>(s, p);
+    return direct ? run<kRowsBf16, PVF_MX_E2M1, kOutBf16>(s, p) : run<kRowsBf16, PVF_MX_E2M1, kOutBf16, false>(s, p);
+  }
   return p.w_fmt == PVF_MX_E4M3 ? run_mx<PVF_MX_E4M3>(s, p) : run_mx<PVF_MX_E2M1>(s, p);
 }
 

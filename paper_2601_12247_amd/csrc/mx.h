@@ -85,6 +85,14 @@ __device__ __forceinline__ uint4 load8_raw(const bf16_t *p, int left) {
   for (int e = 0; e < 8; ++e) h[e] = e < left ? reinterpret_cast<const uint16_t *>(p)[e] : 0u;
   return make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
 }
+__device__ __forceinline__ uint4 load4_raw(const float *p, int left) {
+  if (left >= 4) {
+    typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(4)));
+    const u4 a = *reinterpret_cast<const u4 *>(p);
+    return make_uint4(a[0], a[1], a[2], a[3]);
+  }
+  return make_uint4(left > 0 ? __float_as_uint(p[0]) : 0u, left > 1 ? __float_as_uint(p[1]) : 0u, left > 2 ? __float_as_uint(p[2]) : 0u, 0u);
+}
 __device__ __forceinline__ void load8(const bf16_t *p, int left, float *v) {
   const uint4 a = load8_raw(p, left);
   const uint32_t w[4] = {a.x, a.y, a.z, a.w};

@@ -216,6 +216,24 @@ def test_products_of_whole_numbers(M, N, K, fmt, dtype, residual):
     assert untouched()
 
 
+LARGE = [(64, 4096, 300), (64, 12288, 256), (320, 4100, 385), (320, 12288, 256), (256, 24576, 128), (640, 4096, 300), (500, 12300, 200), (1280, 4096, 256), (1300, 4000, 130),
+         (2560, 4096, 256), (2500, 4011, 100), (2560, 12288, 384), (2049, 9000, 513)]
+
+
+@pytest.mark.parametrize("M,N,K", LARGE)
+@pytest.mark.parametrize("fmt,dtype", [(R.E4M3, "bf16"), (R.E2M1, "bf16"), (R.E4M3, "f32"), (R.E2M1, "f32")])
+def test_products_of_whole_numbers_on_every_tile(M, N, K, fmt, dtype):
+    """Sizes at which the tiles of many rows are taken, whole and ragged, one stage of k and several."""
+    a, a_b, av = whole(M, K, R.E4M3, M + K)
+    w, w_b, wv = whole(N, K, fmt, N + K + 1)
+    out, untouched = guarded((M, N), DT[dtype], 0xa5)
+    res = torch.randint(-50, 51, (M, N), generator=torch.Generator().manual_seed(3)).to(DT[dtype])
+    B.gemm_mx(*R.pack(a, a_b, R.E4M3), *R.pack(w, w_b, fmt), residual=res.cuda(), out=out)
+    want = cuda64(av, wv) + res.double()
+    assert torch.equal(out.cpu(), want.float().to(DT[dtype]))
+    assert untouched()
+
+
 @pytest.mark.parametrize("M,N,K", [(1, 40, 128), (5, 33, 65), (64, 96, 1411), (70, 200, 256), (300, 140, 4096)])
 @pytest.mark.parametrize("fmt", [R.E4M3, R.E2M1])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -231,7 +249,8 @@ def test_products_of_random_rows(M, N, K, fmt, dtype):
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 1, 33), (1, 64, 128), (1, 12288, 4096), (2, 17, 31), (16, 48, 300), (17, 33, 1411), (33, 100, 129), (64, 257, 4096), (65, 130, 640),
-                                   (130, 300, 264), (320, 1024, 2048), (511, 769, 520), (1024, 384, 1000)])
+                                   (130, 300, 264), (320, 1024, 2048), (511, 769, 520), (1024, 384, 1000), (4, 4096, 512), (3, 300, 1024), (16, 12288, 256), (33, 4001, 1411),
+                                   (64, 4096, 256), (64, 12288, 520), (320, 4096, 512), (330, 12300, 264)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("residual,shift", [(False, 0), (True, 0), (False, 1)])
 def test_4_bit_products_of_whole_numbers(M, N, K, dtype, residual, shift):
@@ -339,7 +358,7 @@ def within_codes(got, want_values, slack):
 
 
 @pytest.mark.parametrize("M,ff,K", [(1, 1, 32), (1, 32, 128), (3, 17, 33), (16, 200, 300), (17, 129, 1411), (64, 256, 4096), (65, 130, 640), (130, 500, 260), (257, 384, 512),
-                                    (320, 1024, 1024), (515, 257, 384)])
+                                    (320, 1024, 1024), (515, 257, 384), (64, 4100, 256), (1, 12288, 256), (320, 12288, 128), (1100, 3000, 264)])
 @pytest.mark.parametrize("fmt", [R.E4M3, R.E2M1])
 def test_swiglu(M, ff, K, fmt):
     """The slack of a product is that of test_products_of_random_rows without a rounding to bf16; silu(g) u moves by at most 1.1 |u| dg + |silu(g)| du
