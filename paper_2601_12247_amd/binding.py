@@ -445,22 +445,25 @@ def mx_empty(rows: int, K: int, fmt: int = MX_E4M3, device="cuda"):
 
 def _mx_format(codes: torch.Tensor, scales: torch.Tensor, rows: int, Kp: int) -> int:
     """The format of checked codes and scales."""
-    fmt = MX_E4M3 if codes.dtype == torch.float8_e4m3fn else MX_E2M1
-    assert fmt == MX_E4M3 or codes.dtype == torch.uint8, f"codes are float8_e4m3fn or uint8, not {codes.dtype}"
-    assert codes.shape == (rows, Kp if fmt == MX_E4M3 else Kp // 2), f"codes of {rows} rows of {Kp}: {tuple(codes.shape)}"
-    assert scales.dtype == torch.float8_e8m0fnu and scales.shape == (Kp // 128, rows, 4), \
+    if codes.dtype is torch.float8_e4m3fn:
+        fmt, width = MX_E4M3, Kp
+    else:
+        assert codes.dtype is torch.uint8, f"codes are float8_e4m3fn or uint8, not {codes.dtype}"
+        fmt, width = MX_E2M1, Kp // 2
+    assert codes.shape == (rows, width), f"codes of {rows} rows of {Kp}: {tuple(codes.shape)}"
+    assert scales.dtype is torch.float8_e8m0fnu and scales.shape == (Kp // 128, rows, 4), \
         f"scales of {rows} rows of {Kp}: {scales.dtype} {tuple(scales.shape)}"
     return fmt
 
 
 def _mx_call(fn, tensors, *args) -> None:
-    """fn(stream, *args) on the device that the tensors are on.  Costs a microsecond beside the launch, so the stream is asked for as a
-    number: torch.cuda.current_stream() takes three."""
+    """fn(stream, *args) on the device that the tensors are on.  Costs a microsecond beside the launch, so the device and its stream are asked
+    for as numbers: torch.cuda.current_stream() takes three."""
     dev = tensors[0].get_device()
     for t in tensors:
         assert t is None or (t.get_device() == dev and t.is_contiguous()), "contiguous tensors on one device required"
     assert dev >= 0, "device-resident tensors required"
-    if dev != torch.cuda.current_device():
+    if dev != torch._C._cuda_getDevice():
         with torch.cuda.device(dev):
             status = fn(torch._C._cuda_getCurrentRawStream(dev), *args)
     else:
@@ -491,8 +494,10 @@ def add_rmsnorm_mx(x: torch.Tensor, gain: torch.Tensor, eps: float, residual: Op
     assert _mx_format(codes, scales, M, mx_width(d)) == MX_E4M3, "the norm writes MX_E4M3"
     if residual is not None and sum_out is None:
         sum_out = torch.empty_like(x)
-    assert gain.shape == (d,) and gain.dtype == x.dtype
-    assert all(t is None or (t.shape == x.shape and t.dtype == x.dtype) for t in (residual, sum_out))
+    dtype, shape = x.dtype, x.shape
+    assert gain.dtype is dtype and gain.shape == (d,), "gain is [d] of x's type"
+    assert residual is None or (residual.dtype is dtype and residual.shape == shape), "the residual is like x"
+    assert sum_out is None or (sum_out.dtype is dtype and sum_out.shape == shape), "the sum is like x"
     _mx_call(lib().pvf_add_rmsnorm_mx, (x, residual, gain, sum_out, codes, scales), _dtype_code(x.dtype), x.data_ptr(), _p(residual),
              gain.data_ptr(), _p(sum_out), codes.data_ptr(), scales.data_ptr(), M, d, eps)
     return x if sum_out is None else sum_out, codes, scales
@@ -506,7 +511,8 @@ def gemm_mx(A: torch.Tensor, a_scales: torch.Tensor, W: torch.Tensor, w_scales: 
     fmt = _mx_format(W, w_scales, N, Kp)
     if out is None:
         out = torch.empty(M, N, dtype=dtype if residual is None else residual.dtype, device=A.device)
-    assert out.shape == (M, N) and (residual is None or (residual.shape == (M, N) and residual.dtype == out.dtype))
+    assert out.shape == (M, N), "the result is [M, N]"
+    assert residual is None or (residual.dtype is out.dtype and residual.shape == out.shape), "the residual is like the result"
     _mx_call(lib().pvf_gemm_mx, (A, a_scales, W, w_scales, out, residual), fmt, _dtype_code(out.dtype), A.data_ptr(), a_scales.data_ptr(),
              W.data_ptr(), w_scales.data_ptr(), out.data_ptr(), _p(residual), M, N, Kp)
     return out
@@ -532,7 +538,8 @@ def gemm_w4(x: torch.Tensor, W: torch.Tensor, w_scales: torch.Tensor, residual: 
     assert _mx_format(W, w_scales, N, mx_width(K)) == MX_E2M1, "W is MX_E2M1"
     if out is None:
         out = torch.empty(M, N, dtype=x.dtype, device=x.device)
-    assert all(t is None or (t.shape == (M, N) and t.dtype == x.dtype) for t in (out, residual))
+    assert out.dtype is x.dtype and out.shape == (M, N), "the result is [M, N] of x's type"
+    assert residual is None or (residual.dtype is x.dtype and residual.shape == out.shape), "the residual is like the result"
     _mx_call(lib().pvf_gemm_w4, (x, W, w_scales, out, residual), _dtype_code(x.dtype), x.data_ptr(), W.data_ptr(), w_scales.data_ptr(),
              out.data_ptr(), _p(residual), M, N, K)
     return out

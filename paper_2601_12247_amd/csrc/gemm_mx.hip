@@ -35,6 +35,8 @@ constexpr bool codes_in(int rows) { return rows == kRowsMx || rows == kRowsMxExa
 
 __device__ __forceinline__ float silu_f(float g) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
 
+// The four registers of 32 e2m1 codes; the instruction does not read the others.
+__device__ __forceinline__ intx8 join(intx4 lo) { return __builtin_shufflevector(lo, lo, 0, 1, 2, 3, -1, -1, -1, -1); }
 __device__ __forceinline__ intx8 join(intx4 lo, intx4 hi) { return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7); }
 
 // Eight codes (two words of e4m3, one of e2m1) times 2^(b - 127) as bfloat16.
@@ -76,12 +78,12 @@ __device__ __forceinline__ void split3(const float *x, bf16x8 *p) {
 }
 
 // ---- results ------------------------------------------------------------------------------------------------------
-// Columns n .. n + 3 of row m.
-template <typename T> __device__ __forceinline__ void store_row4(floatx4 v, int m, int n, const MxGemm &p) {
+// Columns n .. n + 3 of row m, those from n_from on.
+template <typename T> __device__ __forceinline__ void store_row4(floatx4 v, int m, int n, const MxGemm &p, int n_from = 0) {
   const int N = p.N;
   T *row = (T *)p.C + (int64_t)m * N;
   const T *res = p.residual ? (const T *)p.residual + (int64_t)m * N : nullptr;
-  if (N % 4 == 0 && n < N) {                                 // a row begins as C does, at an element: unaligned vectors
+  if (N % 4 == 0 && n < N && n >= n_from) {                                 // a row begins as C does, at an element: unaligned vectors
     float x[4] = {v[0], v[1], v[2], v[3]};
     if constexpr (sizeof(T) == 2) {
       typedef uint32_t u2 __attribute__((ext_vector_type(2), aligned(2)));
@@ -108,7 +110,7 @@ template <typename T> __device__ __forceinline__ void store_row4(floatx4 v, int 
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e)
-    if (n + e < N) row[n + e] = from_float<T>(v[e] + (res ? to_float(res[n + e]) : 0.f));
+    if (n + e < N && n + e >= n_from) row[n + e] = from_float<T>(v[e] + (res ? to_float(res[n + e]) : 0.f));
 }
 
 // silu(gate) * up of 32 columns from c0 on, of which the lane has 4 g .. + 3 and 16 + 4 g .. + 3: a block, as codes and scale.  All 64 lanes.
@@ -146,12 +148,95 @@ template <int N> __device__ __forceinline__ void wait_vmcnt() {
 
 struct TileMap { int tiles_m, tiles_n, group_m; };
 
-// Where 16-byte chunk c of a row lies in LDS rows of R bytes: the reads of an operand (16 rows, one chunk each) touch every bank once.
-template <int R> __device__ __forceinline__ int swizzle(int row) { return R >= 256 ? row & 15 : R == 128 ? row >> 1 & 7 : row >> 2 & 3; }
+// Chunk c of a row lies at place c ^ swizzle(row) of an LDS row of R bytes, so that the reads of an operand (lane (r, g): row r, chunk c0 + X g) touch
+// every bank once per 16 lanes.  ds_read_b128 takes lanes 0-3, 12-15 and 20-27 together, then 4-11, 16-19 and 28-31, and so on: rows whose
+// bits 2 and 3 are equal with one g, the other rows with the next.  So the places of the first have to be those of the second moved by X.
+template <int R, int X> __device__ __forceinline__ int swizzle(int row) {
+  const int t = row >> 2 & 3;
+  if (R == 64) return 0x78 >> 2 * t & 3;                     // 0, 2, 3, 1 (X = 1)
+  if (R == 128) return X == 1 ? row >> 1 & 7 : (row >> 1 & 4) | (row >> 2 & 1) | (row & 2);      // X = 2: bits 0 and 1 of row / 2 exchanged
+  return X <= 2 ? row & 15 : (row & 3) | (X == 4 ? 0x78 >> 2 * t & 3 : t ^ t >> 1) << 2;         // X = 8: 0, 1, 3, 2
+}
+
+// ---- operands of 128 k in registers -----------------------------------------------------------------------------------
+// Lane (r, g) of a wave whose results are 16 MT rows x 16 NT columns.  Chunks of 16 bytes: of the scaled instruction's e4m3 rows the g-th and
+// the 4 + g-th, of all others the kA (kW) from kA g on.
+template <int ROWS, int WF, int MT, int NT> struct Operands {
+  static constexpr bool kCodes = codes_in(ROWS), kW8 = WF == PVF_MX_E4M3;
+  static constexpr int kA = kCodes ? 2 : ROWS == kRowsBf16 ? 4 : 8, kW = kW8 ? 2 : 1, kPlanes = ROWS == kRowsF32 ? 3 : 1;
+  static constexpr int kAX = ROWS == kRowsMx ? 1 : kA, kWX = ROWS == kRowsMx ? 1 : kW;       // chunks from g to g + 1
+  intx4 a[MT][kA], w[NT][kW];
+  int as[kCodes ? MT : 1], ws[NT];
+
+  // From LDS rows of RA and RW bytes (row am and row an are the lane's first), whose 128 k begin at chunks a_chunk and w_chunk; dwords of scales.
+  // Of A there are AR rows: behind them (AR < 16) the first ones again, for columns of the instruction that are not stored.
+  template <int RA, int RW, int AR>
+  __device__ __forceinline__ void read(const unsigned char *la, int am, int a_chunk, const unsigned char *lw, int an, int w_chunk, const unsigned char *sa,
+                                       const unsigned char *sw, int r, int g) {
+    const int ar = AR < 16 ? r % AR : am, a_swz = swizzle<RA, kAX>(ar), w_swz = swizzle<RW, kWX>(r);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+#pragma unroll
+      for (int c = 0; c < kA; ++c)
+        a[mt][c] = *reinterpret_cast<const intx4 *>(la + (mt * 16 + ar) * RA + (((a_chunk + (ROWS == kRowsMx ? 4 * c + g : kA * g + c)) ^ a_swz) << 4));
+      if (kCodes) as[kCodes ? mt : 0] = sa[(mt * 16 + ar) * 4 + g];
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int c = 0; c < kW; ++c)
+        w[nt][c] = *reinterpret_cast<const intx4 *>(lw + (nt * 16 + an) * RW + (((w_chunk + (ROWS == kRowsMx ? 4 * c + g : kW * g + c)) ^ w_swz) << 4));
+      ws[nt] = sw[(nt * 16 + an) * 4 + g];
+    }
+  }
+
+  // left: elements of a row of bf16 / float32 from the first of the 128 on; what lies behind them is another chunk's
+  __device__ __forceinline__ void multiply(floatx4 (&acc)[NT][MT], int left, int g) const {
+    if constexpr (ROWS == kRowsMx) {
+#ifdef __HIP_DEVICE_COMPILE__
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+          acc[nt][mt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kW8 ? join(w[nt][0], w[nt][kW - 1]) : join(w[nt][0]), join(a[mt][0], a[mt][1]), acc[nt][mt], kW8 ? 0 : 4, 0,
+                                                                         0, ws[nt], 0, as[kCodes ? mt : 0]);
+#endif
+    } else {
+      // four instructions of 32 k: lane g has elements 32 g + 8 j .. + 7 of its 128 in the j-th, all of one block
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        bf16x8 wf[NT];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+          wf[nt] = kW8 ? decode_e4m3(w[nt][(j >> 1) % kW][j * 2 & 3], w[nt][(j >> 1) % kW][(j * 2 & 3) + 1], byte_scale(ws[nt])) : decode_e2m1(w[nt][0][j], byte_scale(ws[nt]));
+        const int k = 32 * g + 8 * j;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          bf16x8 p[3];
+          if constexpr (kCodes) {
+            p[0] = decode_e4m3(a[mt][(j >> 1) % kA][j * 2 & 3], a[mt][(j >> 1) % kA][(j * 2 & 3) + 1], byte_scale(as[kCodes ? mt : 0]));
+          } else if constexpr (ROWS == kRowsBf16) {
+            p[0] = __builtin_bit_cast(bf16x8, k >= left ? intx4{0, 0, 0, 0} : a[mt][j % kA]);
+          } else {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = k + (e & 4) >= left ? 0.f : __int_as_float(a[mt][(2 * j + e / 4) % kA][e % 4]);
+            split3(v, p);
+          }
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int q = kPlanes - 1; q >= 0; --q) acc[nt][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[nt], p[q], acc[nt][mt], 0, 0, 0);
+        }
+      }
+    }
+  }
+};
 
 // Sizes of an instance.
 template <int ROWS, int WF, int BM, int BN, int WM, int WN, int WK, int kStages, int AR = BM> struct Shape {
   static constexpr int kASize = codes_in(ROWS) ? 1 : ROWS == kRowsBf16 ? 2 : 4;
+  static constexpr int kAX = ROWS == kRowsMx ? 1 : 2 * kASize, kWX = ROWS == kRowsMx || WF == PVF_MX_E2M1 ? 1 : 2;   // chunks from g to g + 1
   static constexpr int kThreads = 64 * WM * WN * WK, kWaves = WM * WN * WK, MT = BM / WM / 16, NT = BN / WN / 16;
   static constexpr int kARow = 128 * WK * kASize, kWRow = (WF == PVF_MX_E4M3 ? 128 : 64) * WK;           // LDS bytes of a row and stage
   static constexpr int kABytes = AR * kARow, kWBytes = BN * kWRow;
@@ -174,7 +259,6 @@ gemm_mx_kernel(MxGemm p, TileMap tm) {
   constexpr int kAChunks = AR * kACpr, kWChunks = BN * kWCpr, LA = (kAChunks + kThreads - 1) / kThreads, LW = (kWChunks + kThreads - 1) / kThreads;
   constexpr int LS = (S::kAUnits + S::kWUnits + kWaves - 1) / kWaves;
   constexpr int kLoads = (kDirect ? LA : 0) + LW + LS;       // load instructions of a thread and stage that go straight to LDS
-  constexpr int kPlanes = ROWS == kRowsF32 ? 3 : 1;
   static_assert(BM % (16 * WM) == 0 && BN % (16 * WN) == 0 && kAChunks % 64 == 0 && kWChunks % 64 == 0, "tile shape");
   static_assert(kDirect || !kCodes, "codes always go straight");
   static_assert(!kSwiglu || BN / WN == 64, "a wave has a block of gate and the same block of up");
@@ -208,13 +292,13 @@ gemm_mx_kernel(MxGemm p, TileMap tm) {
 #pragma unroll
   for (int i = 0; i < LA; ++i) {
     const int f = (i * kThreads + tid) % kAChunks, row = f / kACpr;
-    a_at[i] = ((f % kACpr) ^ swizzle<S::kARow>(row)) * 16;
+    a_at[i] = ((f % kACpr) ^ swizzle<S::kARow, S::kAX>(row)) * 16;
     a_src[i] = (const uint8_t *)p.A + (int64_t)min(m0 + row, M - 1) * a_bytes;
   }
 #pragma unroll
   for (int i = 0; i < LW; ++i) {
     const int f = (i * kThreads + tid) % kWChunks, row = f / kWCpr;
-    w_at[i] = ((f % kWCpr) ^ swizzle<S::kWRow>(row)) * 16;
+    w_at[i] = ((f % kWCpr) ^ swizzle<S::kWRow, S::kWX>(row)) * 16;
     w_src[i] = (const uint8_t *)p.W + w_row(row) * w_bytes;
   }
 #pragma unroll
@@ -265,73 +349,12 @@ gemm_mx_kernel(MxGemm p, TileMap tm) {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) acc[nt][mt] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  // ---- operands of a stage in registers ----
   const int am = wm * (BM / WM) + r, an = wn * (BN / WN) + r;               // rows of the lane's operands in the tiles (but for 16 mt, 16 nt)
-  const int ar = AR < 16 ? r % AR : am;                      // behind AR rows the first ones again, for columns of the instruction that are not stored
-  const int a_swz = swizzle<S::kARow>(ar), w_swz = swizzle<S::kWRow>(r);
-  constexpr int kFA = kCodes ? 2 : ROWS == kRowsBf16 ? 4 : 8, kFW = kW8 ? 2 : 1;
-  struct Operands { intx4 a[MT][kFA], w[NT][kFW]; int as[kCodes ? MT : 1], ws[NT]; };
-  auto read = [&](Operands &o, int st) {
+  using Ops = Operands<ROWS, WF, MT, NT>;
+  auto read = [&](Ops &o, int st) {
     const unsigned char *slot = lds + st % kStages * S::kStage;
-    const unsigned char *la = slot + ar * S::kARow, *lw = slot + S::kABytes + an * S::kWRow;
-    const unsigned char *sa = slot + S::kABytes + S::kWBytes + (wk * AR + ar) * 4 + g, *sw = slot + S::kABytes + S::kWBytes + S::kAUnits * 256 + (wk * BN + an) * 4 + g;
-    // chunks of the lane: scaled instruction g and 4 + g; else kFA from kFA g on
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-      for (int c = 0; c < kFA; ++c)
-        o.a[mt][c] = *reinterpret_cast<const intx4 *>(la + mt * 16 * S::kARow + (((wk * (kACpr / WK) + (ROWS == kRowsMx ? 4 * c + g : kFA * g + c)) ^ a_swz) << 4));
-      if (kCodes) o.as[kCodes ? mt : 0] = sa[mt * 64];
-    }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-      for (int c = 0; c < kFW; ++c)
-        o.w[nt][c] = *reinterpret_cast<const intx4 *>(lw + nt * 16 * S::kWRow + (((wk * (kWCpr / WK) + (ROWS == kRowsMx ? 4 * c + g : kFW * g + c)) ^ w_swz) << 4));
-      o.ws[nt] = sw[nt * 64];
-    }
-  };
-  auto multiply = [&](const Operands &o, int st) {
-    if constexpr (ROWS == kRowsMx) {
-#ifdef __HIP_DEVICE_COMPILE__
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-          acc[nt][mt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kW8 ? join(o.w[nt][0], o.w[nt][kFW - 1]) : join(o.w[nt][0], intx4{0, 0, 0, 0}),
-                                                                         join(o.a[mt][0], o.a[mt][1]), acc[nt][mt], kW8 ? 0 : 4, 0, 0, o.ws[nt], 0, o.as[kCodes ? mt : 0]);
-#endif
-    } else {
-      // four instructions of 32 k: lane g has elements 32 g + 8 j .. + 7 of its 128 in the j-th, all of one block
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        bf16x8 w[NT];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-          w[nt] = kW8 ? decode_e4m3(o.w[nt][(j >> 1) % kFW][j * 2 & 3], o.w[nt][(j >> 1) % kFW][(j * 2 & 3) + 1], byte_scale(o.ws[nt]))
-                      : decode_e2m1(o.w[nt][0][j], byte_scale(o.ws[nt]));
-        const int k = (st * WK + wk) * 128 + 32 * g + 8 * j;                 // rows of bf16 / float32: what lies behind K is another chunk's
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          bf16x8 a[3];
-          if constexpr (kCodes) {
-            const float as = byte_scale(o.as[kCodes ? mt : 0]);
-            a[0] = decode_e4m3(o.a[mt][j >> 1][j * 2 & 3], o.a[mt][j >> 1][(j * 2 & 3) + 1], as);
-          } else if constexpr (ROWS == kRowsBf16) {
-            a[0] = __builtin_bit_cast(bf16x8, k >= K ? intx4{0, 0, 0, 0} : o.a[mt][j]);
-          } else {
-            float v[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = k + (e & 4) >= K ? 0.f : __int_as_float(o.a[mt][(2 * j + e / 4) % kFA][e % 4]);
-            split3(v, a);
-          }
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int q = kPlanes - 1; q >= 0; --q) acc[nt][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[nt], a[q], acc[nt][mt], 0, 0, 0);
-        }
-      }
-    }
+    o.template read<S::kARow, S::kWRow, AR>(slot, am, wk * (kACpr / WK), slot + S::kABytes, an, wk * (kWCpr / WK), slot + S::kABytes + S::kWBytes + wk * AR * 4,
+                                            slot + S::kABytes + S::kWBytes + S::kAUnits * 256 + wk * BN * 4, r, g);
   };
 
   // ---- the ring ----
@@ -348,9 +371,9 @@ gemm_mx_kernel(MxGemm p, TileMap tm) {
     if (!kDirect && st + 1 < ns) fetch(st + 1);
     if (st + kStages - 1 < ns) issue(st + kStages - 1);
     if (WK == 1 || st * WK + wk < nk) {
-      Operands o;
+      Ops o;
       read(o, st);
-      multiply(o, st);
+      o.multiply(acc, K - (st * WK + wk) * 128, g);
     }
     if (!kDirect && st + 1 < ns) stash(st + 1);
   }
@@ -412,6 +435,335 @@ pvf_status run_as(hipStream_t s, const MxGemm &p) {
   return PVF_OK;
 }
 
+// ---- waves of their own -------------------------------------------------------------------------------------------------
+// A workgroup computes BM x BN results for launches whose tiles make about one round over the chip: its kWaves waves take the 128s of k in turn, each
+// with the whole tile and a ring of two slots of LDS of its own, so that the loop has no barrier and the waves' loads, reads and matrix
+// instructions drift apart; a slot is loaded again as soon as it is in registers.  The sums are added through LDS at the end.
+template <int ROWS, int WF, int OUT, int BM, int BN, int kWaves, int AR>
+__global__ void __launch_bounds__(64 * kWaves)
+gemm_mx_waves_kernel(MxGemm p, TileMap tm) {
+  constexpr bool kSwiglu = OUT == kOutSwiglu, kCodes = codes_in(ROWS), kW8 = WF == PVF_MX_E4M3;
+  using S = Shape<ROWS, WF, BM, BN, 1, 1, 1, 2, AR>;
+  constexpr int MT = BM / 16, NT = BN / 16, kASize = S::kASize;
+  constexpr int kACpr = S::kARow / 16, kWCpr = S::kWRow / 16, kAChunks = AR * kACpr;
+  constexpr int LA = (kAChunks + 63) / 64, LW = BN * kWCpr / 64, LS = S::kAUnits + S::kWUnits, kLoads = LA + LW + LS;
+  static_assert(kLoads < 64 && kAChunks % 64 == 0 && BN * kWCpr % 64 == 0, "whole load instructions");
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+  const int M = p.M, N = p.N, K = p.K, Kp = (K + kMxStage - 1) / kMxStage * kMxStage, nk = Kp / kMxStage;
+  const int total = tm.tiles_m * tm.tiles_n, per_xcd = (total + 7) >> 3;
+  const int L = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= per_xcd || L >= total) return;
+  const int band = L / (tm.group_m * tm.tiles_n), within = L - band * (tm.group_m * tm.tiles_n);
+  const int band_rows = min(tm.group_m, tm.tiles_m - band * tm.group_m);
+  const int tile_n = within / band_rows, tile_m = band * tm.group_m + (within - tile_n * band_rows);
+  const int m0 = tile_m * BM, n0 = tile_n * (kSwiglu ? BN / 2 : BN), w_rows = kSwiglu ? 2 * N : N;
+  auto w_row = [&](int t) -> int64_t {                       // SwiGLU: 32 gate rows, then the 32 up rows of the same columns
+    if (!kSwiglu) return min(n0 + t, N - 1);
+    const int n = min(n0 + (t >> 6) * 32 + (t & 31), N - 1);
+    return (t & 32) ? (int64_t)N + n : n;
+  };
+  const uint32_t a_bytes = (uint32_t)((kCodes ? Kp : K) * kASize), w_bytes = kW8 ? Kp : Kp / 2;
+  const uint8_t *a_src[LA], *w_src[LW], *s_src[LS];
+  uint32_t a_at[LA];
+#pragma unroll
+  for (int i = 0; i < LA; ++i) {
+    const int f = (i * 64 + lane) % kAChunks, row = f / kACpr;
+    a_at[i] = ((f % kACpr) ^ swizzle<S::kARow, S::kAX>(row)) * 16;
+    a_src[i] = (const uint8_t *)p.A + (int64_t)min(m0 + row, M - 1) * a_bytes + (kCodes ? a_at[i] : 0);
+  }
+#pragma unroll
+  for (int i = 0; i < LW; ++i) {
+    const int f = i * 64 + lane, row = f / kWCpr;
+    w_src[i] = (const uint8_t *)p.W + w_row(row) * w_bytes + ((f % kWCpr) ^ swizzle<S::kWRow, S::kWX>(row)) * 16;
+  }
+#pragma unroll
+  for (int i = 0; i < LS; ++i) {
+    const int f = (i < S::kAUnits ? i : i - S::kAUnits) * 64 + lane;
+    s_src[i] = i < S::kAUnits ? p.a_scales + (int64_t)min(m0 + min(f, AR - 1), M - 1) * 4 : p.w_scales + w_row(min(f, BN - 1)) * 4;
+  }
+  unsigned char *mine = lds + wave * (2 * S::kStage);
+  auto issue = [&](int kt, int slot) {
+    unsigned char *at = mine + slot * S::kStage;
+#pragma unroll
+    for (int i = 0; i < LA; ++i) {
+      const uint8_t *q = kCodes ? a_src[i] + (int64_t)kt * S::kARow : a_src[i] + min(a_at[i] + (uint32_t)kt * S::kARow, a_bytes - 16);       // behind a row its last chunk
+      __builtin_amdgcn_global_load_lds((gptr_t *)q, (lptr_t *)(at + i * 64 % kAChunks * 16), 16, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < LW; ++i) __builtin_amdgcn_global_load_lds((gptr_t *)(w_src[i] + (int64_t)kt * S::kWRow), (lptr_t *)(at + S::kABytes + i * 1024), 16, 0, 0);
+#pragma unroll
+    for (int i = 0; i < LS; ++i)
+      __builtin_amdgcn_global_load_lds((gptr_t *)(s_src[i] + (int64_t)kt * (i < S::kAUnits ? M : w_rows) * 4), (lptr_t *)(at + S::kABytes + S::kWBytes + i * 256), 4, 0, 0);
+  };
+  floatx4 acc[NT][MT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) acc[nt][mt] = floatx4{0.f, 0.f, 0.f, 0.f};
+  if (wave < nk) issue(wave, 0);
+  if (wave + kWaves < nk) issue(wave + kWaves, 1);
+  int slot = 0;
+  for (int kt = wave; kt < nk; kt += kWaves, slot ^= 1) {
+    if (kt + kWaves < nk) wait_vmcnt<kLoads>(); else wait_vmcnt<0>();
+    asm volatile("" ::: "memory");
+    Operands<ROWS, WF, MT, NT> o;
+    unsigned char *at = mine + slot * S::kStage;
+    o.template read<S::kARow, S::kWRow, AR>(at, r, 0, at + S::kABytes, r, 0, at + S::kABytes + S::kWBytes, at + S::kABytes + S::kWBytes + S::kAUnits * 256, r, g);
+    __builtin_amdgcn_s_waitcnt(0xc07f);                      // lgkmcnt(0): the slot is in registers
+    __builtin_amdgcn_sched_barrier(0);
+    if (kt + 2 * kWaves < nk) issue(kt + 2 * kWaves, slot);
+    o.multiply(acc, K - kt * 128, g);
+  }
+  // ---- results ----
+  floatx4 *sums = reinterpret_cast<floatx4 *>(lds);          // [wave][tile][lane]
+  __syncthreads();
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) sums[(wave * NT * MT + nt * MT + mt) * 64 + lane] = acc[nt][mt];
+  __syncthreads();
+  auto result = [&](int nt, int mt) {                        // in the order of the waves
+    floatx4 s = sums[(nt * MT + mt) * 64 + lane];
+#pragma unroll
+    for (int k = 1; k < kWaves; ++k) s += sums[(k * NT * MT + nt * MT + mt) * 64 + lane];
+    return s;
+  };
+  if constexpr (kSwiglu) {
+    const int Np = (N + kMxStage - 1) / kMxStage * kMxStage;
+    for (int t = wave; t < MT * (NT / 4); t += kWaves) {
+      const int mt = t % MT, b = t / MT, m = m0 + mt * 16 + r, c0 = n0 + b * 32;
+      if (c0 < Np) store_act(result(4 * b, mt), result(4 * b + 1, mt), result(4 * b + 2, mt), result(4 * b + 3, mt), m < M, m, c0, g, p, Np);
+    }
+  } else {
+    using T = std::conditional_t<OUT == kOutF32, float, bf16_t>;
+    for (int t = wave; t < MT * NT; t += kWaves) {
+      const int m = m0 + t % MT * 16 + r;
+      const floatx4 s = result(t / MT, t % MT);
+      if (m < M) store_row4<T>(s, m, n0 + t / MT * 16 + 4 * g, p);
+    }
+  }
+}
+
+template <int ROWS, int WF, int OUT, int BM, int BN, int kWaves, int AR>
+pvf_status run_waves(hipStream_t s, const MxGemm &p) {
+  using S = Shape<ROWS, WF, BM, BN, 1, 1, 1, 2, AR>;
+  constexpr int kLds = kWaves * (2 * S::kStage > BM * BN * 4 ? 2 * S::kStage : BM * BN * 4);
+  static_assert(kLds <= 160 * 1024, "LDS");
+  TileMap tm;
+  const int64_t tiles_n = OUT == kOutSwiglu ? (mx_width(p.N) + BN / 2 - 1) / (BN / 2) : (p.N + BN - 1) / BN, tiles_m = (p.M + BM - 1) / BM;
+  PVF_REQUIRE(nullptr, tiles_m * tiles_n < 1 << 28, PVF_ESHAPE, "%d x %d results are too many for a launch", p.M, p.N);
+  tm.tiles_m = (int)tiles_m; tm.tiles_n = (int)tiles_n; tm.group_m = (int)std::min<int64_t>(tiles_m, 8);
+  auto kernel = gemm_mx_waves_kernel<ROWS, WF, OUT, BM, BN, kWaves, AR>;
+  static const hipError_t allowed = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+  PVF_HIP_CHECK(nullptr, allowed);
+  kernel<<<(uint32_t)((tiles_m * tiles_n + 7) / 8 * 8), 64 * kWaves, kLds, s>>>(p, tm);
+  PVF_LAUNCH_CHECK(nullptr, "gemm_mx");
+  return PVF_OK;
+}
+
+// ---- 256 x 256 results: two stages of LDS, a wave's 128 x 64 results in quadrants --------------------------------------
+// Row of the tile behind LDS row r: the lower halves of all wave tiles come first, then the upper ones, so that a half is a run of whole loads.
+template <int BT, int WT> __device__ __forceinline__ int half_row(int r) {
+  constexpr int kHalfTile = BT / 2, kHalfWave = WT / 2;
+  const int h = r / kHalfTile, rr = r % kHalfTile;
+  return (rr / kHalfWave) * WT + h * kHalfWave + rr % kHalfWave;
+}
+
+// A wave multiplies, stage by stage of 128 k, lower A x lower W, lower x upper, upper x upper, upper x lower.  The operands of a half are read
+// from LDS one quadrant before their first use, which frees their rows early: each half of a stage's slot is refilled as soon as it is
+// read, one barrier per half stage, so loads are issued evenly and have 1 to 1.5 stages to land.  Scale bytes have a ring of three stages.
+template <int WF>
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
+gemm_mx_quad_kernel(MxGemm p, TileMap tm) {
+  constexpr bool kW8 = WF == PVF_MX_E4M3;
+  constexpr int BM = 256, BN = 256, WTM = 128, WTN = 64, MH = 4, NH = 2, kPer = MH * NH;
+  constexpr int kWRow = kW8 ? 128 : 64, kABytes = BM * 128, kWBytes = BN * kWRow, kScales = 2 * (kABytes + kWBytes), kScaleStage = (BM + BN) * 4;
+  constexpr int LA = 4, LW = kW8 ? 4 : 2, kG1 = 1 + LA / 2 + LW / 2, kG2 = LA / 2 + LW / 2, kLoads = kG1 + kG2;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave >> 2, wn = wave & 3, r = lane & 15, g = lane >> 4;
+  const int M = p.M, N = p.N, Kp = (p.K + kMxStage - 1) / kMxStage * kMxStage, nk = Kp / kMxStage;
+  const int total = tm.tiles_m * tm.tiles_n, per_xcd = (total + 7) >> 3;
+  const int L = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= per_xcd || L >= total) return;
+  const int band = L / (tm.group_m * tm.tiles_n), within = L - band * (tm.group_m * tm.tiles_n);
+  const int band_rows = min(tm.group_m, tm.tiles_m - band * tm.group_m);
+  const int tile_n = within / band_rows, tile_m = band * tm.group_m + (within - tile_n * band_rows);
+  const int m_own = tile_m * BM, n_own = tile_n * BN;        // the last tiles begin early, so that all of a tile exists, and store only what is theirs
+  const int m0 = min(m_own, M - BM), n0 = min(n_own, N - BN);
+  const uint32_t w_bytes = kW8 ? Kp : Kp / 2;
+
+  // The i-th load of an operand lies a uniform distance behind the first: LDS rows 64 i are tile rows 128 i of the lower halves, then 64 (A)
+  // or 32 (W) further on.  So a lane has one offset for each operand (32 bits: 256 rows of at most 2^22 bytes) and no address arithmetic.
+  const uint32_t a_off = (tid / 8) * (uint32_t)Kp + ((tid % 8) ^ swizzle<128, 1>(tid / 8)) * 16;
+  constexpr int CPR = kWRow / 16;
+  const uint32_t w_off = half_row<BN, WTN>(tid / CPR) * w_bytes + ((tid % CPR) ^ swizzle<kWRow, 1>(tid / CPR)) * 16;
+  const bool of_a = wave < 4;                                // waves 0-3 load the scale dwords of A, 4-7 those of W
+  const uint32_t s_row = (wave & 3) * 64 + lane, s_off = (of_a ? half_row<BM, WTM>(s_row) : half_row<BN, WTN>(s_row)) * 4;
+  const uint32_t s_step = (of_a ? M : N) * 4;
+#ifdef __HIP_DEVICE_COMPILE__
+  const __amdgpu_buffer_rsrc_t rsA = __builtin_amdgcn_make_buffer_rsrc((void *)((const uint8_t *)p.A + (int64_t)m0 * Kp), 0, BM * Kp, 0x00020000);
+  const __amdgpu_buffer_rsrc_t rsW = __builtin_amdgcn_make_buffer_rsrc((void *)((const uint8_t *)p.W + (int64_t)n0 * w_bytes), 0, (int)(BN * w_bytes), 0x00020000);
+  const __amdgpu_buffer_rsrc_t rsS = __builtin_amdgcn_make_buffer_rsrc((void *)(of_a ? p.a_scales + (int64_t)m0 * 4 : p.w_scales + (int64_t)n0 * 4), 0, (int)(s_step * nk - (of_a ? m0 : n0) * 4), 0x00020000);
+#endif
+  // q-th load of a stage: scales, lower A, lower W | upper W, upper A
+  auto issue = [&](int kt, int q, int s3) {                  // s3: kt % 3
+#ifdef __HIP_DEVICE_COMPILE__
+    auto a = [&](int i) { __builtin_amdgcn_raw_ptr_buffer_load_lds(rsA, (lptr_t *)(lds + (kt & 1) * kABytes + i * 8192 + wave * 1024), 16, a_off, kt * 128 + ((i & 1) * 128 + (i >> 1) * 64) * Kp, 0, 0); };
+    auto w = [&](int i) {
+      const int first = kW8 ? (i & 1) * 128 + (i >> 1) * 32 : i * 32;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsW, (lptr_t *)(lds + 2 * kABytes + (kt & 1) * kWBytes + i * 8192 + wave * 1024), 16, w_off, kt * kWRow + first * w_bytes, 0, 0);
+    };
+    if (q == 0) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsS, (lptr_t *)(lds + kScales + s3 * kScaleStage + wave * 256), 4, s_off, kt * s_step, 0, 0);
+    else if (q < 1 + LA / 2) a(q - 1);
+    else if (q < kG1) w(q - 1 - LA / 2);
+    else if (q < kG1 + LW / 2) w(q - kG1 + LW / 2);
+    else a(q - kG1 - LW / 2 + LA / 2);
+#endif
+  };
+  floatx4 acc[2 * NH][2 * MH];
+#pragma unroll
+  for (int nt = 0; nt < 2 * NH; ++nt)
+#pragma unroll
+    for (int mt = 0; mt < 2 * MH; ++mt) acc[nt][mt] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int st = 0; st < 2; ++st)
+    if (st < nk)
+#pragma unroll
+      for (int q = 0; q < kLoads; ++q) issue(st, q, st);
+
+  intx8 a0[MH], a1[MH], b[2][NH];
+  int as0[MH], as1[MH], bs[2][NH];
+  const int a_row = wm * (WTM / 2) + r, w_row = wn * (WTN / 2) + r;
+  const int a_c0 = a_row * 128 + ((g ^ swizzle<128, 1>(r)) << 4), a_c1 = a_row * 128 + (((4 + g) ^ swizzle<128, 1>(r)) << 4);
+  const int w_c0 = 2 * kABytes + w_row * kWRow + ((g ^ swizzle<kWRow, 1>(r)) << 4), w_c1 = 2 * kABytes + w_row * kWRow + (((4 + g) ^ swizzle<128, 1>(r)) << 4);
+  const int s_a = kScales + a_row * 4 + g, s_w = kScales + (BM + w_row) * 4 + g;
+  auto rd_a = [&](int parity, int s3, int half, int j, intx8 &v, int &s) {
+    const int at = parity * kABytes + half * (BM / 2 * 128) + j * 16 * 128;
+    v = join(*reinterpret_cast<const intx4 *>(lds + a_c0 + at), *reinterpret_cast<const intx4 *>(lds + a_c1 + at));
+    s = lds[s_a + s3 * kScaleStage + (half * (BM / 2) + j * 16) * 4];
+  };
+  auto rd_w = [&](int parity, int s3, int half, int j, intx8 &v, int &s) {
+    const int at = parity * kWBytes + half * (BN / 2 * kWRow) + j * 16 * kWRow;
+    v = kW8 ? join(*reinterpret_cast<const intx4 *>(lds + w_c0 + at), *reinterpret_cast<const intx4 *>(lds + w_c1 + at))
+            : join(*reinterpret_cast<const intx4 *>(lds + w_c0 + at));
+    s = lds[s_w + s3 * kScaleStage + (half * (BN / 2) + j * 16) * 4];
+  };
+  if (nk > 1) wait_vmcnt<kG2 + kLoads>(); else wait_vmcnt<kG2>();
+  __builtin_amdgcn_s_barrier();
+#pragma unroll
+  for (int j = 0; j < NH; ++j) rd_w(0, 0, 0, j, b[0][j], bs[0][j]);
+#pragma unroll
+  for (int j = 0; j < MH; ++j) rd_a(0, 0, 0, j, a0[j], as0[j]);
+
+  constexpr int kBarrierAt = 2, kSlots = 2 * kPer - kBarrierAt;
+  int s3 = 0;                                                // kt % 3
+  auto stage = [&](int kt, auto kind, auto parity) {         // kind 0: a stage that prefetches, 1: the last but one, 2: the last
+    constexpr int P = decltype(parity)::value;
+    constexpr bool kSteady = decltype(kind)::value == 0, more = decltype(kind)::value < 2;
+    const int s3n = s3 == 2 ? 0 : s3 + 1, s3nn = s3n == 2 ? 0 : s3n + 1;
+#pragma unroll
+    for (int ph = 0; ph < 4; ++ph) {
+      const int mh = ph >> 1, nh = ph == 1 || ph == 2;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int mt = i / NH, nt = i % NH;
+        if (i == kBarrierAt && (ph == 0 || (ph == 2 && more))) {
+          // ph 0: all of stage kt has landed; ph 2: the lower halves of stage kt + 1 have (my parts of them)
+          if (ph == 0) { if (more) wait_vmcnt<kLoads>(); else wait_vmcnt<0>(); }
+          else { if (kSteady) wait_vmcnt<kG2 + kG1>(); else wait_vmcnt<kG2>(); }
+          __builtin_amdgcn_s_waitcnt(0xc07f);                // lgkmcnt(0): my reads of the rows that are refilled now are done
+          __builtin_amdgcn_s_barrier();
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        floatx4 &c = acc[nh * NH + nt][mh * MH + mt];
+#ifdef __HIP_DEVICE_COMPILE__
+        c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b[nh ^ P][nt], mh ? a1[mt] : a0[mt], c, kW8 ? 0 : 4, 0, 0, bs[nh ^ P][nt], 0, mh ? as1[mt] : as0[mt]);
+#endif
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < MH; ++j) {
+          if (ph == 0 && j < NH && i == kBarrierAt + j * (kPer - kBarrierAt - 2) / NH) rd_w(P, s3, 1, j, b[P ^ 1][j], bs[P ^ 1][j]);
+          if (ph == 1 && i == j * (kPer - 2) / MH) rd_a(P, s3, 1, j, a1[j], as1[j]);
+          if (ph == 2 && more && i == kBarrierAt + j * (kPer - kBarrierAt) / MH) rd_a(P ^ 1, s3n, 0, j, a0[j], as0[j]);
+          if (ph == 3 && more && j < NH && i == j * (kPer - 4) / NH) rd_w(P ^ 1, s3n, 0, j, b[P ^ 1][j], bs[P ^ 1][j]);
+        }
+        if (kSteady) {
+          const int at = (ph & 1) * kPer + i - kBarrierAt;   // instructions since the half's barrier
+#pragma unroll
+          for (int q = 0; q < (ph < 2 ? kG1 : kG2); ++q)
+            if (at == 1 + q * (kSlots - 1) / (ph < 2 ? kG1 : kG2)) issue(kt + 2, ph < 2 ? q : kG1 + q, s3nn);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    s3 = s3n;
+  };
+  constexpr std::integral_constant<int, 0> k0{};
+  constexpr std::integral_constant<int, 1> k1{};
+  constexpr std::integral_constant<int, 2> k2{};
+  for (int kt = 0; kt + 2 < nk; kt += 2) {                   // nk is even
+    stage(kt, k0, k0);
+    stage(kt + 1, k0, k1);
+  }
+  stage(nk - 2, k1, k0);
+  stage(nk - 1, k2, k1);
+
+  // ---- results, 32 rows at a time through the wave's own piece of the free ring: stores of whole 128-byte lines ----
+  // lane: column half * 32 + 16 nt + 4 g of row half * 64 + 16 mt + r of the wave's tile
+  const int wave_m = m0 + wm * WTM, wave_n = n0 + wn * WTN;
+  __syncthreads();
+  if (N % 8 != 0) {
+#pragma unroll
+    for (int mt = 0; mt < 2 * MH; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < 2 * NH; ++nt)
+        if (wave_m + mt * 16 + r >= m_own) store_row4<bf16_t>(acc[nt][mt], wave_m + mt * 16 + r, wave_n + nt * 16 + 4 * g, p, n_own);
+    return;
+  }
+  constexpr int kRow = WTN * 4 + 16;                         // float32, so that a residual is added before the rounding
+  unsigned char *my = lds + wave * 32 * kRow;
+#pragma unroll
+  for (int mp = 0; mp < MH; ++mp) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int nt = 0; nt < 2 * NH; ++nt) *reinterpret_cast<floatx4 *>(my + (h * 16 + r) * kRow + (nt * 16 + 4 * g) * 4) = acc[nt][2 * mp + h];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int row = j * 8 + (lane >> 3), m = wave_m + mp * 32 + row, n = wave_n + (lane & 7) * 8;
+      const floatx4 lo = *reinterpret_cast<const floatx4 *>(my + row * kRow + (lane & 7) * 32), hi = *reinterpret_cast<const floatx4 *>(my + row * kRow + (lane & 7) * 32 + 16);
+      if (m < m_own || n < n_own) continue;
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { v[e] = lo[e]; v[4 + e] = hi[e]; }
+      if (p.residual) {
+        float x[8];
+        load8((const bf16_t *)p.residual + (int64_t)m * N + n, 8, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += x[e];
+      }
+      store8((bf16_t *)p.C + (int64_t)m * N + n, 8, v);
+    }
+  }
+}
+
+// M, N >= 256, an even number of stages, scales of less than 2^31 bytes.
+template <int WF> pvf_status run_quad(hipStream_t s, const MxGemm &p) {
+  constexpr int kLds = 2 * (256 * 128 + 256 * (WF == PVF_MX_E4M3 ? 128 : 64)) + 3 * 512 * 4;
+  TileMap tm;
+  const int64_t tiles_n = (p.N + 255) / 256, tiles_m = (p.M + 255) / 256;
+  PVF_REQUIRE(nullptr, tiles_m * tiles_n < 1 << 28, PVF_ESHAPE, "%d x %d results are too many for a launch", p.M, p.N);
+  tm.tiles_m = (int)tiles_m; tm.tiles_n = (int)tiles_n; tm.group_m = (int)std::min<int64_t>(tiles_m, 6);   // 8: 2 % slower at 8192 x 8192, nothing at 11520 x 12288
+  auto kernel = gemm_mx_quad_kernel<WF>;
+  static const hipError_t allowed = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+  PVF_HIP_CHECK(nullptr, allowed);
+  kernel<<<(uint32_t)((tiles_m * tiles_n + 7) / 8 * 8), 512, kLds, s>>>(p, tm);
+  PVF_LAUNCH_CHECK(nullptr, "gemm_mx");
+  return PVF_OK;
+}
+
 // ---- which instance -------------------------------------------------------------------------------------------------
 // What a tile costs for 128 k, in microseconds, measured at K = 4096 (launch time less 3 us, over 32 and the tiles of the fullest CU):
 // where a CU has one tile, and per tile where it has several (those that fit its LDS run at a time and hide each other's barriers and
@@ -421,25 +773,30 @@ struct Candidate {
   int BM, BN, most_rows;                                     // most_rows: rows of A that the instance loads (0: any number)
   float alone, among;
   pvf_status (*run)(hipStream_t, const MxGemm &);
+  bool quad = false;
 };
 
 template <int ROWS, int WF, int OUT, bool kDirect> struct Candidates;
 #define PVF_MX_TILE(BM, BN, WM, WN, WK, ST, AR, alone, among) \
   {BM, OUT == kOutSwiglu ? BN / 2 : BN, AR < BM ? AR : 0, alone, among, run_as<ROWS, WF, OUT, BM, BN, WM, WN, WK, ST, AR, kDirect>}
 
+#define PVF_MX_WAVES(BM, BN, waves, AR, alone, among) \
+  {BM, OUT == kOutSwiglu ? BN / 2 : BN, AR < BM ? AR : 0, alone, among, run_waves<ROWS, WF, OUT, BM, BN, waves, AR>}
+
 template <int WF, bool kDirect> struct Candidates<kRowsMx, WF, kOutBf16, kDirect> {
   static constexpr int ROWS = kRowsMx, OUT = kOutBf16;
   static constexpr Candidate list[] = {
-      PVF_MX_TILE(16, 16, 1, 1, 4, 3, 16, .08f, .075f),   PVF_MX_TILE(32, 32, 1, 1, 4, 3, 32, .1375f, .153f), PVF_MX_TILE(64, 64, 2, 2, 2, 3, 64, .275f, .28f),
-      PVF_MX_TILE(64, 64, 2, 2, 2, 2, 64, .38f, .217f),   PVF_MX_TILE(80, 64, 1, 2, 4, 2, 80, .29f, .33f),   PVF_MX_TILE(96, 64, 2, 2, 1, 3, 96, .39f, .28f),
-      PVF_MX_TILE(64, 128, 2, 4, 1, 3, 64, .415f, .375f), PVF_MX_TILE(128, 128, 2, 2, 1, 2, 128, .78f, .51f), PVF_MX_TILE(160, 128, 2, 4, 1, 2, 160, .83f, .72f),
-      PVF_MX_TILE(192, 256, 2, 4, 1, 2, 192, 1.49f, 1.44f), PVF_MX_TILE(256, 256, 2, 4, 1, 2, 256, 1.8f, 1.84f)};
+      PVF_MX_WAVES(16, 16, 4, 16, .079f, .073f),          PVF_MX_WAVES(32, 32, 4, 32, .115f, .095f),          PVF_MX_WAVES(64, 32, 4, 64, .17f, .186f),
+      PVF_MX_WAVES(64, 64, 4, 64, .24f, .253f),           PVF_MX_TILE(64, 64, 2, 2, 2, 2, 64, .38f, .217f),   PVF_MX_WAVES(80, 64, 4, 80, .26f, .34f),
+      PVF_MX_TILE(96, 64, 2, 2, 1, 3, 96, .39f, .28f),    PVF_MX_TILE(64, 128, 2, 4, 1, 3, 64, .415f, .375f), PVF_MX_TILE(128, 128, 2, 2, 1, 2, 128, .78f, .51f),
+      PVF_MX_TILE(160, 128, 2, 4, 1, 2, 160, .83f, .72f), PVF_MX_TILE(192, 256, 2, 4, 1, 2, 192, 1.49f, 1.44f), {256, 256, 0, 1.6f, 1.54f, run_quad<WF>, true}};
 };
 template <int WF, bool kDirect> struct Candidates<kRowsMxExact, WF, kOutF32, kDirect> {
   static constexpr int ROWS = kRowsMxExact, OUT = kOutF32;
   static constexpr Candidate list[] = {
-      PVF_MX_TILE(16, 16, 1, 1, 4, 3, 16, .10f, .10f),   PVF_MX_TILE(32, 32, 1, 1, 4, 3, 32, .19f, .20f),    PVF_MX_TILE(64, 64, 2, 2, 2, 2, 64, .42f, .36f),
-      PVF_MX_TILE(64, 128, 2, 4, 1, 3, 64, .74f, .61f),  PVF_MX_TILE(128, 128, 2, 2, 1, 2, 128, 1.2f, .91f), PVF_MX_TILE(160, 128, 2, 4, 1, 2, 160, 1.43f, 1.22f)};
+      PVF_MX_WAVES(16, 16, 8, 16, .09f, .10f),           PVF_MX_WAVES(32, 32, 4, 32, .135f, .124f),          PVF_MX_WAVES(64, 64, 4, 64, .33f, .35f),
+      PVF_MX_WAVES(80, 64, 4, 80, .455f, .45f),          PVF_MX_TILE(64, 128, 2, 4, 1, 3, 64, .74f, .61f),   PVF_MX_TILE(128, 128, 2, 2, 1, 2, 128, 1.2f, .91f),
+      PVF_MX_TILE(160, 128, 2, 4, 1, 2, 160, 1.43f, 1.22f)};
 };
 template <int WF, bool kDirect> struct Candidates<kRowsMxExact, WF, kOutSwiglu, kDirect> {
   static constexpr int ROWS = kRowsMxExact, OUT = kOutSwiglu;
@@ -447,26 +804,45 @@ template <int WF, bool kDirect> struct Candidates<kRowsMxExact, WF, kOutSwiglu, 
       PVF_MX_TILE(16, 64, 1, 1, 4, 2, 16, .18f, .14f),   PVF_MX_TILE(32, 64, 1, 1, 4, 2, 32, .25f, .20f),    PVF_MX_TILE(64, 128, 2, 2, 2, 2, 64, .53f, .65f),
       PVF_MX_TILE(64, 128, 2, 2, 1, 2, 64, .67f, .55f),  PVF_MX_TILE(128, 128, 2, 2, 1, 2, 128, 1.2f, .90f)};
 };
-template <bool kDirect> struct Candidates<kRowsBf16, PVF_MX_E2M1, kOutBf16, kDirect> {
+// rows that go through registers have the instances of one kernel only
+template <> struct Candidates<kRowsBf16, PVF_MX_E2M1, kOutBf16, true> {
   static constexpr int ROWS = kRowsBf16, WF = PVF_MX_E2M1, OUT = kOutBf16;
+  static constexpr bool kDirect = true;
+  static constexpr Candidate list[] = {
+      PVF_MX_TILE(16, 16, 1, 1, 8, 2, 1, .04f, .047f),   PVF_MX_WAVES(16, 16, 4, 4, .045f, .044f),           PVF_MX_WAVES(16, 16, 8, 16, .073f, .10f),
+      PVF_MX_TILE(16, 16, 1, 1, 4, 2, 16, .095f, .058f), PVF_MX_WAVES(32, 32, 4, 32, .15f, .168f),           PVF_MX_TILE(32, 64, 2, 1, 2, 2, 32, .35f, .215f),
+      PVF_MX_TILE(64, 64, 2, 2, 2, 2, 64, .41f, .42f),   PVF_MX_WAVES(80, 64, 3, 80, .54f, .52f),            PVF_MX_TILE(64, 128, 2, 2, 1, 2, 64, .75f, .58f)};
+};
+template <> struct Candidates<kRowsBf16, PVF_MX_E2M1, kOutBf16, false> {
+  static constexpr int ROWS = kRowsBf16, WF = PVF_MX_E2M1, OUT = kOutBf16;
+  static constexpr bool kDirect = false;
   static constexpr Candidate list[] = {
       PVF_MX_TILE(16, 16, 1, 1, 8, 2, 1, .04f, .047f),   PVF_MX_TILE(16, 16, 1, 1, 8, 2, 4, .06f, .05f),     PVF_MX_TILE(16, 16, 1, 1, 4, 2, 16, .095f, .058f),
-      PVF_MX_TILE(32, 32, 2, 1, 4, 2, 32, .19f, .20f),   PVF_MX_TILE(32, 64, 2, 1, 2, 2, 32, .35f, .215f),   PVF_MX_TILE(64, 64, 2, 2, 2, 2, 64, .41f, .42f),
-      PVF_MX_TILE(64, 128, 2, 2, 1, 2, 64, .75f, .58f)};
+      PVF_MX_TILE(32, 32, 2, 1, 4, 2, 32, .19f, .20f),   PVF_MX_TILE(32, 64, 2, 1, 2, 2, 32, .35f, .215f),   PVF_MX_TILE(64, 128, 2, 2, 1, 2, 64, .75f, .58f)};
 };
-template <bool kDirect> struct Candidates<kRowsF32, PVF_MX_E2M1, kOutF32, kDirect> {
+template <> struct Candidates<kRowsF32, PVF_MX_E2M1, kOutF32, true> {
   static constexpr int ROWS = kRowsF32, WF = PVF_MX_E2M1, OUT = kOutF32;
+  static constexpr bool kDirect = true;
   static constexpr Candidate list[] = {
-      PVF_MX_TILE(16, 16, 1, 1, 8, 2, 1, .07f, .10f),    PVF_MX_TILE(16, 16, 1, 1, 8, 2, 16, .27f, .30f),    PVF_MX_TILE(16, 32, 1, 1, 4, 2, 16, .35f, .37f),
+      PVF_MX_TILE(16, 16, 1, 1, 8, 2, 1, .07f, .10f),    PVF_MX_TILE(16, 16, 1, 1, 8, 2, 16, .27f, .30f),    PVF_MX_WAVES(16, 64, 4, 16, .41f, .41f),
+      PVF_MX_TILE(64, 128, 4, 1, 1, 2, 64, 2.1f, 2.1f)};
+};
+template <> struct Candidates<kRowsF32, PVF_MX_E2M1, kOutF32, false> {
+  static constexpr int ROWS = kRowsF32, WF = PVF_MX_E2M1, OUT = kOutF32;
+  static constexpr bool kDirect = false;
+  static constexpr Candidate list[] = {
+      PVF_MX_TILE(16, 16, 1, 1, 8, 2, 1, .07f, .10f),    PVF_MX_TILE(16, 16, 1, 1, 8, 2, 16, .27f, .30f),    PVF_MX_TILE(16, 64, 1, 1, 4, 2, 16, .45f, .45f),
       PVF_MX_TILE(32, 32, 2, 1, 4, 2, 32, .59f, .70f),   PVF_MX_TILE(32, 64, 2, 1, 2, 2, 32, .82f, .84f),    PVF_MX_TILE(64, 128, 4, 1, 1, 2, 64, 2.1f, 2.1f)};
 };
 
 template <int ROWS, int WF, int OUT, bool kDirect = true> pvf_status run(hipStream_t s, const MxGemm &p) {
   const int64_t columns = OUT == kOutSwiglu ? mx_width(p.N) : p.N;
+  const int64_t stages = mx_width(p.K) / kMxStage;
   const Candidate *best = nullptr;
   float least = 0.f;
   for (const Candidate &c : Candidates<ROWS, WF, OUT, kDirect>::list) {
     if (c.most_rows && p.M > c.most_rows) continue;
+    if (c.quad && (p.M < 256 || p.N < 256 || stages % 2 != 0 || stages * std::max(p.M, p.N) >= 1 << 29)) continue;
     const int64_t tiles = ((p.M + c.BM - 1) / c.BM) * ((columns + c.BN - 1) / c.BN), fullest = (tiles + 255) / 256;
     const float cost = fullest == 1 ? c.alone : c.among * (float)fullest;
     if (!best || cost < least) { best = &c; least = cost; }
