@@ -173,36 +173,42 @@ template <int ROWS, int WF, int MT, int NT> struct Operands {
   template <int RA, int RW, int AR>
   __device__ __forceinline__ void read(const unsigned char *la, int am, int a_chunk, const unsigned char *lw, int an, int w_chunk, const unsigned char *sa,
                                        const unsigned char *sw, int r, int g) {
-    const int ar = AR < 16 ? r % AR : am, a_swz = swizzle<RA, kAX>(ar), w_swz = swizzle<RW, kWX>(r);
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-      for (int c = 0; c < kA; ++c)
-        a[mt][c] = *reinterpret_cast<const intx4 *>(la + (mt * 16 + ar) * RA + (((a_chunk + (ROWS == kRowsMx ? 4 * c + g : kA * g + c)) ^ a_swz) << 4));
-      if (kCodes) as[kCodes ? mt : 0] = sa[(mt * 16 + ar) * 4 + g];
-    }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-      for (int c = 0; c < kW; ++c)
-        w[nt][c] = *reinterpret_cast<const intx4 *>(lw + (nt * 16 + an) * RW + (((w_chunk + (ROWS == kRowsMx ? 4 * c + g : kW * g + c)) ^ w_swz) << 4));
-      ws[nt] = sw[(nt * 16 + an) * 4 + g];
+    for (int q = 0; q < kPieces; ++q) read_piece<RA, RW, AR>(q, la, am, a_chunk, lw, an, w_chunk, sa, sw, r, g);
+  }
+  static constexpr int kAPieces = MT * (kA + kCodes), kPieces = kAPieces + NT * (kW + 1);
+  template <int RA, int RW, int AR>
+  __device__ __forceinline__ void read_piece(int q, const unsigned char *la, int am, int a_chunk, const unsigned char *lw, int an, int w_chunk, const unsigned char *sa,
+                                             const unsigned char *sw, int r, int g) {
+    const int ar = AR < 16 ? r % AR : am;
+    if (q < kAPieces) {
+      const int mt = q / (kA + kCodes), c = q % (kA + kCodes);
+      if (c < kA) a[mt][c % kA] = *reinterpret_cast<const intx4 *>(la + (mt * 16 + ar) * RA + (((a_chunk + (ROWS == kRowsMx ? 4 * c + g : kA * g + c)) ^ swizzle<RA, kAX>(ar)) << 4));
+      else as[kCodes ? mt : 0] = sa[(mt * 16 + ar) * 4 + g];
+    } else {
+      const int nt = (q - kAPieces) / (kW + 1), c = (q - kAPieces) % (kW + 1);
+      if (c < kW) w[nt][c % kW] = *reinterpret_cast<const intx4 *>(lw + (nt * 16 + an) * RW + (((w_chunk + (ROWS == kRowsMx ? 4 * c + g : kW * g + c)) ^ swizzle<RW, kWX>(r)) << 4));
+      else ws[nt] = sw[(nt * 16 + an) * 4 + g];
     }
   }
 
-  // left: elements of a row of bf16 / float32 from the first of the 128 on; what lies behind them is another chunk's
-  __device__ __forceinline__ void multiply(floatx4 (&acc)[NT][MT], int left, int g) const {
+  // Matrix instructions of 128 k; multiply calls then(i) behind the i-th.  left: elements of a row of bf16 / float32 from the first of the 128 on;
+  // what lies behind them is another chunk's.
+  static constexpr int kInstrs = NT * MT * (ROWS == kRowsMx ? 1 : 4 * kPlanes);
+  template <typename F> __device__ __forceinline__ void multiply(floatx4 (&acc)[NT][MT], int left, int g, F then) const {
     if constexpr (ROWS == kRowsMx) {
-#ifdef __HIP_DEVICE_COMPILE__
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int mt = 0; mt < MT; ++mt) {
+#ifdef __HIP_DEVICE_COMPILE__
           acc[nt][mt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kW8 ? join(w[nt][0], w[nt][kW - 1]) : join(w[nt][0]), join(a[mt][0], a[mt][1]), acc[nt][mt], kW8 ? 0 : 4, 0,
                                                                          0, ws[nt], 0, as[kCodes ? mt : 0]);
 #endif
+          then(nt * MT + mt);
+        }
     } else {
-      // four instructions of 32 k: lane g has elements 32 g + 8 j .. + 7 of its 128 in the j-th, all of one block
+      // four steps of 32 k: lane g has elements 32 g + 8 j .. + 7 of its 128 in the j-th, all of one block
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         bf16x8 wf[NT];
@@ -226,7 +232,10 @@ template <int ROWS, int WF, int MT, int NT> struct Operands {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int q = kPlanes - 1; q >= 0; --q) acc[nt][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[nt], p[q], acc[nt][mt], 0, 0, 0);
+            for (int q = 0; q < kPlanes; ++q) {              // the least part first
+              acc[nt][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[nt], p[kPlanes - 1 - q], acc[nt][mt], 0, 0, 0);
+              then(((j * MT + mt) * NT + nt) * kPlanes + q);
+            }
         }
       }
     }
@@ -373,7 +382,7 @@ gemm_mx_kernel(MxGemm p, TileMap tm) {
     if (WK == 1 || st * WK + wk < nk) {
       Ops o;
       read(o, st);
-      o.multiply(acc, K - (st * WK + wk) * 128, g);
+      o.multiply(acc, K - (st * WK + wk) * 128, g, [](int) {});
     }
     if (!kDirect && st + 1 < ns) stash(st + 1);
   }
@@ -482,38 +491,80 @@ gemm_mx_waves_kernel(MxGemm p, TileMap tm) {
     const int f = (i < S::kAUnits ? i : i - S::kAUnits) * 64 + lane;
     s_src[i] = i < S::kAUnits ? p.a_scales + (int64_t)min(m0 + min(f, AR - 1), M - 1) * 4 : p.w_scales + w_row(min(f, BN - 1)) * 4;
   }
-  unsigned char *mine = lds + wave * (2 * S::kStage);
-  auto issue = [&](int kt, int slot) {
-    unsigned char *at = mine + slot * S::kStage;
-#pragma unroll
-    for (int i = 0; i < LA; ++i) {
-      const uint8_t *q = kCodes ? a_src[i] + (int64_t)kt * S::kARow : a_src[i] + min(a_at[i] + (uint32_t)kt * S::kARow, a_bytes - 16);       // behind a row its last chunk
-      __builtin_amdgcn_global_load_lds((gptr_t *)q, (lptr_t *)(at + i * 64 % kAChunks * 16), 16, 0, 0);
+  unsigned char *own = lds + wave * (2 * S::kStage);
+  auto issue = [&](int kt, int slot, int l) {                // l-th load of a stage
+    unsigned char *at = own + slot * S::kStage;
+    if (l < LA) {
+      const uint8_t *q = kCodes ? a_src[l % LA] + (int64_t)kt * S::kARow : a_src[l % LA] + min(a_at[l % LA] + (uint32_t)kt * S::kARow, a_bytes - 16);      // behind a row its last chunk
+      __builtin_amdgcn_global_load_lds((gptr_t *)q, (lptr_t *)(at + l * 64 % kAChunks * 16), 16, 0, 0);
+    } else if (l < LA + LW) {
+      __builtin_amdgcn_global_load_lds((gptr_t *)(w_src[(l - LA) % LW] + (int64_t)kt * S::kWRow), (lptr_t *)(at + S::kABytes + (l - LA) * 1024), 16, 0, 0);
+    } else {
+      const int i = l - LA - LW;
+      __builtin_amdgcn_global_load_lds((gptr_t *)(s_src[i % LS] + (int64_t)kt * (i < S::kAUnits ? M : w_rows) * 4), (lptr_t *)(at + S::kABytes + S::kWBytes + i * 256), 4, 0, 0);
     }
-#pragma unroll
-    for (int i = 0; i < LW; ++i) __builtin_amdgcn_global_load_lds((gptr_t *)(w_src[i] + (int64_t)kt * S::kWRow), (lptr_t *)(at + S::kABytes + i * 1024), 16, 0, 0);
-#pragma unroll
-    for (int i = 0; i < LS; ++i)
-      __builtin_amdgcn_global_load_lds((gptr_t *)(s_src[i] + (int64_t)kt * (i < S::kAUnits ? M : w_rows) * 4), (lptr_t *)(at + S::kABytes + S::kWBytes + i * 256), 4, 0, 0);
   };
   floatx4 acc[NT][MT];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) acc[nt][mt] = floatx4{0.f, 0.f, 0.f, 0.f};
-  if (wave < nk) issue(wave, 0);
-  if (wave + kWaves < nk) issue(wave + kWaves, 1);
-  int slot = 0;
-  for (int kt = wave; kt < nk; kt += kWaves, slot ^= 1) {
-    if (kt + kWaves < nk) wait_vmcnt<kLoads>(); else wait_vmcnt<0>();
+  const int mine = wave < nk ? (nk - wave + kWaves - 1) / kWaves : 0;       // stages of this wave: wave, wave + kWaves, ...
+  using Ops = Operands<ROWS, WF, MT, NT>;
+  Ops o[2];
+  auto piece = [&](Ops &to, int slot, int q) {
+    const unsigned char *at = own + slot * S::kStage;
+    to.template read_piece<S::kARow, S::kWRow, AR>(q, at, r, 0, at + S::kABytes, r, 0, at + S::kABytes + S::kWBytes, at + S::kABytes + S::kWBytes + S::kAUnits * 256, r, g);
+  };
+  if (mine > 0) {
+#pragma unroll
+    for (int l = 0; l < kLoads; ++l) issue(wave, 0, l);
+    if (mine > 1) {
+#pragma unroll
+      for (int l = 0; l < kLoads; ++l) issue(wave + kWaves, 1, l);
+      wait_vmcnt<kLoads>();
+    } else wait_vmcnt<0>();
     asm volatile("" ::: "memory");
-    Operands<ROWS, WF, MT, NT> o;
-    unsigned char *at = mine + slot * S::kStage;
-    o.template read<S::kARow, S::kWRow, AR>(at, r, 0, at + S::kABytes, r, 0, at + S::kABytes + S::kWBytes, at + S::kABytes + S::kWBytes + S::kAUnits * 256, r, g);
-    __builtin_amdgcn_s_waitcnt(0xc07f);                      // lgkmcnt(0): the slot is in registers
+#pragma unroll
+    for (int q = 0; q < Ops::kPieces; ++q) piece(o[0], 0, q);
+  }
+  // The n-th stage of the wave is multiplied from registers.  Behind its first instructions the stage after the next is asked for (its slot has
+  // been read), in the middle the next one has landed, and behind the last instructions it is read.  Kind 0: all of that, 1: no stage after
+  // the next, 2: the last stage.
+  auto step = [&](int n, auto kind, auto parity) {
+    constexpr int P = decltype(parity)::value, kKind = decltype(kind)::value, U = Ops::kInstrs, kHalf = (U + 1) / 2;
+    if (kKind == 0) __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0): the slot is in registers
     __builtin_amdgcn_sched_barrier(0);
-    if (kt + 2 * kWaves < nk) issue(kt + 2 * kWaves, slot);
-    o.multiply(acc, K - kt * 128, g);
+    auto landed = [&]() {
+      if (kKind == 0) wait_vmcnt<kLoads>(); else wait_vmcnt<0>();
+      asm volatile("" ::: "memory");
+    };
+    o[P].multiply(acc, K - (wave + n * kWaves) * 128, g, [&](int i) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (kKind == 0)
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l)
+          if (l * kHalf / kLoads == i) issue(wave + (n + 2) * kWaves, P, l);
+      if (kKind < 2 && i == kHalf - 1) landed();
+      if (kKind < 2)
+#pragma unroll
+        for (int q = 0; q < Ops::kPieces; ++q)
+          if (U > kHalf ? i == kHalf + q * (U - kHalf) / Ops::kPieces : i == U - 1) piece(o[P ^ 1], P ^ 1, q);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+  constexpr std::integral_constant<int, 0> k0{};
+  constexpr std::integral_constant<int, 1> k1{};
+  constexpr std::integral_constant<int, 2> k2{};
+  if (mine > 0) {
+    int n = 0;
+    for (; n + 3 < mine; n += 2) {
+      step(n, k0, k0);
+      step(n + 1, k0, k1);
+    }
+    if (mine - n == 3) { step(n, k0, k0); step(n + 1, k1, k1); step(n + 2, k2, k0); }
+    else if (mine - n == 2) { step(n, k1, k0); step(n + 1, k2, k1); }
+    else step(n, k2, k0);
   }
   // ---- results ----
   floatx4 *sums = reinterpret_cast<floatx4 *>(lds);          // [wave][tile][lane]
