@@ -613,17 +613,18 @@ pvf_status run_waves(hipStream_t s, const MxGemm &p) {
   return PVF_OK;
 }
 
-// ---- 128 x 128 results of decoded operands ------------------------------------------------------------------------------
-// A stage is four steps of 32 k of 16 matrix instructions a wave.  Between the instructions of a step the operands of the next are decoded (two
+// ---- results of decoded operands, a step ahead ------------------------------------------------------------------------------
+// 32 TM x 128 results, four waves of 16 TM x 64.  A stage is four steps of 32 k of 4 TM matrix instructions a wave.  Between the instructions of a step the operands of the next are decoded (two
 // conversions a matrix instruction) and the codes after those are read from LDS; in the middle of a stage the next one has landed, every wave
-// has read this one, one barrier, and its slot is loaded again.  Two workgroups a CU.
-template <int WF, int OUT>
+// has read this one, one barrier, and its slot is loaded again.  Two workgroups fit a CU's registers.
+template <int WF, int OUT, int TM, int kStages>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 gemm_mx_steps_kernel(MxGemm p, TileMap tm) {
   constexpr bool kSwiglu = OUT == kOutSwiglu, kW8 = WF == PVF_MX_E4M3;
-  constexpr int BM = 128, BN = 128, T = 4;                   // tiles of 16 rows and of 16 columns of a wave
-  using S = Shape<kRowsMxExact, WF, BM, BN, 2, 2, 1, 2>;
-  constexpr int LA = 4, LW = kW8 ? 4 : 2, kLoads = LA + LW + 1, CPR = S::kWRow / 16;
+  constexpr int BM = 32 * TM, BN = 128, T = 4;               // T: tiles of 16 columns of a wave, TM of 16 rows
+  using S = Shape<kRowsMxExact, WF, BM, BN, 2, 2, 1, kStages>;
+  static_assert(kStages % 2 == 0, "the loop takes stages in pairs");
+  constexpr int LA = TM, LW = kW8 ? 4 : 2, kLoads = LA + LW + 1, kUnits = BM / 64, CPR = S::kWRow / 16;
   extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1, r = lane & 15, g = lane >> 4;
   const int M = p.M, N = p.N, Kp = (p.K + kMxStage - 1) / kMxStage * kMxStage, nk = Kp / kMxStage;
@@ -649,11 +650,12 @@ gemm_mx_steps_kernel(MxGemm p, TileMap tm) {
     const int t = i * (256 / CPR) + tid / CPR, n = kSwiglu ? n0 + (t >> 6) * 32 + (t & 31) : n0 + t;
     w_off[i] = (uint32_t)(min(n, N - 1) - n_first) * w_bytes + ((tid % CPR) ^ swizzle<S::kWRow, S::kWX>(t)) * 16;
   }
-  const int s_t = (wave & 1) * 64 + lane;                    // waves 0 and 1 load the scale dwords of A, 2 and 3 those of W
+  // scale dwords, 64 a wave: those of A, then those of W (64 rows of A: the fourth wave repeats the third's)
+  const int unit = min(wave, kUnits + 1), s_t = (unit < kUnits ? unit : unit - kUnits) * 64 + lane;
   int64_t s_at = min(m0 + s_t, M - 1);
-  if (wave >= 2) s_at = !kSwiglu ? min(n0 + s_t, N - 1) : min(n0 + (s_t >> 6) * 32 + (s_t & 31), N - 1) + ((s_t & 32) ? (int64_t)N : 0);
-  const uint8_t *s_src = (wave < 2 ? p.a_scales : p.w_scales) + s_at * 4;
-  const int64_t s_step = (int64_t)(wave < 2 ? M : kSwiglu ? 2 * N : N) * 4;
+  if (unit >= kUnits) s_at = !kSwiglu ? min(n0 + s_t, N - 1) : min(n0 + (s_t >> 6) * 32 + (s_t & 31), N - 1) + ((s_t & 32) ? (int64_t)N : 0);
+  const uint8_t *s_src = (unit < kUnits ? p.a_scales : p.w_scales) + s_at * 4;
+  const int64_t s_step = (int64_t)(unit < kUnits ? M : kSwiglu ? 2 * N : N) * 4;
   auto issue = [&](int kt, int slot, int l) {
     unsigned char *at = lds + slot * S::kStage;
     if (l < LA) __builtin_amdgcn_global_load_lds((gptr_t *)(a_base + (int64_t)kt * 128 + a_off[l % LA]), (lptr_t *)(at + l * 4096 + wave * 1024), 16, 0, 0);
@@ -662,18 +664,18 @@ gemm_mx_steps_kernel(MxGemm p, TileMap tm) {
       const bool up = kSwiglu && (kW8 ? i & 1 : wave >> 1);
       __builtin_amdgcn_global_load_lds((gptr_t *)(w_base + (int64_t)kt * S::kWRow + (up ? (int64_t)N * w_bytes : 0) + w_off[i % LW]), (lptr_t *)(at + S::kABytes + i * 4096 + wave * 1024), 16, 0, 0);
     } else
-      __builtin_amdgcn_global_load_lds((gptr_t *)(s_src + kt * s_step), (lptr_t *)(at + S::kABytes + S::kWBytes + wave * 256), 4, 0, 0);
+      __builtin_amdgcn_global_load_lds((gptr_t *)(s_src + kt * s_step), (lptr_t *)(at + S::kABytes + S::kWBytes + unit * 256), 4, 0, 0);
   };
-  floatx4 acc[T][T];
+  floatx4 acc[T][TM];
 #pragma unroll
   for (int nt = 0; nt < T; ++nt)
 #pragma unroll
-    for (int mt = 0; mt < T; ++mt) acc[nt][mt] = floatx4{0.f, 0.f, 0.f, 0.f};
-  const int am = wm * 64 + r, an = wn * 64 + r;
+    for (int mt = 0; mt < TM; ++mt) acc[nt][mt] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const int am = wm * (16 * TM) + r, an = wn * 64 + r;
   // codes: chunk h of A (and of e4m3 W) in set h; e2m1 W, one chunk a stage, in set kt % 2.  Scales in set kt % 2.
-  intx4 ca[2][T], cw[2][T];
-  int as[2][T], ws[2][T];
-  bf16x8 da[2][T], dw[2][T];                                 // decoded operands of step j in set j % 2
+  intx4 ca[2][TM], cw[2][T];
+  int as[2][TM], ws[2][T];
+  bf16x8 da[2][TM], dw[2][T];                                 // decoded operands of step j in set j % 2
   auto read_a = [&](int slot, int h, int mt) {
     ca[h][mt] = *reinterpret_cast<const intx4 *>(lds + slot * S::kStage + (mt * 16 + am) * 128 + (((2 * g + h) ^ swizzle<128, 2>(r)) << 4));
   };
@@ -683,65 +685,80 @@ gemm_mx_steps_kernel(MxGemm p, TileMap tm) {
   };
   auto read_s = [&](int slot, int set, int q) {
     const unsigned char *at = lds + slot * S::kStage + S::kABytes + S::kWBytes + g;
-    if (q < T) as[set][q % T] = at[(q * 16 + am) * 4]; else ws[set][q % T] = at[BM * 4 + ((q - T) * 16 + an) * 4];
+    if (q < TM) as[set][q % TM] = at[(q * 16 + am) * 4]; else ws[set][(q - TM) % T] = at[BM * 4 + ((q - TM) * 16 + an) * 4];
   };
   auto decode = [&](int j, int set, int f) {                 // fragment f of step j of a stage whose scales are in `set`
     const int h = j >> 1, lo = j * 2 & 3;
     if (f < T) dw[j & 1][f % T] = kW8 ? decode_e4m3(cw[h][f % T][lo], cw[h][f % T][lo + 1], byte_scale(ws[set][f % T])) : decode_e2m1(cw[set][f % T][j], byte_scale(ws[set][f % T]));
-    else da[j & 1][f % T] = decode_e4m3(ca[h][f % T][lo], ca[h][f % T][lo + 1], byte_scale(as[set][f % T]));
+    else da[j & 1][(f - T) % TM] = decode_e4m3(ca[h][(f - T) % TM][lo], ca[h][(f - T) % TM][lo + 1], byte_scale(as[set][(f - T) % TM]));
   };
 #pragma unroll
-  for (int l = 0; l < kLoads; ++l) issue(0, 0, l);
-  if (nk > 1) {
+  for (int st = 0; st < kStages; ++st)
+    if (st < nk)
 #pragma unroll
-    for (int l = 0; l < kLoads; ++l) issue(1, 1, l);
-    wait_vmcnt<kLoads>();
-  } else wait_vmcnt<0>();
+      for (int l = 0; l < kLoads; ++l) issue(st, st, l);
+  if (kStages <= nk) wait_vmcnt<(kStages - 1) * kLoads>(); else wait_vmcnt<0>();
   __builtin_amdgcn_s_barrier();
 #pragma unroll
-  for (int q = 0; q < 2 * T; ++q) read_s(0, 0, q);
+  for (int q = 0; q < TM + T; ++q) read_s(0, 0, q);
 #pragma unroll
-  for (int q = 0; q < T; ++q) { read_w(0, 0, q); read_a(0, 0, q); }
+  for (int q = 0; q < T; ++q) read_w(0, 0, q);
 #pragma unroll
-  for (int f = 0; f < 2 * T; ++f) decode(0, 0, f);
-  // kind 0: two more stages follow, 1: one, 2: none
+  for (int q = 0; q < TM; ++q) read_a(0, 0, q);
+#pragma unroll
+  for (int f = 0; f < T + TM; ++f) decode(0, 0, f);
+  int slot = 0;                                              // of stage kt
+  // kind 0: kStages more stages follow, 1: at least one, 2: none
   auto stage = [&](int kt, auto kind, auto parity) {
-    constexpr int P = decltype(parity)::value, kKind = decltype(kind)::value;
+    constexpr int P = decltype(parity)::value, kKind = decltype(kind)::value, U = T * TM, kFrags = T + TM;
+    const int next = kStages == 2 ? P ^ 1 : slot + 1 == kStages ? 0 : slot + 1, here = kStages == 2 ? P : slot;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if (j == 2 && kKind < 2) {
-        wait_vmcnt<0>();                                     // my loads of the next stage have landed
+        if (kKind == 0) wait_vmcnt<(kStages - 2) * kLoads>(); else wait_vmcnt<0>();      // my loads of the next stage have landed
         __builtin_amdgcn_s_waitcnt(0xc07f);                  // lgkmcnt(0): my reads of this one are done
         __builtin_amdgcn_s_barrier();
       }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < T * T; ++i) {
-        const int nt = i / T, mt = i % T;
+      for (int i = 0; i < U; ++i) {
+        const int nt = i / TM, mt = i % TM;
         acc[nt][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(dw[j & 1][nt], da[j & 1][mt], acc[nt][mt], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
-        if (j == 0 && i < 2 * T) { if (i < T) read_a(P, 1, i % T); else if (kW8) read_w(P, 1, i % T); }
-        if (j == 2 && kKind < 2) {
-          if (i < 2 * T) read_s(P ^ 1, P ^ 1, i);
-          if (i % 2 == 0) { if (i / 2 < T) read_w(P ^ 1, kW8 ? 0 : P ^ 1, i / 2 % T); else read_a(P ^ 1, 0, i / 2 % T); }
-        }
-        if (kKind == 0 && j >= 2) {                          // loads of the stage after the next
+#pragma unroll
+        for (int q = 0; q < kFrags; ++q)
+          if (i == q * U / 2 / kFrags) {
+            if (j == 0) { if (q < TM) read_a(here, 1, q % TM); else if (kW8) read_w(here, 1, (q - TM) % T); }
+            if (j == 2 && kKind < 2) read_s(next, P ^ 1, q);
+            if (j == 2 && kKind < 2) { if (q < T) read_w(next, kW8 ? 0 : P ^ 1, q % T); else read_a(next, 0, (q - T) % TM); }
+          }
+        if (kKind == 0 && j >= 2) {                          // loads of the stage that takes this one's slot
 #pragma unroll
           for (int l = 0; l < kLoads; ++l)
-            if ((j - 2) * T * T + i == 2 + l * (2 * T * T - 4) / kLoads) issue(kt + 2, P, l);
+            if ((j - 2) * U + i == 1 + l * (2 * U - 2) / kLoads) issue(kt + kStages, here, l);
         }
-        if (i % 2 == 1 && (j < 3 || kKind < 2)) decode((j + 1) & 3, j < 3 ? P : P ^ 1, i / 2);
+        if (j < 3 || kKind < 2)
+#pragma unroll
+          for (int f = 0; f < kFrags; ++f)
+            if (i == (f + 1) * U / kFrags - 1) decode((j + 1) & 3, j < 3 ? P : P ^ 1, f);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
+    slot = next;
   };
   constexpr std::integral_constant<int, 0> k0{};
   constexpr std::integral_constant<int, 1> k1{};
   constexpr std::integral_constant<int, 2> k2{};
-  for (int kt = 0; kt + 2 < nk; kt += 2) {                   // nk is even
+  int kt = 0;                                                // nk is even
+  for (; kt + kStages + 1 < nk; kt += 2) {
     stage(kt, k0, k0);
     stage(kt + 1, k0, k1);
   }
+  if constexpr (kStages > 2)
+    for (; kt + 2 < nk; kt += 2) {
+      stage(kt, k1, k0);
+      stage(kt + 1, k1, k1);
+    }
   stage(nk - 2, k1, k0);
   stage(nk - 1, k2, k1);
 
@@ -749,23 +766,24 @@ gemm_mx_steps_kernel(MxGemm p, TileMap tm) {
     const int Np = (N + kMxStage - 1) / kMxStage * kMxStage, c0 = n0 + wn * 32;
     if (c0 >= Np) return;
 #pragma unroll
-    for (int mt = 0; mt < T; ++mt) store_act(acc[0][mt], acc[1][mt], acc[2][mt], acc[3][mt], m0 + am + mt * 16 < M, m0 + am + mt * 16, c0, g, p, Np);
+    for (int mt = 0; mt < TM; ++mt) store_act(acc[0][mt], acc[1][mt], acc[2][mt], acc[3][mt], m0 + am + mt * 16 < M, m0 + am + mt * 16, c0, g, p, Np);
   } else {
 #pragma unroll
-    for (int mt = 0; mt < T; ++mt)
+    for (int mt = 0; mt < TM; ++mt)
 #pragma unroll
       for (int nt = 0; nt < T; ++nt)
         if (m0 + am + mt * 16 < M) store_row4<float>(acc[nt][mt], m0 + am + mt * 16, n0 + wn * 64 + nt * 16 + 4 * g, p);
   }
 }
 
-template <int WF, int OUT> pvf_status run_steps(hipStream_t s, const MxGemm &p) {
-  using S = Shape<kRowsMxExact, WF, 128, 128, 2, 2, 1, 2>;
+template <int WF, int OUT, int TM, int kStages> pvf_status run_steps(hipStream_t s, const MxGemm &p) {
+  using S = Shape<kRowsMxExact, WF, 32 * TM, 128, 2, 2, 1, kStages>;
+  static_assert(S::kLds <= 160 * 1024, "LDS");
   TileMap tm;
-  const int64_t tiles_n = OUT == kOutSwiglu ? mx_width(p.N) / 64 : (p.N + 127) / 128, tiles_m = (p.M + 127) / 128;
+  const int64_t tiles_n = OUT == kOutSwiglu ? mx_width(p.N) / 64 : (p.N + 127) / 128, tiles_m = (p.M + 32 * TM - 1) / (32 * TM);
   PVF_REQUIRE(nullptr, tiles_m * tiles_n < 1 << 28, PVF_ESHAPE, "%d x %d results are too many for a launch", p.M, p.N);
   tm.tiles_m = (int)tiles_m; tm.tiles_n = (int)tiles_n; tm.group_m = (int)std::min<int64_t>(tiles_m, 8);
-  auto kernel = gemm_mx_steps_kernel<WF, OUT>;
+  auto kernel = gemm_mx_steps_kernel<WF, OUT, TM, kStages>;
   static const hipError_t allowed = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
   PVF_HIP_CHECK(nullptr, allowed);
   kernel<<<(uint32_t)((tiles_m * tiles_n + 7) / 8 * 8), 256, S::kLds, s>>>(p, tm);
@@ -999,31 +1017,32 @@ template <int WF, bool kDirect> struct Candidates<kRowsMx, WF, kOutBf16, kDirect
   static constexpr int ROWS = kRowsMx, OUT = kOutBf16;
   static constexpr Candidate list[] = {
       PVF_MX_WAVES(16, 16, 4, 16, .079f, .073f),          PVF_MX_WAVES(32, 32, 4, 32, .115f, .095f),          PVF_MX_WAVES(64, 32, 4, 64, .17f, .186f),
-      PVF_MX_WAVES(64, 64, 4, 64, .24f, .253f),           PVF_MX_TILE(64, 64, 2, 2, 2, 2, 64, .38f, .217f),   PVF_MX_WAVES(80, 64, 4, 80, .26f, .34f),
+      PVF_MX_WAVES(48, 64, 4, 48, .177f, .17f),           PVF_MX_WAVES(64, 64, 4, 64, .24f, .253f),           PVF_MX_TILE(64, 64, 2, 2, 2, 2, 64, .38f, .217f),   PVF_MX_WAVES(80, 64, 4, 80, .26f, .34f),
       PVF_MX_TILE(96, 64, 2, 2, 1, 3, 96, .39f, .28f),    PVF_MX_TILE(64, 128, 2, 4, 1, 3, 64, .415f, .375f), PVF_MX_TILE(128, 128, 2, 2, 1, 2, 128, .78f, .51f),
       PVF_MX_TILE(160, 128, 2, 4, 1, 2, 160, .83f, .72f), PVF_MX_TILE(192, 256, 2, 4, 1, 2, 192, 1.49f, 1.44f), {256, 256, 0, 1.6f, 1.54f, run_quad<WF>, true, 256}};
 };
 template <int WF, bool kDirect> struct Candidates<kRowsMxExact, WF, kOutF32, kDirect> {
   static constexpr int ROWS = kRowsMxExact, OUT = kOutF32;
   static constexpr Candidate list[] = {
-      PVF_MX_WAVES(16, 16, 8, 16, .09f, .10f),           PVF_MX_WAVES(32, 32, 4, 32, .135f, .124f),          PVF_MX_WAVES(64, 64, 4, 64, .33f, .35f),
-      PVF_MX_WAVES(80, 64, 4, 80, .455f, .45f),          PVF_MX_TILE(64, 128, 2, 4, 1, 3, 64, .74f, .61f),   PVF_MX_TILE(128, 128, 2, 2, 1, 2, 128, 1.2f, .91f), {128, 128, 0, 1.1f, .84f, run_steps<WF, OUT>, true},
+      PVF_MX_WAVES(16, 16, 8, 16, .09f, .10f),           PVF_MX_WAVES(32, 32, 4, 32, .135f, .12f),           PVF_MX_WAVES(48, 64, 4, 48, .275f, .27f),
+      PVF_MX_WAVES(64, 64, 4, 64, .325f, .35f),          PVF_MX_WAVES(80, 64, 4, 80, .425f, .45f),          PVF_MX_TILE(64, 128, 2, 4, 1, 3, 64, .74f, .61f),   PVF_MX_TILE(128, 128, 2, 2, 1, 2, 128, 1.2f, .91f), {128, 128, 0, 1.1f, .84f, run_steps<WF, OUT, 4, 2>, true},
       PVF_MX_TILE(160, 128, 2, 4, 1, 2, 160, 1.43f, 1.22f)};
 };
 template <int WF, bool kDirect> struct Candidates<kRowsMxExact, WF, kOutSwiglu, kDirect> {
   static constexpr int ROWS = kRowsMxExact, OUT = kOutSwiglu;
   static constexpr Candidate list[] = {
-      PVF_MX_TILE(16, 64, 1, 1, 4, 2, 16, .18f, .14f),   PVF_MX_TILE(32, 64, 1, 1, 4, 2, 32, .25f, .20f),    PVF_MX_TILE(64, 128, 2, 2, 2, 2, 64, .53f, .65f),
-      PVF_MX_TILE(64, 128, 2, 2, 1, 2, 64, .67f, .55f),  PVF_MX_TILE(128, 128, 2, 2, 1, 2, 128, 1.2f, .90f), {128, 64, 0, 1.1f, .81f, run_steps<WF, OUT>, true}};
+      PVF_MX_TILE(16, 64, 1, 1, 4, 2, 16, .18f, .14f),   PVF_MX_TILE(32, 64, 1, 1, 4, 2, 32, .25f, .20f),    PVF_MX_TILE(64, 128, 2, 2, 1, 2, 64, .67f, .57f),
+      {64, 64, 0, .53f, .65f, run_steps<WF, OUT, 2, 4>, true}, PVF_MX_TILE(128, 128, 2, 2, 1, 2, 128, 1.2f, .90f), {128, 64, 0, 1.1f, .81f, run_steps<WF, OUT, 4, 2>, true}};
 };
 // rows that go through registers have the instances of one kernel only
 template <> struct Candidates<kRowsBf16, PVF_MX_E2M1, kOutBf16, true> {
   static constexpr int ROWS = kRowsBf16, WF = PVF_MX_E2M1, OUT = kOutBf16;
   static constexpr bool kDirect = true;
   static constexpr Candidate list[] = {
-      PVF_MX_TILE(16, 16, 1, 1, 8, 2, 1, .04f, .047f),   PVF_MX_WAVES(16, 16, 4, 4, .045f, .044f),           PVF_MX_WAVES(16, 16, 8, 16, .073f, .10f),
-      PVF_MX_TILE(16, 16, 1, 1, 4, 2, 16, .095f, .058f), PVF_MX_WAVES(32, 32, 4, 32, .15f, .168f),           PVF_MX_TILE(32, 64, 2, 1, 2, 2, 32, .35f, .215f),
-      PVF_MX_TILE(64, 64, 2, 2, 2, 2, 64, .41f, .42f),   PVF_MX_WAVES(80, 64, 3, 80, .54f, .52f),            PVF_MX_TILE(64, 128, 2, 2, 1, 2, 64, .75f, .58f)};
+      PVF_MX_TILE(16, 16, 1, 1, 8, 2, 1, .04f, .047f),   PVF_MX_WAVES(16, 16, 4, 4, .045f, .044f),           PVF_MX_WAVES(16, 16, 8, 16, .06f, .10f),
+      PVF_MX_TILE(16, 16, 1, 1, 4, 2, 16, .095f, .058f), PVF_MX_WAVES(16, 64, 8, 16, .154f, .153f),          PVF_MX_WAVES(32, 32, 4, 32, .135f, .154f),
+      PVF_MX_TILE(32, 64, 2, 1, 2, 2, 32, .35f, .205f),  PVF_MX_WAVES(48, 64, 4, 48, .27f, .27f),            PVF_MX_WAVES(32, 128, 4, 32, .327f, .33f),
+      PVF_MX_WAVES(80, 64, 3, 80, .49f, .47f),           PVF_MX_TILE(64, 128, 2, 2, 1, 2, 64, .75f, .58f)};
 };
 template <> struct Candidates<kRowsBf16, PVF_MX_E2M1, kOutBf16, false> {
   static constexpr int ROWS = kRowsBf16, WF = PVF_MX_E2M1, OUT = kOutBf16;
@@ -1036,8 +1055,8 @@ template <> struct Candidates<kRowsF32, PVF_MX_E2M1, kOutF32, true> {
   static constexpr int ROWS = kRowsF32, WF = PVF_MX_E2M1, OUT = kOutF32;
   static constexpr bool kDirect = true;
   static constexpr Candidate list[] = {
-      PVF_MX_TILE(16, 16, 1, 1, 8, 2, 1, .07f, .10f),    PVF_MX_TILE(16, 16, 1, 1, 8, 2, 16, .27f, .30f),    PVF_MX_WAVES(16, 64, 4, 16, .41f, .41f),
-      PVF_MX_TILE(64, 128, 4, 1, 1, 2, 64, 2.1f, 2.1f)};
+      PVF_MX_TILE(16, 16, 1, 1, 8, 2, 1, .07f, .10f),    PVF_MX_TILE(16, 16, 1, 1, 8, 2, 16, .27f, .30f),    PVF_MX_WAVES(16, 64, 4, 16, .39f, .39f),
+      PVF_MX_WAVES(16, 128, 4, 16, .53f, .54f),          PVF_MX_TILE(64, 128, 4, 1, 1, 2, 64, 2.1f, 2.1f)};
 };
 template <> struct Candidates<kRowsF32, PVF_MX_E2M1, kOutF32, false> {
   static constexpr int ROWS = kRowsF32, WF = PVF_MX_E2M1, OUT = kOutF32;

@@ -217,7 +217,8 @@ def test_products_of_whole_numbers(M, N, K, fmt, dtype, residual):
 
 
 LARGE = [(64, 4096, 300), (64, 12288, 256), (320, 4100, 385), (320, 12288, 256), (256, 24576, 128), (640, 4096, 300), (500, 12300, 200), (1280, 4096, 256), (1300, 4000, 130),
-         (2560, 4096, 256), (2500, 4011, 100), (2560, 12288, 384), (2049, 9000, 513)]
+         (2560, 4096, 256), (2500, 4011, 100), (2560, 12288, 384), (2049, 9000, 513), (320, 4096, 512), (192, 4096, 1100), (256, 4096, 640), (2560, 12288, 512), (2049, 9000, 200),
+         (2300, 12289, 250), (1024, 24576, 128)]
 
 
 @pytest.mark.parametrize("M,N,K", LARGE)
@@ -358,7 +359,7 @@ def within_codes(got, want_values, slack):
 
 
 @pytest.mark.parametrize("M,ff,K", [(1, 1, 32), (1, 32, 128), (3, 17, 33), (16, 200, 300), (17, 129, 1411), (64, 256, 4096), (65, 130, 640), (130, 500, 260), (257, 384, 512),
-                                    (320, 1024, 1024), (515, 257, 384), (64, 4100, 256), (1, 12288, 256), (320, 12288, 128), (1100, 3000, 264)])
+                                    (320, 1024, 1024), (515, 257, 384), (64, 4100, 256), (1, 12288, 256), (320, 12288, 128), (1100, 3000, 264), (64, 12288, 1024), (50, 12300, 140), (300, 12288, 384), (2560, 2100, 700)])
 @pytest.mark.parametrize("fmt", [R.E4M3, R.E2M1])
 def test_swiglu(M, ff, K, fmt):
     """The slack of a product is that of test_products_of_random_rows without a rounding to bf16; silu(g) u moves by at most 1.1 |u| dg + |silu(g)| du
