@@ -314,8 +314,8 @@ pvf_status pvf_rmsnorm(void *stream, int32_t dtype, const void *x, const void *g
  * Scales are the smallest powers of two, from 2^-127 on, that bring a block's largest magnitude to 448 (6) at most, so nothing
  * saturates; elements are rounded to the nearest code, ties to even.  A block that holds a NaN or an infinity has scale byte 255, which
  * stands for NaN, and zero codes: every result that reads it is NaN.
- * codes, scales and rows of bf16 / float32 may begin at any element but for this: codes at multiples of 16 bytes, scales of 4.  Sizes are at most
- * 2^28, K at most 2^24.  The calls use no workspace: those on different streams may overlap, and all may be captured into a graph. */
+ * codes, scales and rows of bf16 / float32 may begin at any element but for this: codes at multiples of 16 bytes, scales of 4.  Rows (M, N) are
+ * at most 2^28, elements of a row (K, ff) at most 2^22.  Elements below 2^-126 may count as zero in a product.  The calls use no workspace: those on different streams may overlap, and all may be captured into a graph. */
 enum { PVF_MX_E4M3 = 0, PVF_MX_E2M1 = 1 };
 
 /* codes, scales = x [M, K] (dtype PVF_F32 / PVF_BF16) in format fmt. */
@@ -327,7 +327,7 @@ pvf_status pvf_add_rmsnorm_mx(void *stream, int32_t dtype, const void *x, const 
                               void *codes, void *scales, int32_t M, int32_t d, float eps);
 
 /* C[M,N] = A[M,K] * W[N,K]^T (+ residual[M,N]); A in PVF_MX_E4M3, W in w_fmt, C and residual in dtype.  residual may be NULL and may
- * alias C.  Sums are kept in float32, but for PVF_BF16 results (and pvf_gemm_mx_swiglu) the scaled matrix instruction first adds groups of 8
+ * alias C.  Sums are kept in float32, but for PVF_BF16 results the scaled matrix instruction first adds groups of 8
  * neighbouring k, whose products it cuts off 13 bits below the group's largest (1.5e-5 of a result on random operands). */
 pvf_status pvf_gemm_mx(void *stream, int32_t w_fmt, int32_t dtype, const void *A, const void *a_scales, const void *W,
                        const void *w_scales, void *C, const void *residual, int32_t M, int32_t N, int32_t K);

@@ -278,8 +278,8 @@ gemm_mx_kernel(MxGemm p, TileMap tm) {
 
   // the 32 workgroups that an XCD runs at a time cover a patch of tiles and share operands through its L2
   const int total = tm.tiles_m * tm.tiles_n, per_xcd = (total + 7) >> 3;
-  const int L = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= per_xcd || L >= total) return;
+  const int block = mx_block(), L = (block & 7) * per_xcd + (block >> 3);
+  if (block >> 3 >= per_xcd || L >= total) return;
   const int band = L / (tm.group_m * tm.tiles_n), within = L - band * (tm.group_m * tm.tiles_n);
   const int band_rows = min(tm.group_m, tm.tiles_m - band * tm.group_m);
   const int tile_n = within / band_rows, tile_m = band * tm.group_m + (within - tile_n * band_rows);
@@ -439,7 +439,7 @@ pvf_status run_as(hipStream_t s, const MxGemm &p) {
   // once per kernel instance; a function-local static is initialised exactly once even with concurrent callers
   static const hipError_t allowed = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
   PVF_HIP_CHECK(nullptr, allowed);
-  kernel<<<(uint32_t)((tiles_m * tiles_n + 7) / 8 * 8), S::kThreads, S::kLds, s>>>(p, tm);
+  kernel<<<mx_grid((tiles_m * tiles_n + 7) / 8 * 8), S::kThreads, S::kLds, s>>>(p, tm);
   PVF_LAUNCH_CHECK(nullptr, "gemm_mx");
   return PVF_OK;
 }
@@ -461,8 +461,8 @@ gemm_mx_waves_kernel(MxGemm p, TileMap tm) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   const int M = p.M, N = p.N, K = p.K, Kp = (K + kMxStage - 1) / kMxStage * kMxStage, nk = Kp / kMxStage;
   const int total = tm.tiles_m * tm.tiles_n, per_xcd = (total + 7) >> 3;
-  const int L = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= per_xcd || L >= total) return;
+  const int block = mx_block(), L = (block & 7) * per_xcd + (block >> 3);
+  if (block >> 3 >= per_xcd || L >= total) return;
   const int band = L / (tm.group_m * tm.tiles_n), within = L - band * (tm.group_m * tm.tiles_n);
   const int band_rows = min(tm.group_m, tm.tiles_m - band * tm.group_m);
   const int tile_n = within / band_rows, tile_m = band * tm.group_m + (within - tile_n * band_rows);
@@ -608,7 +608,7 @@ pvf_status run_waves(hipStream_t s, const MxGemm &p) {
   auto kernel = gemm_mx_waves_kernel<ROWS, WF, OUT, BM, BN, kWaves, AR>;
   static const hipError_t allowed = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
   PVF_HIP_CHECK(nullptr, allowed);
-  kernel<<<(uint32_t)((tiles_m * tiles_n + 7) / 8 * 8), 64 * kWaves, kLds, s>>>(p, tm);
+  kernel<<<mx_grid((tiles_m * tiles_n + 7) / 8 * 8), 64 * kWaves, kLds, s>>>(p, tm);
   PVF_LAUNCH_CHECK(nullptr, "gemm_mx");
   return PVF_OK;
 }
@@ -629,8 +629,8 @@ gemm_mx_steps_kernel(MxGemm p, TileMap tm) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1, r = lane & 15, g = lane >> 4;
   const int M = p.M, N = p.N, Kp = (p.K + kMxStage - 1) / kMxStage * kMxStage, nk = Kp / kMxStage;
   const int total = tm.tiles_m * tm.tiles_n, per_xcd = (total + 7) >> 3;
-  const int L = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= per_xcd || L >= total) return;
+  const int block = mx_block(), L = (block & 7) * per_xcd + (block >> 3);
+  if (block >> 3 >= per_xcd || L >= total) return;
   const int band = L / (tm.group_m * tm.tiles_n), within = L - band * (tm.group_m * tm.tiles_n);
   const int band_rows = min(tm.group_m, tm.tiles_m - band * tm.group_m);
   const int tile_n = within / band_rows, tile_m = band * tm.group_m + (within - tile_n * band_rows);
@@ -786,7 +786,7 @@ template <int WF, int OUT, int TM, int kStages> pvf_status run_steps(hipStream_t
   auto kernel = gemm_mx_steps_kernel<WF, OUT, TM, kStages>;
   static const hipError_t allowed = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
   PVF_HIP_CHECK(nullptr, allowed);
-  kernel<<<(uint32_t)((tiles_m * tiles_n + 7) / 8 * 8), 256, S::kLds, s>>>(p, tm);
+  kernel<<<mx_grid((tiles_m * tiles_n + 7) / 8 * 8), 256, S::kLds, s>>>(p, tm);
   PVF_LAUNCH_CHECK(nullptr, "gemm_mx");
   return PVF_OK;
 }
@@ -814,8 +814,8 @@ gemm_mx_quad_kernel(MxGemm p, TileMap tm) {
   const int wm = wave >> 2, wn = wave & 3, r = lane & 15, g = lane >> 4;
   const int M = p.M, N = p.N, Kp = (p.K + kMxStage - 1) / kMxStage * kMxStage, nk = Kp / kMxStage;
   const int total = tm.tiles_m * tm.tiles_n, per_xcd = (total + 7) >> 3;
-  const int L = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= per_xcd || L >= total) return;
+  const int block = mx_block(), L = (block & 7) * per_xcd + (block >> 3);
+  if (block >> 3 >= per_xcd || L >= total) return;
   const int band = L / (tm.group_m * tm.tiles_n), within = L - band * (tm.group_m * tm.tiles_n);
   const int band_rows = min(tm.group_m, tm.tiles_m - band * tm.group_m);
   const int tile_n = within / band_rows, tile_m = band * tm.group_m + (within - tile_n * band_rows);
@@ -988,7 +988,7 @@ template <int WF> pvf_status run_quad(hipStream_t s, const MxGemm &p) {
   auto kernel = gemm_mx_quad_kernel<WF>;
   static const hipError_t allowed = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
   PVF_HIP_CHECK(nullptr, allowed);
-  kernel<<<(uint32_t)((tiles_m * tiles_n + 7) / 8 * 8), 512, kLds, s>>>(p, tm);
+  kernel<<<mx_grid((tiles_m * tiles_n + 7) / 8 * 8), 512, kLds, s>>>(p, tm);
   PVF_LAUNCH_CHECK(nullptr, "gemm_mx");
   return PVF_OK;
 }

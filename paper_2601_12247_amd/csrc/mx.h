@@ -30,6 +30,14 @@ struct MxGemm {
 pvf_status launch_gemm_mx(hipStream_t s, const MxGemm &g);
 
 #ifdef __HIPCC__
+// A launch takes fewer than 2^32 threads along x: workgroups from the 2^22th on go on in y.
+constexpr int kMxGridBits = 22;
+inline dim3 mx_grid(int64_t n) {
+  const int64_t x = n < 1 << kMxGridBits ? n : 1 << kMxGridBits;
+  return dim3((uint32_t)x, (uint32_t)((n + x - 1) / x), 1);
+}
+__device__ __forceinline__ int mx_block() { return (int)(blockIdx.x + (blockIdx.y << kMxGridBits)); }
+
 // Byte of a block's scale from the bits of its largest magnitude: the smallest power of two, from 2^-127 on, with amax <= top * 2^e
 // (top = 448 = 1.75 2^8 or 6 = 1.5 2^2: the carry out of the mantissa decides), so that no element saturates.  NaN and infinities: 255.
 template <int FMT> __device__ __forceinline__ int mx_scale_byte(uint32_t amax_bits) {

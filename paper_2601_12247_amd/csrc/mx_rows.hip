@@ -12,8 +12,8 @@ namespace {
 template <typename T, int FMT, int kRows>
 __global__ void __launch_bounds__(256)
 quant_mx_kernel(const T *__restrict__ x, uint8_t *__restrict__ codes, uint32_t *__restrict__ scales, int M, int K, int Kp) {
-  const int strips = (Kp + 511) / 512, lane = threadIdx.x & 63, k = blockIdx.x % strips * 512 + lane * 8;
-  const int m0 = (blockIdx.x / strips * 4 + (threadIdx.x >> 6)) * kRows;
+  const int strips = (Kp + 511) / 512, lane = threadIdx.x & 63, block = mx_block(), k = block % strips * 512 + lane * 8;
+  const int m0 = (block / strips * 4 + (threadIdx.x >> 6)) * kRows;
   float v[kRows][8];
 #pragma unroll
   for (int r = 0; r < kRows; ++r) load8(x + (int64_t)min(m0 + r, M - 1) * K + min(k, K), K - k, v[r]);
@@ -36,7 +36,8 @@ add_rmsnorm_mx_kernel(const T *x, const T *residual, const T *__restrict__ gain,
   __shared__ double part[4];
   __shared__ float row_inv;
   const int tid = threadIdx.x;
-  const int64_t m = blockIdx.x;
+  const int64_t m = mx_block();
+  if (m >= M) return;
   const T *xr = x + m * d, *rr = residual ? residual + m * d : nullptr;
   float h[kHeld][8];
   double ss = 0;
@@ -96,8 +97,8 @@ pvf_status launch_quant_mx(hipStream_t s, int dtype, const void *x, int fmt, voi
     constexpr int F = decltype(f)::value;
     constexpr int kRows = 4;
     const int64_t grid = (int64_t)((Kp + 511) / 512) * ((M + 4 * kRows - 1) / (4 * kRows));
-    PVF_REQUIRE(nullptr, grid <= INT32_MAX, PVF_ESHAPE, "quant_mx: %d x %d elements are too many for a launch", M, K);
-    quant_mx_kernel<T, F, kRows><<<(uint32_t)grid, 256, 0, s>>>((const T *)x, (uint8_t *)codes, (uint32_t *)scales, M, K, Kp);
+    PVF_REQUIRE(nullptr, grid < 1 << 28, PVF_ESHAPE, "quant_mx: %d x %d elements are too many for a launch", M, K);
+    quant_mx_kernel<T, F, kRows><<<mx_grid(grid), 256, 0, s>>>((const T *)x, (uint8_t *)codes, (uint32_t *)scales, M, K, Kp);
     PVF_LAUNCH_CHECK(nullptr, "quant_mx");
     return PVF_OK;
   };
@@ -114,7 +115,7 @@ pvf_status launch_add_rmsnorm_mx(hipStream_t s, int dtype, const void *x, const 
   auto run = [&](auto t) {
     using T = decltype(t);
     auto go = [&](auto v) {
-      add_rmsnorm_mx_kernel<T, decltype(v)::value><<<M, 256, 0, s>>>((const T *)x, (const T *)residual, (const T *)gain, (T *)sum,
+      add_rmsnorm_mx_kernel<T, decltype(v)::value><<<mx_grid(M), 256, 0, s>>>((const T *)x, (const T *)residual, (const T *)gain, (T *)sum,
                                                                      (uint8_t *)codes, (uint32_t *)scales, M, d, dp, eps);
     };
     if (dp <= 2048) go(std::integral_constant<int, 1>{});

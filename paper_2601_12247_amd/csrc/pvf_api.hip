@@ -1055,7 +1055,7 @@ static pvf_status check_mx(const char *call, const void *codes, const void *scal
 }
 static pvf_status check_mx_sizes(const char *call, int32_t M, int32_t N, int32_t K) {
   PVF_REQUIRE(nullptr, M >= 0 && N >= 0 && K > 0, PVF_EINVAL, "%s: bad size (%d, %d, %d)", call, M, N, K);
-  PVF_REQUIRE(nullptr, M <= 1 << 28 && N <= 1 << 28 && K <= 1 << 24, PVF_ESHAPE, "%s: size (%d, %d, %d) beyond 2^28 rows or 2^24 elements", call, M, N, K);
+  PVF_REQUIRE(nullptr, M <= 1 << 28 && N <= 1 << 28 && K <= 1 << 22, PVF_ESHAPE, "%s: size (%d, %d, %d) beyond 2^28 rows or 2^22 elements", call, M, N, K);
   return PVF_OK;
 }
 static bool at_element(int dtype, const void *p) { return (uintptr_t)p % (dtype == PVF_F32 ? 4 : 2) == 0; }
@@ -1101,7 +1101,7 @@ extern "C" pvf_status pvf_gemm_mx_swiglu(void *stream, int32_t w_fmt, const void
                                          void *act, void *act_scales, int32_t M, int32_t ff, int32_t K) {
   PVF_REQUIRE(nullptr, w_fmt == PVF_MX_E4M3 || w_fmt == PVF_MX_E2M1, PVF_EINVAL, "pvf_gemm_mx_swiglu: w_fmt=%d", w_fmt);
   if (const pvf_status st = check_mx_sizes("pvf_gemm_mx_swiglu", M, ff, K)) return st;
-  PVF_REQUIRE(nullptr, ff <= 1 << 24, PVF_ESHAPE, "pvf_gemm_mx_swiglu: ff=%d beyond 2^24", ff);
+  PVF_REQUIRE(nullptr, ff <= 1 << 22, PVF_ESHAPE, "pvf_gemm_mx_swiglu: ff=%d beyond 2^22", ff);
   if (M == 0 || ff == 0) return PVF_OK;
   if (const pvf_status st = check_mx("pvf_gemm_mx_swiglu (A)", A, a_scales)) return st;
   if (const pvf_status st = check_mx("pvf_gemm_mx_swiglu (W)", W, w_scales)) return st;

@@ -166,6 +166,30 @@ def test_norm_of_rows_that_are_zero_or_not_finite():
     assert torch.isnan(v[1]).all() and torch.isfinite(v[0]).all()
 
 
+def test_norm_of_more_rows_than_a_launch_has_along_x():
+    """2^24 rows are 2^32 threads.  The last rows are those of a call of their own, and nothing lies behind them."""
+    M, d = (1 << 24) + 5, 32
+    x = torch.zeros(M, d, dtype=torch.bfloat16, device="cuda")
+    x[-300:] = rows(300, d, "bf16", 5).cuda()
+    gain = torch.ones(d, dtype=torch.bfloat16, device="cuda")
+    out, untouched = guarded_mx(M, d)
+    B.add_rmsnorm_mx(x, gain, 1e-5, out=out)
+    _, codes, scales = B.add_rmsnorm_mx(x[-300:], gain, 1e-5)
+    assert torch.equal(out[0][-300:].view(torch.uint8), codes.view(torch.uint8)) and torch.equal(out[1][:, -300:].view(torch.uint8), scales.view(torch.uint8))
+    assert not bool(out[0][:-300].view(torch.uint8).any()) and untouched()
+
+
+def test_quantiser_of_more_rows_than_a_launch_has_along_x():
+    M = 1 << 28
+    x = torch.zeros(M, 1, dtype=torch.bfloat16, device="cuda")
+    x[-300:] = rows(300, 1, "bf16", 6).cuda()
+    out, untouched = guarded_mx(M, 1, R.E2M1)
+    B.quant_mx(x, R.E2M1, out=out)
+    codes, scales = B.quant_mx(x[-300:], R.E2M1)
+    assert torch.equal(out[0][-300:], codes) and torch.equal(out[1][:, -300:].view(torch.uint8), scales.view(torch.uint8))
+    assert untouched()
+
+
 # ---------------------------------------------------------------- products
 def whole(M, K, fmt, seed):
     """Codes of whole numbers up to 4 and scales of 2^-1 .. 2^1, and their values."""
@@ -287,6 +311,17 @@ def test_4_bit_products_of_random_rows(M, N, K, dtype):
         assert (got - want).norm() <= 1e-6 * want.norm()
 
 
+def test_4_bit_products_of_more_tiles_than_a_launch_has_along_x():
+    """Tiles of 16 rows and 512 threads: 2^27 rows are 2^32 threads."""
+    M = (1 << 27) + 3
+    x = (torch.arange(M, device="cuda", dtype=torch.int32) % 1021).float()[:, None]
+    w, w_b = torch.zeros(1, 128, dtype=torch.int64), torch.full((1, 4), 127)
+    w[0, 0] = 5                                              # 3.0
+    out, untouched = guarded((M, 1), torch.float32, 0xa5)
+    B.gemm_w4(x, *R.pack(w, w_b, R.E2M1), out=out)
+    assert torch.equal(out, x * 3) and untouched()
+
+
 @pytest.mark.parametrize("call", ["mx_e4m3", "mx_e2m1", "mx_f32", "w4_bf16", "w4_f32"])
 def test_scales_over_their_whole_range(call):
     """Every scale byte from 0 to 254 stands for its power of two, 255 for NaN.  Rows with 2^(127 - b) against weights with 2^(b - 127), so that
@@ -324,6 +359,40 @@ def test_4_bit_products_of_rows_that_are_not_finite(dtype):
     got = B.gemm_w4(x.cuda(), *R.pack(w, w_b, R.E2M1)).cpu()
     assert (got[0] == 300).all() and (got[3] == 300).all()
     assert (got[1] == float("inf")).all() and torch.isnan(got[2]).all()
+
+
+@pytest.mark.parametrize("call,M,N", [("mx_e4m3", 4096, 4096), ("mx_e4m3", 70, 300), ("mx_e2m1", 1, 4096), ("mx_f32", 4096, 4096), ("mx_f32", 33, 500), ("w4_bf16", 1, 300),
+                                      ("w4_f32", 1, 300), ("w4_f32", 40, 4096)])
+def test_products_of_the_longest_rows(call, M, N):
+    """2^22 elements a row, all zero but 2000 whole numbers, the last element among them: offsets within a tile of 256 rows reach 2^30 bytes."""
+    K, g = 1 << 22, torch.Generator().manual_seed(M + N)
+    fmt = R.E4M3 if call in ("mx_e4m3", "mx_f32") else R.E2M1
+    at = torch.cat([torch.randperm(K // 2 - 1, generator=g)[:1999] * 2 + torch.randint(0, 2, (1999,), generator=g), torch.tensor([K - 1])]).unique().cuda()
+    a = torch.randint(-4, 5, (M, len(at)), generator=g).float().cuda()
+    w = torch.randint(-4, 5, (N, len(at)), generator=g).float().cuda()
+    want = (a.double() @ w.double().t().contiguous()).float()
+    ones = lambda rows: torch.full((K // 128, rows, 4), 127, dtype=torch.uint8, device="cuda").view(torch.float8_e8m0fnu)
+
+    def e4m3(v):
+        codes = torch.zeros(v.shape[0], K, dtype=torch.uint8, device="cuda")
+        codes[:, at] = v.to(torch.float8_e4m3fn).view(torch.uint8)
+        return codes.view(torch.float8_e4m3fn), ones(v.shape[0])
+
+    if fmt == R.E4M3:
+        W = e4m3(w)
+    else:                                                    # no two of the 2000 share a byte
+        codes = torch.zeros(N, K // 2, dtype=torch.uint8, device="cuda")
+        four = torch.tensor([0, 2, 4, 5, 6], dtype=torch.uint8, device="cuda")[w.abs().long()] + (w < 0).to(torch.uint8) * 8
+        codes[:, at // 2] = four << (at % 2 * 4).to(torch.uint8)
+        W = codes, ones(N)
+    dtype = torch.float32 if call.endswith("f32") else torch.bfloat16
+    if call.startswith("w4"):
+        x = torch.zeros(M, K, dtype=dtype, device="cuda")
+        x[:, at] = a.to(dtype)
+        got = B.gemm_w4(x, *W)
+    else:
+        got = B.gemm_mx(*e4m3(a), *W, dtype=dtype)
+    assert torch.equal(got, want.to(dtype))
 
 
 def test_product_into_its_residual():

@@ -117,6 +117,16 @@ def test_products_refuse():
     assert f(None, 0, None, None, None, None, None, 0, 1, 32) == 0
 
 
+def test_rows_of_more_than_2_22_elements_are_refused():
+    n = (1 << 22) + 1
+    refused(B.lib().pvf_quant_mx(None, 0, P, 0, P, P, 1, n), "ESHAPE", "2^22")
+    refused(B.lib().pvf_add_rmsnorm_mx(None, 0, P, P, P, P, P, P, 1, n, 1e-5), "ESHAPE", "2^22")
+    refused(B.lib().pvf_gemm_mx(None, 0, 0, P, P, P, P, P, None, 1, 1, n), "ESHAPE", "2^22")
+    refused(B.lib().pvf_gemm_mx_swiglu(None, 0, P, P, P, P, P, P, 1, n, 32), "ESHAPE", "2^22")
+    refused(B.lib().pvf_gemm_mx_swiglu(None, 0, P, P, P, P, P, P, 1, 32, n), "ESHAPE", "2^22")
+    refused(B.lib().pvf_gemm_w4(None, 0, P, P, P, P, None, 1, 1, n), "ESHAPE", "2^22")
+
+
 def test_binding_refuses():
     """What the binding can tell from shapes and types alone, on CPU tensors."""
     x = torch.zeros(4, 200)
