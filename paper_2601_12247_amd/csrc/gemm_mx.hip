@@ -62,19 +62,35 @@ __device__ __forceinline__ bf16x8 decode_e2m1(int w, float scale) {
 // The conversions take the exponent bits of a float32 as their scale, which are the scale byte: 0 is 2^-127, 255 NaN.
 __device__ __forceinline__ float byte_scale(int b) { return __uint_as_float((uint32_t)b << 23); }
 
-// x = p[0] + p[1] + p[2] exactly, 8 bits of the mantissa each, cut off and not rounded so that nothing overflows; what is not finite is
-// in p[0] alone.
+// x = p[0] + p[1] + p[2] exactly, 8 bits of the mantissa each, cut off and not rounded so that nothing overflows.  What is not finite has to
+// be in p[0] alone: a NaN makes NaN of the other parts, which is as good, an infinity is looked for in all eight at once (taking it out element by
+// element was half of the instructions).
 __device__ __forceinline__ void split3(const float *x, bf16x8 *p) {
+  uint32_t hi[8], mid[8], lo[8];
+  float top = fabsf(x[0]);
+#pragma unroll
+  for (int e = 1; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const uint32_t u = __float_as_uint(x[e]);
-    const bool fine = (u & 0x7f800000u) != 0x7f800000u;
-    const float r = fine ? x[e] - __uint_as_float(u & 0xffff0000u) : 0.f;
-    const float b = __uint_as_float(__float_as_uint(r) & 0xffff0000u);
-    p[0][e] = fine ? __builtin_bit_cast(bf16_t, (uint16_t)(u >> 16)) : (bf16_t)x[e];
-    p[1][e] = __builtin_bit_cast(bf16_t, (uint16_t)(__float_as_uint(r) >> 16));
-    p[2][e] = (bf16_t)(r - b);
+    hi[e] = __float_as_uint(x[e]);
+    const float r = x[e] - __uint_as_float(hi[e] & 0xffff0000u);
+    mid[e] = __float_as_uint(r);
+    lo[e] = __float_as_uint(r - __uint_as_float(mid[e] & 0xffff0000u));
   }
+  if (top == __builtin_inff()) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (fabsf(x[e]) == __builtin_inff()) mid[e] = lo[e] = 0;
+  }
+  intx4 w[3];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {                              // the upper halves of two words
+    w[0][e] = (int)__builtin_amdgcn_perm(hi[2 * e + 1], hi[2 * e], 0x07060302u);
+    w[1][e] = (int)__builtin_amdgcn_perm(mid[2 * e + 1], mid[2 * e], 0x07060302u);
+    w[2][e] = (int)__builtin_amdgcn_perm(lo[2 * e + 1], lo[2 * e], 0x07060302u);
+  }
+#pragma unroll
+  for (int q = 0; q < 3; ++q) p[q] = __builtin_bit_cast(bf16x8, w[q]);
 }
 
 // ---- results ------------------------------------------------------------------------------------------------------
