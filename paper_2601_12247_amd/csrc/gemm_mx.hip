@@ -1071,15 +1071,17 @@ template <> struct Candidates<kRowsF32, PVF_MX_E2M1, kOutF32, true> {
   static constexpr int ROWS = kRowsF32, WF = PVF_MX_E2M1, OUT = kOutF32;
   static constexpr bool kDirect = true;
   static constexpr Candidate list[] = {
-      PVF_MX_TILE(16, 16, 1, 1, 8, 2, 1, .07f, .10f),    PVF_MX_TILE(16, 16, 1, 1, 8, 2, 16, .27f, .30f),    PVF_MX_WAVES(16, 64, 4, 16, .39f, .39f),
-      PVF_MX_WAVES(16, 128, 4, 16, .53f, .54f),          PVF_MX_TILE(64, 128, 4, 1, 1, 2, 64, 2.1f, 2.1f)};
+      PVF_MX_TILE(16, 16, 1, 1, 8, 2, 1, .16f, .14f),    PVF_MX_TILE(16, 64, 1, 1, 8, 2, 1, .25f, .24f),     PVF_MX_TILE(16, 16, 1, 1, 8, 2, 16, .18f, .225f),
+      PVF_MX_WAVES(16, 64, 8, 4, .265f, .295f),          PVF_MX_WAVES(16, 64, 4, 16, .36f, .375f),           PVF_MX_WAVES(16, 128, 4, 16, .53f, .54f),
+      PVF_MX_TILE(64, 128, 4, 1, 1, 2, 64, 1.92f, 1.98f)};
 };
 template <> struct Candidates<kRowsF32, PVF_MX_E2M1, kOutF32, false> {
   static constexpr int ROWS = kRowsF32, WF = PVF_MX_E2M1, OUT = kOutF32;
   static constexpr bool kDirect = false;
   static constexpr Candidate list[] = {
-      PVF_MX_TILE(16, 16, 1, 1, 8, 2, 1, .07f, .10f),    PVF_MX_TILE(16, 16, 1, 1, 8, 2, 16, .27f, .30f),    PVF_MX_TILE(16, 64, 1, 1, 4, 2, 16, .45f, .45f),
-      PVF_MX_TILE(32, 32, 2, 1, 4, 2, 32, .59f, .70f),   PVF_MX_TILE(32, 64, 2, 1, 2, 2, 32, .82f, .84f),    PVF_MX_TILE(64, 128, 4, 1, 1, 2, 64, 2.1f, 2.1f)};
+      PVF_MX_TILE(16, 16, 1, 1, 8, 2, 1, .20f, .16f),    PVF_MX_TILE(16, 64, 1, 1, 8, 2, 1, .32f, .33f),     PVF_MX_TILE(16, 64, 1, 1, 8, 2, 4, .36f, .36f),
+      PVF_MX_TILE(16, 16, 1, 1, 8, 2, 16, .37f, .38f),   PVF_MX_TILE(16, 64, 1, 1, 4, 2, 16, .57f, .60f),    PVF_MX_TILE(32, 32, 2, 1, 4, 2, 32, .62f, .70f),
+      PVF_MX_TILE(32, 64, 2, 1, 2, 2, 32, 1.0f, 1.1f),   PVF_MX_TILE(64, 128, 4, 1, 1, 2, 64, 2.9f, 2.5f),   PVF_MX_TILE(32, 128, 2, 1, 2, 2, 32, 1.45f, 1.45f)};
 };
 
 template <int ROWS, int WF, int OUT, bool kDirect = true> pvf_status run(hipStream_t s, const MxGemm &p) {

@@ -275,7 +275,8 @@ def test_products_of_random_rows(M, N, K, fmt, dtype):
 
 @pytest.mark.parametrize("M,N,K", [(1, 1, 33), (1, 64, 128), (1, 12288, 4096), (2, 17, 31), (16, 48, 300), (17, 33, 1411), (33, 100, 129), (64, 257, 4096), (65, 130, 640),
                                    (130, 300, 264), (320, 1024, 2048), (511, 769, 520), (1024, 384, 1000), (4, 4096, 512), (3, 300, 1024), (16, 12288, 256), (33, 4001, 1411),
-                                   (64, 4096, 256), (64, 12288, 520), (320, 4096, 512), (330, 12300, 264)])
+                                   (64, 4096, 256), (64, 12288, 520), (320, 4096, 512), (330, 12300, 264),
+                                   (1, 12289, 1030), (4, 12288, 1024), (4, 12289, 1031), (2560, 4096, 200), (330, 12289, 515)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("residual,shift", [(False, 0), (True, 0), (False, 1)])
 def test_4_bit_products_of_whole_numbers(M, N, K, dtype, residual, shift):
