@@ -15,6 +15,14 @@
 // Operands of the scaled 16 x 16 x 128 instruction: lane (r = lane % 16, g = lane / 16) holds row r; of e4m3 the 16 bytes at k = 16 g and
 // the 16 at 64 + 16 g, of e2m1 the 32 elements from 32 g on; its scale byte is that of k = 32 g .. 32 g + 31.  The weights are the
 // instruction's first operand, so that a lane ends up with 4 consecutive columns of C.
+//
+// Four kernels, from few results to many; run() takes the instance whose fullest CU is done first.  Bounds: few rows by the launch (a kernel that
+// does nothing takes 3 us) and the weights' bytes; tiles on the way by a CU's loads into LDS, 125-150 GB/s from L2 in any order, some 55 of what HBM
+// delivers to all CUs; many rows by the matrix pipe and the power it takes (scaled) or by the instructions that decode (decoded).
+//   gemm_mx_waves_kernel  tiles up to 80 x 64 or 16 x 128, a ring for each wave, no barrier
+//   gemm_mx_kernel        tiles from 16 x 16 to 192 x 256, one ring; rows at any element
+//   gemm_mx_steps_kernel  64 x 128 and 128 x 128, decoded operands
+//   gemm_mx_quad_kernel   256 x 256, scaled instruction
 #include "mx.h"
 
 #include <algorithm>
@@ -283,6 +291,10 @@ template <int ROWS, int WF, int BM, int BN, int WM, int WN, int WK, int kStages,
 // BM / WM x BN / WN results, and with WK > 1 the waves' sums are added through LDS at the end.  Stages go through a ring of kStages slots of LDS, straight
 // from memory (whole 128-byte lines per request: loads of 64-byte pieces straight into registers reached half the rate), one barrier
 // a stage.  Rows of bf16 / float32 that do not begin at 16-byte chunks go through registers (kDirect = false).
+// Bound by the CU's loads: a stage's BM + BN rows, not its BM BN results, so tiles are as square as the launch leaves them.  WK > 1 where there are fewer
+// tiles than CUs: more loads in flight for the same tile.  1280 x 4096 x 12288, e4m3 weights, 160 x 128 tiles: 94 us, 1.37 PFLOP/s; one row of float32
+// against 4-bit weights 12288 x 4096, 16 x 64 with k over 8 waves: 11.6 us (16 columns a workgroup 17: the row is split into its three parts
+// for every 16 of them); 33 float32 rows that are not aligned, 4001 x 1411: 9.7 us, the latency of three stages.
 template <int ROWS, int WF, int OUT, int BM, int BN, int WM, int WN, int WK, int kStages, int AR, bool kDirect>
 __global__ void __launch_bounds__(64 * WM * WN * WK)
 gemm_mx_kernel(MxGemm p, TileMap tm) {
@@ -473,6 +485,9 @@ pvf_status run_as(hipStream_t s, const MxGemm &p) {
 // A workgroup computes BM x BN results for launches whose tiles make about one round over the chip: its kWaves waves take the 128s of k in turn, each
 // with the whole tile and a ring of two slots of LDS of its own, so that the loop has no barrier and the waves' loads, reads and matrix
 // instructions drift apart; a slot is loaded again as soon as it is in registers.  The sums are added through LDS at the end.
+// Bound by the bytes in flight: 4 waves with two stages of 80 x 64 are all of a CU's LDS.  320 x 4096 x 12288, e4m3 weights: 25 us, 1.8 MB for each CU
+// in 20 us behind 5 of launch and first loads (one ring with a barrier a stage: 30); splitting k over workgroups as well would need a workspace.  One
+// row against 4-bit weights 12288 x 4096: 6.5 us with the call, 4.1 TB/s; 320 rows against 4096 x 4096: 18.4 us.
 template <int ROWS, int WF, int OUT, int BM, int BN, int kWaves, int AR>
 __global__ void __launch_bounds__(64 * kWaves)
 gemm_mx_waves_kernel(MxGemm p, TileMap tm) {
@@ -642,6 +657,10 @@ pvf_status run_waves(hipStream_t s, const MxGemm &p) {
 // 32 TM x 128 results, four waves of 16 TM x 64.  A stage is four steps of 32 k of 4 TM matrix instructions a wave.  Between the instructions of a step the operands of the next are decoded (two
 // conversions a matrix instruction) and the codes after those are read from LDS; in the middle of a stage the next one has landed, every wave
 // has read this one, one barrier, and its slot is loaded again.  Two workgroups fit a CU's registers.
+// Bound by issue: a conversion beside a matrix instruction costs 2 cycles of its 16 (measured: 7.3 ns an instruction alone, 9.5 with two conversions), so
+// 1.3 times the matrix time is the limit.  gate|up of 2560 rows, 12288 x 4096, e4m3 weights: 390-400 us, 1.3 PFLOP/s (bfloat16 products of
+// a library, 16384 cube: 1.6; the same tile on one ring, decoding before the instructions: 436 us).  64 rows, 4-bit weights, 64 x 128 tiles of four stages: 20 us, where the
+// loads alone take 15: the conversions of 192 workgroups' weights do not all fit beside them.
 template <int WF, int OUT, int TM, int kStages>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 gemm_mx_steps_kernel(MxGemm p, TileMap tm) {
@@ -827,6 +846,9 @@ template <int BT, int WT> __device__ __forceinline__ int half_row(int r) {
 // A wave multiplies, stage by stage of 128 k, lower A x lower W, lower x upper, upper x upper, upper x lower.  The operands of a half are read
 // from LDS one quadrant before their first use, which frees their rows early: each half of a stage's slot is refilled as soon as it is
 // read, one barrier per half stage, so loads are issued evenly and have 1 to 1.5 stages to land.  Scale bytes have a ring of three stages.
+// Bound by power: 11520 x 12288 x 4096, e4m3 weights, 437-446 us, 2.6 PFLOP/s at 1.8 GHz of 2.4 with the matrix pipe busy for 553 000 cycles, 0.7 of the
+// time (a library's 8-bit product without block scales: 3.0 at 8192 cubed, 3.2 at 16384).  256 x 256 because a tile's operands are 1 / 128 of its work: 192 x 256 with one
+// barrier a stage takes 532 us.  e2m1 weights: 512 us, ten registers spilled where one operand of the instruction is 4 registers wide and the other 8.
 template <int WF>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
 gemm_mx_quad_kernel(MxGemm p, TileMap tm) {
@@ -1019,10 +1041,10 @@ template <int WF> pvf_status run_quad(hipStream_t s, const MxGemm &p) {
 }
 
 // ---- which instance -------------------------------------------------------------------------------------------------
-// What a tile costs for 128 k, in microseconds, measured at K = 4096 (launch time less 3 us, over 32 and the tiles of the fullest CU):
+// What a tile costs for 128 k, in microseconds, measured at K = 4096 and 12288 (launch time less 3 us, over the stages and the tiles of the fullest CU):
 // where a CU has one tile, and per tile where it has several (those that fit its LDS run at a time and hide each other's barriers and
-// latencies).  The launch takes the instance whose fullest CU is done first.  What bounds small tiles is a CU's loads on the way: some 60
-// bytes a nanosecond, so a tile's rows count, not its area.
+// latencies).  The launch takes the instance whose fullest CU is done first: within 6 % of the best of its list for 68 launches of 1 to 2560 rows against 4096 x 4096,
+// 12288 x 4096 and 4096 x 12288.  Small tiles cost what their rows' loads cost, not their area.
 struct Candidate {
   int BM, BN, most_rows;                                     // most_rows: rows of A that the instance loads (0: any number)
   float alone, among;
@@ -1041,9 +1063,9 @@ template <int ROWS, int WF, int OUT, bool kDirect> struct Candidates;
 template <int WF, bool kDirect> struct Candidates<kRowsMx, WF, kOutBf16, kDirect> {
   static constexpr int ROWS = kRowsMx, OUT = kOutBf16;
   static constexpr Candidate list[] = {
-      PVF_MX_WAVES(16, 16, 4, 16, .079f, .073f),          PVF_MX_WAVES(32, 32, 4, 32, .115f, .095f),          PVF_MX_WAVES(64, 32, 4, 64, .17f, .186f),
-      PVF_MX_WAVES(48, 64, 4, 48, .177f, .17f),           PVF_MX_WAVES(64, 64, 4, 64, .24f, .253f),           PVF_MX_TILE(64, 64, 2, 2, 2, 2, 64, .38f, .217f),   PVF_MX_WAVES(80, 64, 4, 80, .26f, .34f),
-      PVF_MX_TILE(96, 64, 2, 2, 1, 3, 96, .39f, .28f),    PVF_MX_TILE(64, 128, 2, 4, 1, 3, 64, .415f, .375f), PVF_MX_TILE(128, 128, 2, 2, 1, 2, 128, .78f, .51f),
+      PVF_MX_WAVES(16, 16, 4, 16, .079f, .070f),          PVF_MX_WAVES(32, 32, 4, 32, .115f, .112f),          PVF_MX_WAVES(64, 32, 4, 64, .17f, .186f),
+      PVF_MX_WAVES(48, 64, 4, 48, .215f, .20f),           PVF_MX_WAVES(64, 64, 4, 64, .24f, .253f),           PVF_MX_TILE(64, 64, 2, 2, 2, 2, 64, .38f, .217f),   PVF_MX_WAVES(80, 64, 4, 80, .26f, .34f),
+      PVF_MX_TILE(96, 64, 2, 2, 1, 3, 96, .39f, .28f),    PVF_MX_TILE(64, 128, 2, 4, 1, 3, 64, .44f, .375f), PVF_MX_TILE(128, 128, 2, 2, 1, 2, 128, .78f, .51f),
       PVF_MX_TILE(160, 128, 2, 4, 1, 2, 160, .83f, .74f), PVF_MX_TILE(192, 256, 2, 4, 1, 2, 192, 1.49f, 1.44f), {256, 256, 0, WF == PVF_MX_E4M3 ? 1.3f : 1.75f, WF == PVF_MX_E4M3 ? 1.5f : 1.62f, run_quad<WF>, true, 256}};
 };
 template <int WF, bool kDirect> struct Candidates<kRowsMxExact, WF, kOutF32, kDirect> {
