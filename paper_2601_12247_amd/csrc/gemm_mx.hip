@@ -26,6 +26,7 @@
 #include "mx.h"
 
 #include <algorithm>
+#include <atomic>
 
 namespace pvf {
 namespace {
@@ -464,6 +465,17 @@ gemm_mx_kernel(MxGemm p, TileMap tm) {
   }
 }
 
+// Lets a kernel have so much LDS on the current device: asked for once a device (bits of `done`), by concurrent first callers perhaps twice.
+pvf_status allow_lds(const void *kernel, int bytes, std::atomic<uint64_t> &done) {
+  int device = 0;
+  PVF_HIP_CHECK(nullptr, hipGetDevice(&device));
+  const uint64_t bit = 1ull << (device & 63);
+  if (done.load(std::memory_order_relaxed) & bit) return PVF_OK;
+  PVF_HIP_CHECK(nullptr, hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  done.fetch_or(bit, std::memory_order_relaxed);
+  return PVF_OK;
+}
+
 template <int ROWS, int WF, int OUT, int BM, int BN, int WM, int WN, int WK, int kStages, int AR = BM, bool kDirect = true>
 pvf_status run_as(hipStream_t s, const MxGemm &p) {
   using S = Shape<ROWS, WF, BM, BN, WM, WN, WK, kStages, AR>;
@@ -473,9 +485,8 @@ pvf_status run_as(hipStream_t s, const MxGemm &p) {
   PVF_REQUIRE(nullptr, tiles_m * tiles_n < 1 << 28, PVF_ESHAPE, "%d x %d results are too many for a launch", p.M, p.N);
   tm.tiles_m = (int)tiles_m; tm.tiles_n = (int)tiles_n; tm.group_m = (int)std::min<int64_t>(tiles_m, 8);
   auto kernel = gemm_mx_kernel<ROWS, WF, OUT, BM, BN, WM, WN, WK, kStages, AR, kDirect>;
-  // once per kernel instance; a function-local static is initialised exactly once even with concurrent callers
-  static const hipError_t allowed = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
-  PVF_HIP_CHECK(nullptr, allowed);
+  static std::atomic<uint64_t> allowed{0};
+  if (const pvf_status st = allow_lds((const void *)kernel, S::kLds, allowed)) return st;
   kernel<<<mx_grid((tiles_m * tiles_n + 7) / 8 * 8), S::kThreads, S::kLds, s>>>(p, tm);
   PVF_LAUNCH_CHECK(nullptr, "gemm_mx");
   return PVF_OK;
@@ -646,8 +657,8 @@ pvf_status run_waves(hipStream_t s, const MxGemm &p) {
   PVF_REQUIRE(nullptr, tiles_m * tiles_n < 1 << 28, PVF_ESHAPE, "%d x %d results are too many for a launch", p.M, p.N);
   tm.tiles_m = (int)tiles_m; tm.tiles_n = (int)tiles_n; tm.group_m = (int)std::min<int64_t>(tiles_m, 8);
   auto kernel = gemm_mx_waves_kernel<ROWS, WF, OUT, BM, BN, kWaves, AR>;
-  static const hipError_t allowed = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-  PVF_HIP_CHECK(nullptr, allowed);
+  static std::atomic<uint64_t> allowed{0};
+  if (const pvf_status st = allow_lds((const void *)kernel, kLds, allowed)) return st;
   kernel<<<mx_grid((tiles_m * tiles_n + 7) / 8 * 8), 64 * kWaves, kLds, s>>>(p, tm);
   PVF_LAUNCH_CHECK(nullptr, "gemm_mx");
   return PVF_OK;
@@ -828,8 +839,8 @@ template <int WF, int OUT, int TM, int kStages> pvf_status run_steps(hipStream_t
   PVF_REQUIRE(nullptr, tiles_m * tiles_n < 1 << 28, PVF_ESHAPE, "%d x %d results are too many for a launch", p.M, p.N);
   tm.tiles_m = (int)tiles_m; tm.tiles_n = (int)tiles_n; tm.group_m = (int)std::min<int64_t>(tiles_m, 8);
   auto kernel = gemm_mx_steps_kernel<WF, OUT, TM, kStages>;
-  static const hipError_t allowed = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds);
-  PVF_HIP_CHECK(nullptr, allowed);
+  static std::atomic<uint64_t> allowed{0};
+  if (const pvf_status st = allow_lds((const void *)kernel, S::kLds, allowed)) return st;
   kernel<<<mx_grid((tiles_m * tiles_n + 7) / 8 * 8), 256, S::kLds, s>>>(p, tm);
   PVF_LAUNCH_CHECK(nullptr, "gemm_mx");
   return PVF_OK;
@@ -1033,8 +1044,8 @@ template <int WF> pvf_status run_quad(hipStream_t s, const MxGemm &p) {
   PVF_REQUIRE(nullptr, tiles_m * tiles_n < 1 << 28, PVF_ESHAPE, "%d x %d results are too many for a launch", p.M, p.N);
   tm.tiles_m = (int)tiles_m; tm.tiles_n = (int)tiles_n; tm.group_m = (int)std::min<int64_t>(tiles_m, 6);   // 8: 2 % slower at 8192 x 8192, nothing at 11520 x 12288
   auto kernel = gemm_mx_quad_kernel<WF>;
-  static const hipError_t allowed = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-  PVF_HIP_CHECK(nullptr, allowed);
+  static std::atomic<uint64_t> allowed{0};
+  if (const pvf_status st = allow_lds((const void *)kernel, kLds, allowed)) return st;
   kernel<<<mx_grid((tiles_m * tiles_n + 7) / 8 * 8), 512, kLds, s>>>(p, tm);
   PVF_LAUNCH_CHECK(nullptr, "gemm_mx");
   return PVF_OK;

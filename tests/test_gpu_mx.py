@@ -396,6 +396,30 @@ def test_products_of_the_longest_rows(call, M, N):
     assert torch.equal(got, want.to(dtype))
 
 
+@pytest.mark.parametrize("M,N,K", [(5, 33, 128), (70, 200, 256), (300, 4096, 512), (2560, 4096, 256), (2560, 12288, 256)])
+@pytest.mark.parametrize("fmt,dtype", [(R.E4M3, "bf16"), (R.E2M1, "bf16"), (R.E4M3, "f32")])
+def test_results_and_residuals_may_begin_at_any_element(M, N, K, fmt, dtype):
+    a, a_b, av = whole(M, K, R.E4M3, M + K)
+    w, w_b, wv = whole(N, K, fmt, N + K + 1)
+    res = torch.randint(-50, 51, (M, N), generator=torch.Generator().manual_seed(3)).to(DT[dtype])
+    want = (cuda64(av, wv) + res.double()).float().to(DT[dtype])
+    for c, r in ((1, 3), (3, 0), (4, 1)):
+        buf = torch.full((M * N + 16,), 77.0, dtype=DT[dtype], device="cuda")
+        out = buf[c:c + M * N].view(M, N)
+        B.gemm_mx(*R.pack(a, a_b, R.E4M3), *R.pack(w, w_b, fmt), residual=shifted(res, r), out=out)
+        assert torch.equal(out.cpu(), want)
+        assert bool((buf[:c] == 77).all() and (buf[c + M * N:] == 77).all())
+
+
+def test_norm_of_rows_that_begin_at_any_element():
+    """x, residual, gain and sum each at another element."""
+    x, r, gain = rows(37, 515, "bf16", 1), rows(37, 515, "bf16", 2), rows(1, 515, "bf16", 3)[0]
+    h, codes, scales = B.add_rmsnorm_mx(x.cuda(), gain.cuda(), 1e-5, residual=r.cuda())
+    out = shifted(torch.zeros_like(x), 5)
+    _, c, s = B.add_rmsnorm_mx(shifted(x, 1), shifted(gain, 3), 1e-5, residual=shifted(r, 2), sum_out=out)
+    assert torch.equal(out, h) and torch.equal(c.view(torch.uint8), codes.view(torch.uint8)) and torch.equal(s.view(torch.uint8), scales.view(torch.uint8))
+
+
 def test_product_into_its_residual():
     a, a_b, av = whole(70, 512, R.E4M3, 1)
     w, w_b, wv = whole(200, 512, R.E2M1, 2)
