@@ -44,13 +44,21 @@ constexpr bool codes_in(int rows) { return rows == kRowsMx || rows == kRowsMxExa
 
 // silu(g) within 2^-22: each rounding here moves codes of an 8-bit result that lie between two.  exp(-g) = 2^p with what p lost put back, its
 // sum with one with what that lost, and a Newton step behind the reciprocal.  Past |g| = 80 the plain form: there a
-// power may be 0 or infinite.  12288 x 4096 weights in 4 bits, 64 rows: 1 of 900000 codes differs from the definition in 64 bits, 1 of 120000 with the plain form; no time.
+// power may be 0 or infinite (to -256: far_act).  12288 x 4096 weights in 4 bits, 64 rows: 1 of 900000 codes differs from the definition in 64 bits, 1 of 120000 with the plain form; no time.
+constexpr float kLog2e = 0x1.715476p+0f, kLog2eRest = 0x1.4ae0cp-26f, kLn2 = 0x1.62e43p-1f;
 __device__ __forceinline__ float silu_f(float g) {
-  constexpr float kLog2e = 0x1.715476p+0f, kRest = 0x1.4ae0cp-26f, kLn2 = 0x1.62e43p-1f;
-  const float p = -g * kLog2e, e = __builtin_amdgcn_exp2f(p), ec = fmaf(e, kLn2 * fmaf(-g, kRest, fmaf(-g, kLog2e, -p)), e);
+  const float p = -g * kLog2e, e = __builtin_amdgcn_exp2f(p), ec = fmaf(e, kLn2 * fmaf(-g, kLog2eRest, fmaf(-g, kLog2e, -p)), e);
   const float d = 1.0f + ec, b = d - 1.0f, lost = (1.0f - (d - b)) + (ec - b), r = __builtin_amdgcn_rcpf(d);
   const float near = fmaf(fmaf(-d, r, 1.0f) - lost * r, r, r);
   return g * (fabsf(g) < 80.f ? near : __builtin_amdgcn_rcpf(1.0f + e));
+}
+
+// silu(g) u for g of -256 to -80, where 1 + exp(-g) is exp(-g) in any type here: g exp(g) u with the power of two put on last.  silu(g) by itself is below
+// float32's normal range from -92 on and its divisor above float32 from -89 on, while the product may be any code: a block's scale goes down to 2^-127.  (u 2^-64: what
+// that loses is below 2^-168 in the product.)  Below -256 the product is less than 2^-230: zero.
+__device__ __forceinline__ float far_act(float g, float u) {
+  const float q = g * kLog2e, n = rintf(q), e = __builtin_amdgcn_exp2f(q - n), ec = fmaf(e, kLn2 * fmaf(g, kLog2eRest, fmaf(g, kLog2e, -q)), e);
+  return __builtin_ldexpf(g * ec * (u * 0x1p-64f), (int)n + 64);
 }
 
 // The four registers of 32 e2m1 codes; the instruction does not read the others.
@@ -149,13 +157,25 @@ template <typename T> __device__ __forceinline__ void store_row4(floatx4 v, int 
 
 // silu(gate) * up of 32 columns from c0 on, of which the lane has 4 g .. + 3 and 16 + 4 g .. + 3: a block, as codes and scale.  All 64 lanes.
 __device__ __forceinline__ void store_act(floatx4 g0, floatx4 g1, floatx4 u0, floatx4 u1, bool live, int m, int c0, int g, const MxGemm &p, int Np) {
-  float v[8];
-  uint32_t am = 0;
+  float v[8], lowest = 0.f;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    v[e] = c0 + 4 * g + e < p.N ? silu_f(g0[e]) * u0[e] : 0.f;
-    v[4 + e] = c0 + 16 + 4 * g + e < p.N ? silu_f(g1[e]) * u1[e] : 0.f;
-    am = max(am, max(abs_bits(v[e]), abs_bits(v[4 + e])));
+    v[e] = silu_f(g0[e]) * u0[e];
+    v[4 + e] = silu_f(g1[e]) * u1[e];
+    lowest = fminf(lowest, fminf(g0[e], g1[e]));
+  }
+  if (__any(lowest <= -80.f)) {                              // hardly ever, so its instructions are jumped over (2560 x 12288 x 4096: 397 us with it, 396 without)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float gate = e < 4 ? g0[e & 3] : g1[e & 3], up = e < 4 ? u0[e & 3] : u1[e & 3];
+      if (gate <= -80.f && gate >= -256.f) v[e] = far_act(gate, up);
+    }
+  }
+  uint32_t am = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if (c0 + (e & 4) * 4 + 4 * g + (e & 3) >= p.N) v[e] = 0.f;
+    am = max(am, abs_bits(v[e]));
   }
   am = max(am, (uint32_t)__shfl_xor((int)am, 16, kWave));
   am = max(am, (uint32_t)__shfl_xor((int)am, 32, kWave));
