@@ -342,6 +342,13 @@ pvf_status pvf_gemm_mx_swiglu(void *stream, int32_t w_fmt, const void *A, const 
 pvf_status pvf_gemm_w4(void *stream, int32_t dtype, const void *x, const void *W, const void *w_scales, void *C,
                        const void *residual, int32_t M, int32_t N, int32_t K);
 
+/* Which kernel instance one of these products takes: *index of the *count that its launches choose from, by sizes, types and alignment alone (nothing is
+ * launched and no GPU is needed), so that a check can tell whether it runs them all.  call: PVF_MX_CALL_GEMM, PVF_MX_CALL_SWIGLU (N = ff; dtype is not
+ * read) or PVF_MX_CALL_W4 (w_fmt is not read); aligned: whether x of PVF_MX_CALL_W4 begins at a multiple of 16 bytes. */
+enum { PVF_MX_CALL_GEMM = 0, PVF_MX_CALL_SWIGLU = 1, PVF_MX_CALL_W4 = 2 };
+pvf_status pvf_gemm_mx_instance(int32_t call, int32_t w_fmt, int32_t dtype, int32_t aligned, int32_t M, int32_t N, int32_t K,
+                                int32_t *index, int32_t *count);
+
 /* In-place rotary embedding of the q and k thirds of qkv [S*T, 3*d] (row m is canvas
  * position m % T), then out[S*T, d] = softmax(q k^T / sqrt(d_head)) v per canvas and head,
  * over all T keys.

@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(HERE, "libpvf.so")
 
 PVF_F32, PVF_BF16 = 0, 1
 MX_E4M3, MX_E2M1 = 0, 1   # PVF_MX_E4M3, PVF_MX_E2M1
+MX_GEMM, MX_SWIGLU, MX_W4 = 0, 1, 2   # PVF_MX_CALL_*
 PVF_ROUTES_PLAN, PVF_ROUTES_AR, PVF_ROUTES_CAL, PVF_ROUTES_XRANDOM, PVF_ROUTES_XPLANNING = 1, 2, 4, 8, 16
 PVF_ROUTE_NONE, PVF_ROUTE_PLAN, PVF_ROUTE_AR, PVF_ROUTE_CAL = 0, 1, 2, 3
 ROUTE_NONE, ROUTE_PLAN, ROUTE_AR = 0, 1, 2
@@ -31,7 +32,8 @@ EXPORTS = ["pvf_create", "pvf_destroy", "pvf_last_error", "pvf_workspace_bytes",
            "pvf_epilogue", "pvf_round", "pvf_state_init", "pvf_decode", "pvf_stage1", "pvf_gemm",
            "pvf_gemm_swiglu", "pvf_rmsnorm", "pvf_rope_attention", "pvf_fill_normal", "pvf_entropy",
            "pvf_plan_vocab_select", "pvf_qkv_attention", "pvf_rope_attention_noalloc", "pvf_round_sync", "pvf_ctx_gemm",
-           "pvf_ctx_gemm_swiglu", "pvf_quant_mx", "pvf_add_rmsnorm_mx", "pvf_gemm_mx", "pvf_gemm_mx_swiglu", "pvf_gemm_w4"]
+           "pvf_ctx_gemm_swiglu", "pvf_quant_mx", "pvf_add_rmsnorm_mx", "pvf_gemm_mx", "pvf_gemm_mx_swiglu", "pvf_gemm_w4",
+           "pvf_gemm_mx_instance"]
 
 
 class PvfError(RuntimeError):
@@ -147,6 +149,7 @@ def lib() -> C.CDLL:
                                          C.c_void_p, C.c_int32, C.c_int32, C.c_int32]
         L.pvf_gemm_w4.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                   C.c_int32, C.c_int32, C.c_int32]
+        L.pvf_gemm_mx_instance.argtypes = [C.c_int32] * 7 + [C.POINTER(C.c_int32)] * 2
         L.pvf_fill_normal.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_uint64,
                                       C.c_float, C.c_float]
         for name in EXPORTS:
@@ -543,6 +546,14 @@ def gemm_w4(x: torch.Tensor, W: torch.Tensor, w_scales: torch.Tensor, residual: 
     _mx_call(lib().pvf_gemm_w4, (x, W, w_scales, out, residual), _dtype_code(x.dtype), x.data_ptr(), W.data_ptr(), w_scales.data_ptr(),
              out.data_ptr(), _p(residual), M, N, K)
     return out
+
+
+def gemm_mx_instance(call: int, M: int, N: int, K: int, w_fmt: int = MX_E4M3, dtype: torch.dtype = torch.bfloat16, aligned: bool = True):
+    """(index, count): the kernel instance that gemm_mx, gemm_mx_swiglu (N = ff) or gemm_w4 (call = MX_GEMM, MX_SWIGLU, MX_W4) takes, of those that
+    it chooses from; aligned: whether x of gemm_w4 begins at a multiple of 16 bytes."""
+    index, count = C.c_int32(), C.c_int32()
+    _check(lib().pvf_gemm_mx_instance(call, w_fmt, _dtype_code(dtype), int(aligned), M, N, K, C.byref(index), C.byref(count)))
+    return index.value, count.value
 
 
 def rope_attention(qkv: torch.Tensor, S: int, T: int, n_heads: int, d_head: int,

@@ -16,7 +16,7 @@
 // the 16 at 64 + 16 g, of e2m1 the 32 elements from 32 g on; its scale byte is that of k = 32 g .. 32 g + 31.  The weights are the
 // instruction's first operand, so that a lane ends up with 4 consecutive columns of C.
 //
-// Four kernels, from few results to many; run() takes the instance whose fullest CU is done first.  Bounds: few rows by the launch (a kernel that
+// Four kernels, from few results to many; choose() takes the instance whose fullest CU is done first.  Bounds: few rows by the launch (a kernel that
 // does nothing takes 3 us) and the weights' bytes; tiles on the way by a CU's loads into LDS, 125-150 GB/s from L2 in any order, some 55 of what HBM
 // delivers to all CUs; many rows by the matrix pipe and the power it takes (scaled) or by the instructions that decode (decoded).
 //   gemm_mx_waves_kernel  tiles up to 80 x 64 or 16 x 128, a ring for each wave, no barrier
@@ -27,6 +27,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <iterator>
 
 namespace pvf {
 namespace {
@@ -1117,7 +1118,7 @@ template <> struct Candidates<kRowsBf16, PVF_MX_E2M1, kOutBf16, true> {
   static constexpr int ROWS = kRowsBf16, WF = PVF_MX_E2M1, OUT = kOutBf16;
   static constexpr bool kDirect = true;
   static constexpr Candidate list[] = {
-      PVF_MX_TILE(16, 16, 1, 1, 8, 2, 1, .056f, .047f),  PVF_MX_WAVES(16, 16, 4, 4, .06f, .044f),            PVF_MX_WAVES(16, 16, 8, 16, .055f, .10f),
+      PVF_MX_WAVES(16, 16, 4, 4, .06f, .044f),           PVF_MX_WAVES(16, 16, 8, 16, .055f, .10f),
       PVF_MX_TILE(16, 16, 1, 1, 4, 2, 16, .095f, .058f), PVF_MX_WAVES(16, 64, 8, 16, .154f, .153f),          PVF_MX_WAVES(32, 32, 4, 32, .135f, .154f),
       PVF_MX_TILE(32, 64, 2, 1, 2, 2, 32, .35f, .205f),  PVF_MX_WAVES(48, 64, 4, 48, .27f, .27f),            PVF_MX_WAVES(32, 128, 4, 32, .327f, .33f),
       PVF_MX_WAVES(80, 64, 3, 80, .49f, .47f),           PVF_MX_TILE(64, 128, 2, 2, 1, 2, 64, .75f, .58f)};
@@ -1146,7 +1147,7 @@ template <> struct Candidates<kRowsF32, PVF_MX_E2M1, kOutF32, false> {
       PVF_MX_TILE(32, 64, 2, 1, 2, 2, 32, 1.0f, 1.1f),   PVF_MX_TILE(64, 128, 4, 1, 1, 2, 64, 2.9f, 2.5f),   PVF_MX_TILE(32, 128, 2, 1, 2, 2, 32, 1.45f, 1.45f)};
 };
 
-template <int ROWS, int WF, int OUT, bool kDirect = true> pvf_status run(hipStream_t s, const MxGemm &p) {
+template <int ROWS, int WF, int OUT, bool kDirect = true> MxInstance choose(const MxGemm &p) {
   const int64_t columns = OUT == kOutSwiglu ? mx_width(p.N) : p.N;
   const int64_t stages = mx_width(p.K) / kMxStage;
   const Candidate *best = nullptr;
@@ -1158,25 +1159,30 @@ template <int ROWS, int WF, int OUT, bool kDirect = true> pvf_status run(hipStre
     const float cost = fullest == 1 ? c.alone : c.among * (float)fullest;
     if (!best || cost < least) { best = &c; least = cost; }
   }
-  return best->run(s, p);
+  const auto &list = Candidates<ROWS, WF, OUT, kDirect>::list;
+  return {best->run, (int)(best - list), (int)std::size(list)};
 }
 
-template <int WF> pvf_status run_mx(hipStream_t s, const MxGemm &p) {
-  if (p.c_scales) return run<kRowsMxExact, WF, kOutSwiglu>(s, p);
-  if (p.dtype == PVF_F32) return run<kRowsMxExact, WF, kOutF32>(s, p);
-  return run<kRowsMx, WF, kOutBf16>(s, p);
+template <int WF> MxInstance choose_mx(const MxGemm &p) {
+  if (p.c_scales) return choose<kRowsMxExact, WF, kOutSwiglu>(p);
+  if (p.dtype == PVF_F32) return choose<kRowsMxExact, WF, kOutF32>(p);
+  return choose<kRowsMx, WF, kOutBf16>(p);
 }
 
 }  // namespace
 
-pvf_status launch_gemm_mx(hipStream_t s, const MxGemm &p) {
-  if (p.M == 0 || p.N == 0) return PVF_OK;
+MxInstance gemm_mx_instance(const MxGemm &p) {
   if (!p.a_scales) {                                         // rows that begin at 16-byte chunks go straight to LDS
     const bool f32 = p.dtype == PVF_F32, direct = (uintptr_t)p.A % 16 == 0 && p.K % (f32 ? 4 : 8) == 0;
-    if (f32) return direct ? run<kRowsF32, PVF_MX_E2M1, kOutF32>(s, p) : run<kRowsF32, PVF_MX_E2M1, kOutF32, false>(s, p);
-    return direct ? run<kRowsBf16, PVF_MX_E2M1, kOutBf16>(s, p) : run<kRowsBf16, PVF_MX_E2M1, kOutBf16, false>(s, p);
+    if (f32) return direct ? choose<kRowsF32, PVF_MX_E2M1, kOutF32>(p) : choose<kRowsF32, PVF_MX_E2M1, kOutF32, false>(p);
+    return direct ? choose<kRowsBf16, PVF_MX_E2M1, kOutBf16>(p) : choose<kRowsBf16, PVF_MX_E2M1, kOutBf16, false>(p);
   }
-  return p.w_fmt == PVF_MX_E4M3 ? run_mx<PVF_MX_E4M3>(s, p) : run_mx<PVF_MX_E2M1>(s, p);
+  return p.w_fmt == PVF_MX_E4M3 ? choose_mx<PVF_MX_E4M3>(p) : choose_mx<PVF_MX_E2M1>(p);
+}
+
+pvf_status launch_gemm_mx(hipStream_t s, const MxGemm &p) {
+  if (p.M == 0 || p.N == 0) return PVF_OK;
+  return gemm_mx_instance(p).run(s, p);
 }
 
 }  // namespace pvf

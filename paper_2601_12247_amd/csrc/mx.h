@@ -29,6 +29,13 @@ struct MxGemm {
 };
 pvf_status launch_gemm_mx(hipStream_t s, const MxGemm &g);
 
+// The kernel instance that a product's launch takes: `index` of the `count` that products of this kind choose from.
+struct MxInstance {
+  pvf_status (*run)(hipStream_t, const MxGemm &);
+  int index, count;
+};
+MxInstance gemm_mx_instance(const MxGemm &g);
+
 #ifdef __HIPCC__
 // A launch takes fewer than 2^32 threads along x: workgroups from the 2^22th on go on in y.
 constexpr int kMxGridBits = 22;

@@ -1126,6 +1126,25 @@ extern "C" pvf_status pvf_gemm_w4(void *stream, int32_t dtype, const void *x, co
   return launch_gemm_mx((hipStream_t)stream, g);
 }
 
+extern "C" pvf_status pvf_gemm_mx_instance(int32_t call, int32_t w_fmt, int32_t dtype, int32_t aligned, int32_t M, int32_t N, int32_t K,
+                                           int32_t *index, int32_t *count) {
+  PVF_REQUIRE(nullptr, call >= PVF_MX_CALL_GEMM && call <= PVF_MX_CALL_W4, PVF_EINVAL, "pvf_gemm_mx_instance: call=%d", call);
+  const bool w4 = call == PVF_MX_CALL_W4, swiglu = call == PVF_MX_CALL_SWIGLU;
+  if (!swiglu && check_dtype(dtype) != PVF_OK) return PVF_EINVAL;
+  PVF_REQUIRE(nullptr, w4 || w_fmt == PVF_MX_E4M3 || w_fmt == PVF_MX_E2M1, PVF_EINVAL, "pvf_gemm_mx_instance: w_fmt=%d", w_fmt);
+  if (const pvf_status st = check_mx_sizes("pvf_gemm_mx_instance", M, N, K)) return st;
+  PVF_REQUIRE(nullptr, M > 0 && N > 0 && index && count, PVF_EINVAL, "pvf_gemm_mx_instance: nothing to launch, or index or count is NULL");
+  MxGemm g;                                                  // the choice reads which tensors there are and where A begins, not what they hold
+  g.A = (const void *)(uintptr_t)(aligned ? 16 : 4);
+  if (!w4) g.a_scales = (const uint8_t *)4;
+  if (swiglu) g.c_scales = (uint8_t *)4;
+  g.M = M; g.N = N; g.K = K; g.w_fmt = w4 ? PVF_MX_E2M1 : w_fmt; g.dtype = swiglu ? PVF_BF16 : dtype;
+  const MxInstance chosen = gemm_mx_instance(g);
+  *index = chosen.index;
+  *count = chosen.count;
+  return PVF_OK;
+}
+
 // Builds the rotary table on the host for this call, so it synchronises the stream and
 // allocates; it exists for tests, the round itself uses the context's table.
 extern "C" pvf_status pvf_rope_attention(void *stream, int32_t dtype, void *qkv, void *out, int32_t S,
