@@ -46,3 +46,13 @@ def test_instance_refuses():
     assert f(0, 0, 0, 1, 1, 1, (1 << 22) + 1, i, i) == -2
     assert f(0, 0, 0, 1, 1, 1, 32, None, i) == -1 and f(0, 0, 0, 1, 1, 1, 32, i, None) == -1
     assert f(1, 0, 7, 1, 1, 1, 32, i, i) == 0 and f(2, 7, 0, 0, 1, 1, 32, i, i) == 0        # what is not read
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_gpu_tests_run_every_instance(kind):
+    """With one stage of 128 k (or two, where stages go in pairs), and with twelve or more."""
+    from tests.test_gpu_mx_instances import LONG, SHORT
+    for shapes, stages in ((SHORT[kind], range(1, 3)), (LONG[kind], range(11, 100))):
+        taken = [instance(kind, *s) for s in shapes]
+        assert all((K + 127) // 128 in stages for _, _, K in shapes)
+        assert [index for index, _ in taken] == list(range(taken[0][1]))
