@@ -43,8 +43,9 @@ SHORT, LONG = {
     "w4_f32": [(1, 16, 1408), (1, 4107, 1408), (2, 16, 1408), (2, 4111, 1408), (209, 290, 1408), (518, 451, 1408), (1604, 912, 1408)],
     "w4_f32_shifted": [(1, 16, 1411), (1, 8209, 1411), (2, 16, 1411), (5, 16, 1411), (306, 194, 1411), (583, 400, 1411), (404, 615, 1411), (1201, 844, 1411), (843, 582, 1411)],
 }
-# eight waves that share k have several stages each from 1024 elements on
-MORE = {"mx_e4m3_f32": [(1, 16, 4104)], "mx_e2m1_f32": [(3, 33, 4104)], "w4": [(1, 16, 4104), (16, 16, 4104), (1, 12290, 4104)], "w4_shifted": [(1, 16, 4101), (3, 17, 4101)],
+# eight waves that share k have several stages each from 1024 elements on; of few rows as many results as single roundings take to show
+MORE = {"swiglu_e4m3": [(16, 8000, 1411)], "swiglu_e2m1": [(13, 8000, 1411)],
+        "mx_e4m3_f32": [(1, 16, 4104)], "mx_e2m1_f32": [(3, 33, 4104)], "w4": [(1, 16, 4104), (16, 16, 4104), (1, 12290, 4104)], "w4_shifted": [(1, 16, 4101), (3, 17, 4101)],
         "w4_f32": [(1, 16, 4104), (1, 4107, 4104), (9, 16, 4104), (3, 4110, 4104)], "w4_f32_shifted": [(1, 16, 4101), (1, 8209, 4101), (3, 16, 4101), (9, 33, 4101)]}
 PRODUCTS = [k for k in KINDS if not k.startswith("swiglu")]
 

@@ -4,7 +4,9 @@ import torch
 
 from paper_2601_12247_amd import binding as B
 from tests import mx_reference as R
-from tests.test_gpu_mx import cuda64, guarded_mx, within_codes
+from tests.test_gpu_mx import cuda64, guarded_mx, random_mx, within_codes
+from tests.test_gpu_mx_instances import LONG, MORE, SHORT, cases
+from tests.test_mx_instances import KINDS
 
 pytestmark = pytest.mark.gpu
 
@@ -41,4 +43,67 @@ def test_gates_far_below_zero(M, fmt, ups):
     out, untouched = guarded_mx(M, ff)
     B.gemm_mx_swiglu(*R.pack(a, a_b, R.E4M3), *R.pack(w, w_b, fmt), out=out)
     assert within_codes(out, want, 2.0 ** -21 * want.abs() + 2.0 ** -149)
+    assert untouched()
+
+
+def flips(got, want):
+    """How many codes of blocks whose scale is the definition's stand for another value than the definition's, and how many scales differ."""
+    codes, byte = R.unpack(*got, R.E4M3)
+    c, b = R.quantise(want, R.E4M3)
+    same = byte == b
+    return int((R.values(codes, byte, R.E4M3) != R.values(c, b, R.E4M3))[same.repeat_interleave(32, 1)].sum()), int((~same).sum())
+
+
+@pytest.mark.parametrize("kind,M,ff,K", cases(SHORT, LONG, MORE, kinds=["swiglu_e4m3", "swiglu_e2m1"]))
+def test_swiglu_sums_in_float32(kind, M, ff, K):
+    """SwiGLU decodes its operands and adds in float32.  A sum of K products of random signs is off by 0.4 2^-24 of its size at each of at most K / 8 + 16 additions (the root mean
+    square of a rounding of 24 bits), which do not add up one way: 2.5 2^-24 sqrt(K / 8 + 16) of the products' root sum of squares is six times that.  silu(g) u is
+    evaluated within 3 * 2^-23 (an exponential 2^-23; its correction, the reciprocal and two products 2^-24 each).  A code differs from the definition's where
+    its value is nearer to a border of two codes than the error: with a sixth of the bound as the error's size and values that lie anywhere between
+    the borders, in the sum of error / step of all codes.  The instruction with the cut-off would change 0.3 % of the codes, products rounded to bfloat16 some 2 %."""
+    fmt = KINDS[kind][1]
+    a, a_b, av = random_mx(M, K, R.E4M3, M + K)
+    w, w_b, wv = random_mx(2 * ff, K, fmt, ff + 1, 0.05)
+    p, size = cuda64(av, wv), cuda64(av * av, wv * wv).sqrt()
+    err = 2.5 * 2.0 ** -24 * (K / 8 + 16) ** 0.5 * size
+    gate, up = p[:, :ff], p[:, ff:]
+    silu = gate * torch.sigmoid(gate)
+    want = silu * up
+    slack = 1.1 * (up.abs() + err[:, ff:]) * err[:, :ff] + silu.abs() * err[:, ff:] + 3 * 2.0 ** -23 * want.abs()
+    out, untouched = guarded_mx(M, ff)
+    B.gemm_mx_swiglu(*R.pack(a, a_b, R.E4M3), *R.pack(w, w_b, fmt), out=out)
+    assert within_codes(out, want, slack)
+    s = torch.pow(2.0, (R.quantise(want, R.E4M3)[1] - 127).double()).repeat_interleave(32, 1)[:, :ff]
+    step = torch.maximum(torch.pow(2.0, torch.floor(torch.log2(want.abs().clamp(min=2.0 ** -300))) - 3), s * 2.0 ** -9)
+    expected = float((slack / 6 / step).clamp(max=1).sum())
+    codes, scales = flips(out, want)
+    assert codes <= expected + 6 * expected ** 0.5 + 3 and scales <= 1, (codes, expected, scales)
+    assert untouched()
+
+
+@pytest.mark.parametrize("fmt", [R.E4M3, R.E2M1])
+@pytest.mark.parametrize("M", [1, 24, 100])
+def test_silu_to_the_last_bits(M, fmt):
+    """Products that float32 adds exactly, so that what may be off is silu(g) u: 3 * 2^-23 of it (above).  exp(-g) by a product that is rounded before
+    the power is taken would be off by |g| 2^-24: 4 * 2^-23 from 8 on, ten times the bound at the far gates."""
+    ff, K, g = 24576 if M == 1 else 6144, 128, torch.Generator().manual_seed(M)
+    w = torch.zeros(2 * ff, K, dtype=torch.float64)
+    centre = -torch.linspace(-12, 60, ff // 32, dtype=torch.float64).repeat_interleave(32)       # gates of a block lie together, so none is lost under the block's largest
+    left = torch.round((centre + torch.rand(ff, generator=g, dtype=torch.float64)) * 256) / 256
+    for k in (0, 32, 64):                                    # three codes add up to a gate, or nearly
+        w[:ff, k] = left
+        w[:ff, k] = R.values(*R.quantise(w[:ff], fmt), fmt)[:, k]
+        left = left - w[:ff, k]
+    w[ff:, 96] = torch.randint(0, 2, (ff,), generator=g).double() * 2 - 1
+    a = torch.zeros(M, K, dtype=torch.float64)
+    a[:, 0:96:32] = 1 + (torch.arange(M) % 8 / 8.0)[:, None]
+    a[:, 96] = 1.0
+    (w, w_b), (a, a_b) = R.quantise(w, fmt), R.quantise(a, R.E4M3)
+    p = cuda64(R.values(a, a_b, R.E4M3), R.values(w, w_b, fmt))
+    gate, up = p[:, :ff], p[:, ff:]
+    assert torch.equal(p, p.float().double()) and gate.min() > -120
+    want = gate / (1 + torch.exp(-gate)) * up
+    out, untouched = guarded_mx(M, ff)
+    B.gemm_mx_swiglu(*R.pack(a, a_b, R.E4M3), *R.pack(w, w_b, fmt), out=out)
+    assert within_codes(out, want, 3 * 2.0 ** -23 * want.abs())
     assert untouched()
