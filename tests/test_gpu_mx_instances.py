@@ -108,3 +108,15 @@ def test_random_rows(kind, M, N, K):
     tol = HALF_STEP[name] * want.abs() + 2.0 ** -24 * mag * additions + (cut_off(av, wv) if scaled else 0)
     assert bool(((got - want).abs() <= tol).all()), ((got - want).abs() / tol).max()
     assert (got - want).norm() <= (1e-6 if name == "f32" else 2.3e-3) * want.norm()
+
+
+def test_4_bit_products_of_2_32_threads():
+    """The largest number of threads along x is 2^32 - 1: tiles of 16 rows and 512 threads go on in y from 2^27 rows on."""
+    M = (1 << 27) + 3
+    assert B.gemm_mx_instance(B.MX_W4, M, 1, 4, B.MX_E2M1, torch.float32) == B.gemm_mx_instance(B.MX_W4, 16, 16, 4, B.MX_E2M1, torch.float32)     # 16 x 16, eight waves
+    x = (torch.arange(M, device="cuda", dtype=torch.int32) % 1021).float()[:, None].repeat(1, 4)
+    w, w_b = torch.zeros(1, 128, dtype=torch.int64), torch.full((1, 4), 127)
+    w[0, :4] = torch.tensor([5, 2, 0, 10])                   # 3, 1, 0, -1
+    out, untouched = guarded((M, 1), torch.float32, 0xa5)
+    B.gemm_w4(x, *R.pack(w, w_b, R.E2M1), out=out)
+    assert torch.equal(out, x[:, :1] * 3) and untouched()
