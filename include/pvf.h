@@ -315,7 +315,9 @@ pvf_status pvf_rmsnorm(void *stream, int32_t dtype, const void *x, const void *g
  * saturates; elements are rounded to the nearest code, ties to even.  A block that holds a NaN or an infinity has scale byte 255, which
  * stands for NaN, and zero codes: every result that reads it is NaN.
  * codes, scales and rows of bf16 / float32 may begin at any element but for this: codes at multiples of 16 bytes, scales of 4.  Rows (M, N) are
- * at most 2^28, elements of a row (K, ff) at most 2^22.  Elements below 2^-126 may count as zero in a product.  The calls use no workspace: those on different streams may overlap, and all may be captured into a graph. */
+ * at most 2^28, elements of a row (K, ff) at most 2^22.  What lies below 2^-126 of an
+ * element may count as zero in a product, and an element of 2^128 or more (float32 rows are rounded to it from 2.9e38 on) as infinite, but
+ * for PVF_BF16 results of pvf_gemm_mx.  The calls use no workspace: those on different streams may overlap, and all may be captured into a graph. */
 enum { PVF_MX_E4M3 = 0, PVF_MX_E2M1 = 1 };
 
 /* codes, scales = x [M, K] (dtype PVF_F32 / PVF_BF16) in format fmt. */

@@ -120,3 +120,36 @@ def test_4_bit_products_of_2_32_threads():
     out, untouched = guarded((M, 1), torch.float32, 0xa5)
     B.gemm_w4(x, *R.pack(w, w_b, R.E2M1), out=out)
     assert torch.equal(out, x[:, :1] * 3) and untouched()
+
+
+@pytest.mark.parametrize("fmt", [R.E4M3, R.E2M1])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_elements_at_the_ends_of_the_scales(fmt, dtype):
+    """Every magnitude with the scales at either end, against 2^60 or 2^-60.  Bfloat16 results are the exact product rounded.  For float32 results elements become bfloat16: what lies
+    below 2^-126 may be lost, and 2^128 and more is infinite."""
+    n = 126 if fmt == R.E4M3 else 7
+    codes = torch.zeros(n, 128, dtype=torch.int64)
+    codes[:, 0] = torch.arange(1, n + 1)
+    one = torch.zeros(1, 128, dtype=torch.int64)
+    one[0, 0] = 0x38
+    for byte in (0, 1, 2, 7, 8, 240, 246, 247, 248, 253, 254):
+        by = 60 if byte < 127 else -60
+        W = R.pack(codes, torch.full((n, 4), byte), fmt)
+        v = R.values(codes, torch.full((n, 4), byte), fmt)[:, 0]
+        got = B.gemm_mx(*R.pack(one, torch.full((1, 4), 127 + by), R.E4M3), *W, dtype=dtype).cpu().double()[0] * 2.0 ** -by
+        if dtype is torch.bfloat16:
+            assert torch.equal(got, v), byte                 # at most 4 bits each
+        else:
+            assert bool(((got - v).abs() <= 2.0 ** -126)[v < 2.0 ** 128].all()) and torch.equal(got[v >= 2.0 ** -120].isinf(), v[v >= 2.0 ** -120] >= 2.0 ** 128), byte
+
+
+@pytest.mark.parametrize("exponent", [-126, -118, -110, -60])
+def test_parts_of_small_float32_rows(exponent):
+    """Rows of 24 bits go as three parts; what of them lies below 2^-126 may be lost, and no more."""
+    x = torch.zeros(70, 128)
+    x[:, 0] = (1 + torch.rand(70, generator=torch.Generator().manual_seed(1))) * 2.0 ** exponent
+    w, w_b = torch.zeros(33, 128, dtype=torch.int64), torch.full((33, 4), 127 + 100)
+    w[:, 0] = 2                                              # ones
+    got = B.gemm_w4(x.cuda(), *R.pack(w, w_b, R.E2M1)).cpu().double() * 2.0 ** -100
+    assert bool(((got - x[:, :1].double()).abs() <= 2.0 ** -126).all())
+    assert exponent < -103 or torch.equal(got, x[:, :1].double().expand(70, 33))      # the last of 24 bits is above 2^-126
