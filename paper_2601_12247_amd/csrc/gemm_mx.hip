@@ -58,8 +58,8 @@ __device__ __forceinline__ float silu_f(float g) {
 // float32's normal range from -92 on and its divisor above float32 from -89 on, while the product may be any code: a block's scale goes down to 2^-127.  (u 2^-64: what
 // that loses is below 2^-168 in the product.)  Below -256 the product is less than 2^-230: zero.
 __device__ __forceinline__ float far_act(float g, float u) {
-  const float q = g * kLog2e, n = rintf(q), e = __builtin_amdgcn_exp2f(q - n), ec = fmaf(e, kLn2 * fmaf(g, kLog2eRest, fmaf(g, kLog2e, -q)), e);
-  return __builtin_ldexpf(g * ec * (u * 0x1p-64f), (int)n + 64);
+  const float n = rintf(g * kLog2e), f = fmaf(g, kLog2eRest, fmaf(g, kLog2e, -n));      // g log2(e) - n, rounded to 2^-25
+  return __builtin_ldexpf(g * __builtin_amdgcn_exp2f(f) * (u * 0x1p-64f), (int)n + 64);
 }
 
 // The four registers of 32 e2m1 codes; the instruction does not read the others.

@@ -107,3 +107,26 @@ def test_silu_to_the_last_bits(M, fmt):
     B.gemm_mx_swiglu(*R.pack(a, a_b, R.E4M3), *R.pack(w, w_b, fmt), out=out)
     assert within_codes(out, want, 3 * 2.0 ** -23 * want.abs())
     assert untouched()
+
+
+@pytest.mark.parametrize("fmt", [R.E4M3, R.E2M1])
+def test_far_gates_to_the_last_bits(fmt):
+    """As above with gates of -80 to -240 and factors of some 2^100 (400 000 different codes): an argument of the exponential off by half a last place of 128 (2^-17) would move 1 code of 40 000
+    beyond 3 * 2^-23 of the value (the argument is rounded to 2^-25, the exponential off by 2^-23, three products by 2^-24 each)."""
+    M, ff, K, g = 64, 6144, 128, torch.Generator().manual_seed(5)
+    w = torch.zeros(2 * ff, K, dtype=torch.float64)
+    centre = -torch.linspace(81, 127, ff // 32, dtype=torch.float64).repeat_interleave(32)
+    w[:ff, :96] = as_terms(torch.round((centre - torch.rand(ff, generator=g, dtype=torch.float64)) * 256) / 256, fmt)
+    w[ff:, 96] = 2.0 ** 100 * (torch.randint(0, 2, (ff,), generator=g).double() * 2 - 1) * (1 + torch.randint(0, 2, (ff,), generator=g) / 2.0)
+    a = torch.zeros(M, K, dtype=torch.float64)
+    a[:, 0:96:32] = 1 + (torch.arange(M) % 8 / 8.0)[:, None]
+    a[:, 96] = 1 + torch.arange(M) // 8 % 8 / 8.0
+    (w, w_b), (a, a_b) = R.quantise(w, fmt), R.quantise(a, R.E4M3)
+    p = cuda64(R.values(a, a_b, R.E4M3), R.values(w, w_b, fmt))
+    gate, up = p[:, :ff], p[:, ff:]
+    assert torch.equal(p, p.float().double()) and gate.max() <= -80 and gate.min() >= -256
+    want = gate * torch.exp(gate) / (1 + torch.exp(gate)) * up
+    out, untouched = guarded_mx(M, ff)
+    B.gemm_mx_swiglu(*R.pack(a, a_b, R.E4M3), *R.pack(w, w_b, fmt), out=out)
+    assert within_codes(out, want, 3 * 2.0 ** -23 * want.abs() + 2.0 ** -149)
+    assert untouched()
