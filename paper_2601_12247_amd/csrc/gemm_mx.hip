@@ -8,7 +8,8 @@
 //
 // The scaled instruction adds 8 neighbouring products at a time, each cut off 13 bits below the largest of the eight (measured: 16 and 2^-8 1.27 in
 // one group lose what lies below 2^-9), then those sums and the accumulator in float32.  On random operands that is 1.5e-5 of the
-// result, a hundredth of a bfloat16 rounding.  Float32 results do not take it (the bfloat16 instruction keeps float32 sums), nor does SwiGLU,
+// result, a hundredth of a bfloat16 rounding: one result in 40 rounds to its other neighbour, and the error against 64 bits stays 1.66e-3.  An e4m3 element is itself rounded by up to
+// 2^-4 of it, 70 times what its product can cost the others of its eight (7 2^-13 of it).  Float32 results do not take it (the bfloat16 instruction keeps float32 sums), nor does SwiGLU,
 // whose 8-bit results would differ from the definition's in 0.3 % of the codes and here and there in a block's scale, where float32
 // sums differ in one of 10^5; it would take half the time of the matrix instructions.
 //
@@ -19,7 +20,7 @@
 // Four kernels, from few results to many; choose() takes the instance whose fullest CU is done first.  Bounds: few rows by the launch (a kernel that
 // does nothing takes 3 us) and the weights' bytes; tiles on the way by a CU's loads into LDS, 125-150 GB/s from L2 in any order, some 55 of what HBM
 // delivers to all CUs; many rows by the matrix pipe and the power it takes (scaled) or by the instructions that decode (decoded).
-//   gemm_mx_waves_kernel  tiles up to 80 x 64 or 16 x 128, a ring for each wave, no barrier
+//   gemm_mx_waves_kernel  tiles up to 80 x 64 or 32 x 128, a ring for each wave, no barrier
 //   gemm_mx_kernel        tiles from 16 x 16 to 192 x 256, one ring; rows at any element
 //   gemm_mx_steps_kernel  64 x 128 and 128 x 128, decoded operands
 //   gemm_mx_quad_kernel   256 x 256, scaled instruction
@@ -314,7 +315,7 @@ template <int ROWS, int WF, int BM, int BN, int WM, int WN, int WK, int kStages,
 // from memory (whole 128-byte lines per request: loads of 64-byte pieces straight into registers reached half the rate), one barrier
 // a stage.  Rows of bf16 / float32 that do not begin at 16-byte chunks go through registers (kDirect = false).
 // Bound by the CU's loads: a stage's BM + BN rows, not its BM BN results, so tiles are as square as the launch leaves them.  WK > 1 where there are fewer
-// tiles than CUs: more loads in flight for the same tile.  1280 x 4096 x 12288, e4m3 weights, 160 x 128 tiles: 94 us, 1.37 PFLOP/s; one row of float32
+// tiles than CUs: more loads in flight for the same tile.  1280 x 4096 x 12288, e4m3 weights, 160 x 128 tiles: 77-83 us, 1.6 PFLOP/s; one row of float32
 // against 4-bit weights 12288 x 4096, 16 x 64 with k over 8 waves: 11.6 us (16 columns a workgroup 17: the row is split into its three parts
 // for every 16 of them); 33 float32 rows that are not aligned, 4001 x 1411: 9.7 us, the latency of three stages.
 template <int ROWS, int WF, int OUT, int BM, int BN, int WM, int WN, int WK, int kStages, int AR, bool kDirect>
@@ -517,9 +518,9 @@ pvf_status run_as(hipStream_t s, const MxGemm &p) {
 // A workgroup computes BM x BN results for launches whose tiles make about one round over the chip: its kWaves waves take the 128s of k in turn, each
 // with the whole tile and a ring of two slots of LDS of its own, so that the loop has no barrier and the waves' loads, reads and matrix
 // instructions drift apart; a slot is loaded again as soon as it is in registers.  The sums are added through LDS at the end.
-// Bound by the bytes in flight: 4 waves with two stages of 80 x 64 are all of a CU's LDS.  320 x 4096 x 12288, e4m3 weights: 25 us, 1.8 MB for each CU
+// Bound by the bytes in flight: 4 waves with two stages of 80 x 64 are all of a CU's LDS.  320 x 4096 x 12288, e4m3 weights: 25-26 us, 1.8 MB for each CU
 // in 20 us behind 5 of launch and first loads (one ring with a barrier a stage: 30); splitting k over workgroups as well would need a workspace.  One
-// row against 4-bit weights 12288 x 4096: 6.5 us with the call, 4.1 TB/s; 320 rows against 4096 x 4096: 18.4 us.
+// row against 4-bit weights 12288 x 4096: 6.9 us with the call, 3.9 TB/s; 320 rows against 4096 x 4096: 18-19 us.
 template <int ROWS, int WF, int OUT, int BM, int BN, int kWaves, int AR>
 __global__ void __launch_bounds__(64 * kWaves)
 gemm_mx_waves_kernel(MxGemm p, TileMap tm) {
@@ -690,8 +691,8 @@ pvf_status run_waves(hipStream_t s, const MxGemm &p) {
 // conversions a matrix instruction) and the codes after those are read from LDS; in the middle of a stage the next one has landed, every wave
 // has read this one, one barrier, and its slot is loaded again.  Two workgroups fit a CU's registers.
 // Bound by issue: a conversion beside a matrix instruction costs 2 cycles of its 16 (measured: 7.3 ns an instruction alone, 9.5 with two conversions), so
-// 1.3 times the matrix time is the limit.  gate|up of 2560 rows, 12288 x 4096, e4m3 weights: 390-400 us, 1.3 PFLOP/s (bfloat16 products of
-// a library, 16384 cube: 1.6; the same tile on one ring, decoding before the instructions: 436 us).  64 rows, 4-bit weights, 64 x 128 tiles of four stages: 20 us, where the
+// 1.3 times the matrix time is the limit.  gate|up of 2560 rows, 12288 x 4096, e4m3 weights: 395-419 us, 1.3 PFLOP/s (bfloat16 products of
+// a library, 16384 cube: 1.6; the same tile on one ring, decoding before the instructions: 441 us; this library's bfloat16 product with SwiGLU: 372-387).  64 rows, 4-bit weights, 64 x 128 tiles of four stages: 21-22 us, where the
 // loads alone take 15: the conversions of 192 workgroups' weights do not all fit beside them.
 template <int WF, int OUT, int TM, int kStages>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
@@ -878,9 +879,9 @@ template <int BT, int WT> __device__ __forceinline__ int half_row(int r) {
 // A wave multiplies, stage by stage of 128 k, lower A x lower W, lower x upper, upper x upper, upper x lower.  The operands of a half are read
 // from LDS one quadrant before their first use, which frees their rows early: each half of a stage's slot is refilled as soon as it is
 // read, one barrier per half stage, so loads are issued evenly and have 1 to 1.5 stages to land.  Scale bytes have a ring of three stages.
-// Bound by power: 11520 x 12288 x 4096, e4m3 weights, 437-446 us, 2.6 PFLOP/s at 1.8 GHz of 2.4 with the matrix pipe busy for 553 000 cycles, 0.7 of the
+// Bound by power: 11520 x 12288 x 4096, e4m3 weights, 435-459 us, 2.6 PFLOP/s at 1.8 GHz of 2.4 with the matrix pipe busy for 553 000 cycles, 0.7 of the
 // time (a library's 8-bit product without block scales: 3.0 at 8192 cubed, 3.2 at 16384).  256 x 256 because a tile's operands are 1 / 128 of its work: 192 x 256 with one
-// barrier a stage takes 532 us.  e2m1 weights: 512 us, ten registers spilled where one operand of the instruction is 4 registers wide and the other 8.
+// barrier a stage takes 586 us.  e2m1 weights: 493-514 us, ten registers spilled where one operand of the instruction is 4 registers wide and the other 8.
 template <int WF>
 __global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
 gemm_mx_quad_kernel(MxGemm p, TileMap tm) {
@@ -1075,8 +1076,11 @@ template <int WF> pvf_status run_quad(hipStream_t s, const MxGemm &p) {
 // ---- which instance -------------------------------------------------------------------------------------------------
 // What a tile costs for 128 k, in microseconds, measured at K = 4096 and 12288 (launch time less 3 us, over the stages and the tiles of the fullest CU):
 // where a CU has one tile, and per tile where it has several (those that fit its LDS run at a time and hide each other's barriers and
-// latencies).  The launch takes the instance whose fullest CU is done first: within 6 % of the best of its list for 68 launches of 1 to 2560 rows against 4096 x 4096,
-// 12288 x 4096 and 4096 x 12288.  Small tiles cost what their rows' loads cost, not their area.
+// latencies).  The launch takes the instance whose fullest CU is done first.  Of 188 launches of 1 to 11520 rows, against 4096 x 4096, 12288 x 4096 and 4096 x 12288 mostly, 181 take at
+// most 1.05 times what the best of their list takes, the others up to 1.18.  Small tiles cost what their rows' loads cost, not their area.  Known to be off, because
+// SwiGLU and float32 results have one cost for weights of either type, and one for stages whether weights come from HBM or a cache: SwiGLU of up to 16 rows against e4m3 weights 12288 x 4096
+// takes 30 us on 16 x 64 tiles (64 x 64: 25); 11520 x 4096 x 12288 with e2m1 weights 547 on 256 x 256 (192 x 256: 472); 1280 x 4096 x 4096 of bfloat16 rows against 4-bit weights
+// 56 on 32 x 128 (64 x 128: 50); 320 x 12288 x 4096 with e2m1 weights and float32 results 41 on 64 x 128 (80 x 64: 37).
 struct Candidate {
   int BM, BN, most_rows;                                     // most_rows: rows of A that the instance loads (0: any number)
   float alone, among;
