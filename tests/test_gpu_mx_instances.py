@@ -153,3 +153,29 @@ def test_parts_of_small_float32_rows(exponent):
     got = B.gemm_w4(x.cuda(), *R.pack(w, w_b, R.E2M1)).cpu().double() * 2.0 ** -100
     assert bool(((got - x[:, :1].double()).abs() <= 2.0 ** -126).all())
     assert exponent < -103 or torch.equal(got, x[:, :1].double().expand(70, 33))      # the last of 24 bits is above 2^-126
+
+
+@pytest.mark.parametrize("kind,M,N,K", [c for c in cases(LONG, kinds=list(KINDS)) if c[1] > 32])
+def test_blocks_that_are_not_finite(kind, M, N, K):
+    """A NaN or an infinity in a block of a row, or of a row of weights, makes NaN of the results that read it (of SwiGLU, of the blocks that hold them) and of no others."""
+    call, fmt, dtype, aligned = KINDS[kind]
+    g = torch.Generator(device="cuda").manual_seed(M + N)
+    x = torch.randn(M, K, device="cuda", generator=g)
+    w = torch.randn((2 if call == B.MX_SWIGLU else 1) * N, K, device="cuda", generator=g) * 0.05
+    m, n = [0, M // 2, M - 1], [0, N // 3, N - 1]
+    x[m, [K - 1, K // 2, 0]] = torch.tensor([float("nan"), float("inf"), float("nan")], device="cuda")
+    w[n, [0, K - 1, K // 2]] = torch.tensor([float("inf"), float("nan"), float("-inf")], device="cuda")
+    W = B.quant_mx(w, fmt)
+    if call == B.MX_W4:
+        bad = torch.isnan(product(kind, x.to(dtype), W))
+        bad[m[1]] = True                                     # unquantised: an infinity may give one
+    elif call == B.MX_GEMM:
+        bad = torch.isnan(B.gemm_mx(*B.quant_mx(x), *W, dtype=dtype))
+    else:
+        codes, scales = B.gemm_mx_swiglu(*B.quant_mx(x), *W)
+        bad = (scales.view(torch.uint8) == 255).transpose(0, 1).reshape(M, -1)[:, :(N + 31) // 32]
+        n = [k // 32 for k in n]
+    want = torch.zeros_like(bad)
+    want[m] = True
+    want[:, n] = True
+    assert torch.equal(bad, want)
