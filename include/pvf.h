@@ -354,6 +354,63 @@ enum { PVF_MX_CALL_GEMM = 0, PVF_MX_CALL_SWIGLU = 1, PVF_MX_CALL_W4 = 2 };
 pvf_status pvf_gemm_mx_instance(int32_t call, int32_t w_fmt, int32_t dtype, int32_t aligned, int32_t M, int32_t N, int32_t K,
                                 int32_t *index, int32_t *count);
 
+/* ---- keys and values in pages -------------------------------------------------------------
+ * A cache that B requests of different lengths share: pages of page_size tokens in one pool, [n_pages, Hkv, page_size, d_head] each for
+ * keys and values in dtype.  What is in a page is contiguous; pages may lie further apart (page strides, in elements), as in a pool that holds
+ * keys and values, or layers, side by side.  Row b of the table, int32 [B, width] (rows table_stride apart), names the pages of request b in
+ * order: the token at position p lies on page table[b][p / page_size], and its slot is that page * page_size + p % page_size.
+ * All arrays here are dev, int32 ones among them; lengths and counts stay on the GPU.  The calls allocate nothing and may be captured into a graph;
+ * what they keep between their launches is in their outputs or the workspace, so calls on different streams may overlap if those differ.
+ * Sizes: B <= 2^20, M <= 2^24, width * page_size <= 2^30; caches d_head and page_size multiples of 8, up to 256 and 65536, rows and caches at
+ * multiples of 16 bytes with strides of such. */
+
+/* Pages for rows that requests are about to add or write again: request b computes n_rows[b] rows, at positions start[b] .. (start NULL: behind
+ * its seq_len[b] tokens), and is seq_len_out[b] = max(seq_len[b], start[b] + n_rows[b]) tokens long then.  Pages that it lacks are taken from
+ * the end of free_pages[0 .. *n_free), in order of requests, and written into its row of the table.
+ * Request b is admitted (admitted[b] = 1) iff n_rows[b] >= 0, 0 <= start[b] <= seq_len[b], its tokens before and after fit the table, its rows end within
+ * M, and it lacks no page or there are enough for it and all in front of it that are sound so far; others (0) keep their length and get none.
+ * Rows lie behind each other: those of request b are cu_rows[b] .. cu_rows[b + 1] - 1 (cu_rows [B + 1], at most M); pos and slot [M] are their positions
+ * and slots, slot -1 where the request was not admitted or its table holds no page; rows behind the last request have position 0 and slot -1.
+ * place [B + 1] is the number of free pages before and after each request, *n_free_out the last of them.
+ * seq_len_out may be seq_len, n_free_out may be n_free; nothing else may overlap. */
+pvf_status pvf_page_extend(void *stream, const int32_t *seq_len, const int32_t *start, const int32_t *n_rows, int32_t B, int32_t *table,
+                           int32_t width, int64_t table_stride, int32_t page_size, const int32_t *free_pages, int32_t free_cap,
+                           const int32_t *n_free, int32_t M, int32_t *seq_len_out, int32_t *n_free_out, int32_t *cu_rows, int32_t *admitted,
+                           int32_t *place, int32_t *pos, int32_t *slot);
+
+/* Request b keeps its first keep[b] tokens (seq_len_out[b] = min(max(keep[b], 0), seq_len[b]): rejected drafts, or all of an ended request);
+ * the pages behind them go to free_pages[*n_free ..), in order of requests and pages: those of request b to place[b] .. place[b + 1] - 1.
+ * The table stays as it is.  free_pages holds free_cap pages; what would lie behind them is dropped.
+ * seq_len_out may be seq_len or keep, n_free_out may be n_free; nothing else may overlap. */
+pvf_status pvf_page_trim(void *stream, const int32_t *seq_len, const int32_t *keep, int32_t B, const int32_t *table, int32_t width,
+                         int64_t table_stride, int32_t page_size, int32_t *free_pages, int32_t free_cap, const int32_t *n_free,
+                         int32_t *seq_len_out, int32_t *n_free_out, int32_t *place);
+
+/* Fresh rows enter the cache: qkv [M, (H + 2 Hkv) * d_head] (q | k | v, rows qkv_stride apart) holds the projections of rows at positions pos [M];
+ * q_out [M, H * d_head] (rows q_stride apart) = rotated q, and slot[m] of the caches = rotated k and v of row m.  Rotary embedding as in pvf_model_cfg, its
+ * angles in float64, at any position.  A row whose slot lies outside the cache is padding: nothing is written for it.  Slots of a call have to differ
+ * (of rows with one slot, any one's elements may stay).  q_out may be the q part of qkv itself. */
+pvf_status pvf_page_store(void *stream, int32_t dtype, const void *qkv, int64_t qkv_stride, const int32_t *pos, const int32_t *slot, int32_t M,
+                          int32_t H, int32_t Hkv, int32_t d_head, float rope_theta, void *q_out, int64_t q_stride, void *k_cache, void *v_cache,
+                          int32_t n_pages, int32_t page_size, int64_t k_page_stride, int64_t v_page_stride);
+
+/* out[m] = softmax(scale * q[m] k^T) v over the tokens of row m's request: q and out [M, H * d_head] (rows q_stride and out_stride apart), heads
+ * h * H / Hkv .. of the rows share key head h.  Rows cu_rows[b] .. cu_rows[b + 1] - 1 belong to request b (cu_rows NULL: one row each, M = B); rows outside of
+ * all stay as they are.  A row sees all seq_len[b] tokens (causal = 0), or with causal = 1 those up to its own place, the rows of a request being its
+ * last tokens: seq_len[b] - n_rows + i + 1 for row i.  A row that sees no token is zeros; what lies behind the tokens a row sees has no part in it, whatever it
+ * is.  A row that sees a token whose page is outside the cache or whose request is longer than its table is NaN.
+ * Scores, statistics and sums are float32 (probabilities enter the bf16 matrix instruction in two parts, 16 bits), rounded once at the end; the order of
+ * sums goes by the lengths of all requests in the call, so last bits may differ between batches, not between calls.
+ * Long caches are divided over the chip and joined by a second launch: workspace of pvf_page_attention_workspace bytes (0 where nothing is divided;
+ * PVF_PAGE_WORKSPACE suffices for every call; a negative status where the sizes are refused).  Calls that overlap need workspaces of their own. */
+#define PVF_PAGE_WORKSPACE ((int64_t)1 << 26)
+int64_t pvf_page_attention_workspace(int32_t dtype, int32_t B, int32_t M, int32_t H, int32_t Hkv, int32_t d_head, int32_t width, int32_t page_size);
+pvf_status pvf_page_attention(void *stream, int32_t dtype, const void *q, int64_t q_stride, const void *k_cache, const void *v_cache,
+                              int32_t n_pages, int32_t page_size, int64_t k_page_stride, int64_t v_page_stride, const int32_t *table,
+                              int32_t width, int64_t table_stride, const int32_t *seq_len, const int32_t *cu_rows, int32_t B, int32_t M,
+                              int32_t H, int32_t Hkv, int32_t d_head, int32_t causal, float scale, void *out, int64_t out_stride,
+                              void *workspace, int64_t workspace_bytes);
+
 /* In-place rotary embedding of the q and k thirds of qkv [S*T, 3*d] (row m is canvas
  * position m % T), then out[S*T, d] = softmax(q k^T / sqrt(d_head)) v per canvas and head,
  * over all T keys.

@@ -22,6 +22,7 @@ MX_GEMM, MX_SWIGLU, MX_W4 = 0, 1, 2   # PVF_MX_CALL_*
 PVF_ROUTES_PLAN, PVF_ROUTES_AR, PVF_ROUTES_CAL, PVF_ROUTES_XRANDOM, PVF_ROUTES_XPLANNING = 1, 2, 4, 8, 16
 PVF_ROUTE_NONE, PVF_ROUTE_PLAN, PVF_ROUTE_AR, PVF_ROUTE_CAL = 0, 1, 2, 3
 ROUTE_NONE, ROUTE_PLAN, ROUTE_AR = 0, 1, 2
+PAGE_WORKSPACE = 1 << 26   # PVF_PAGE_WORKSPACE
 MAX_K = 32          # PVF_MAX_K of include/pvf.h
 STATUS = {0: "PVF_OK", -1: "PVF_EINVAL", -2: "PVF_ESHAPE", -3: "PVF_ENOMEM", -4: "PVF_EHIP",
           -5: "PVF_ENOTIMPL"}
@@ -33,7 +34,8 @@ EXPORTS = ["pvf_create", "pvf_destroy", "pvf_last_error", "pvf_workspace_bytes",
            "pvf_gemm_swiglu", "pvf_rmsnorm", "pvf_rope_attention", "pvf_fill_normal", "pvf_entropy",
            "pvf_plan_vocab_select", "pvf_qkv_attention", "pvf_rope_attention_noalloc", "pvf_round_sync", "pvf_ctx_gemm",
            "pvf_ctx_gemm_swiglu", "pvf_quant_mx", "pvf_add_rmsnorm_mx", "pvf_gemm_mx", "pvf_gemm_mx_swiglu", "pvf_gemm_w4",
-           "pvf_gemm_mx_instance"]
+           "pvf_gemm_mx_instance", "pvf_page_extend", "pvf_page_trim", "pvf_page_store", "pvf_page_attention_workspace",
+           "pvf_page_attention"]
 
 
 class PvfError(RuntimeError):
@@ -150,11 +152,18 @@ def lib() -> C.CDLL:
         L.pvf_gemm_w4.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                   C.c_int32, C.c_int32, C.c_int32]
         L.pvf_gemm_mx_instance.argtypes = [C.c_int32] * 7 + [C.POINTER(C.c_int32)] * 2
+        p, i, i64, f = C.c_void_p, C.c_int32, C.c_int64, C.c_float
+        L.pvf_page_extend.argtypes = [p, p, p, p, i, p, i, i64, i, p, i, p, i] + [p] * 7
+        L.pvf_page_trim.argtypes = [p, p, p, i, p, i, i64, i, p, i, p, p, p, p]
+        L.pvf_page_store.argtypes = [p, i, p, i64, p, p, i, i, i, i, f, p, i64, p, p, i, i, i64, i64]
+        L.pvf_page_attention_workspace.argtypes = [i] * 8
+        L.pvf_page_attention_workspace.restype = i64
+        L.pvf_page_attention.argtypes = [p, i, p, i64, p, p, i, i, i64, i64, p, i, i64, p, p, i, i, i, i, i, i, f, p, i64, p, i64]
         L.pvf_fill_normal.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_uint64,
                                       C.c_float, C.c_float]
         for name in EXPORTS:
             fn = getattr(L, name)
-            if name not in ("pvf_last_error", "pvf_workspace_bytes", "pvf_destroy"):
+            if name not in ("pvf_last_error", "pvf_workspace_bytes", "pvf_destroy", "pvf_page_attention_workspace"):
                 fn.restype = C.c_int32
         _lib = L
     return _lib
@@ -554,6 +563,149 @@ def gemm_mx_instance(call: int, M: int, N: int, K: int, w_fmt: int = MX_E4M3, dt
     index, count = C.c_int32(), C.c_int32()
     _check(lib().pvf_gemm_mx_instance(call, w_fmt, _dtype_code(dtype), int(aligned), M, N, K, C.byref(index), C.byref(count)))
     return index.value, count.value
+
+
+# ---- keys and values in pages --------------------------------------------------------------
+# A cache is a pair of tensors [n_pages, Hkv, page_size, d_head], pages contiguous but for the distance between them (stride(0)); a table is
+# int32 [B, width]; lengths, counts, positions and slots are int32.
+def _page_call(fn, dev: int, *args) -> None:
+    """fn(stream, *args) on device dev."""
+    if dev < 0:
+        raise AssertionError("device-resident tensors required")
+    if dev != torch._C._cuda_getDevice():
+        with torch.cuda.device(dev):
+            status = fn(torch._C._cuda_getCurrentRawStream(dev), *args)
+    else:
+        status = fn(torch._C._cuda_getCurrentRawStream(dev), *args)
+    if status:
+        _check(status)
+
+
+def _i32(dev: int, n: int, *tensors) -> None:
+    """Contiguous int32 tensors of n elements on device dev."""
+    for t in tensors:
+        assert t.dtype is torch.int32 and t.numel() == n and t.is_contiguous() and t.get_device() == dev, \
+            f"int32 [{n}] on device {dev} required: {t.dtype} {tuple(t.shape)} on {t.device}"
+
+
+def _table(table: torch.Tensor, dev: int, B: int):
+    """(width, distance of rows) of a checked table."""
+    assert table.dtype is torch.int32 and table.dim() == 2 and table.shape[0] == B and table.get_device() == dev, "the table is int32 [B, width] beside the lengths"
+    width = table.shape[1]
+    assert width <= 1 or table.stride(1) == 1, "rows of the table are contiguous"
+    return width, max(table.stride(0), width) if B > 1 else width
+
+
+def _cache(k: torch.Tensor, v: torch.Tensor, dtype: torch.dtype, dev: int):
+    """(n_pages, Hkv, page_size, d_head) of checked caches."""
+    shape = k.shape
+    assert len(shape) == 4 and v.shape == shape and k.dtype is dtype and v.dtype is dtype and k.get_device() == dev and v.get_device() == dev, \
+        "caches are [n_pages, Hkv, page_size, d_head] of the rows' type, beside them"
+    _, Hkv, P, dh = shape
+    for c in (k, v):
+        s = c.stride()
+        assert (dh == 1 or s[3] == 1) and (P == 1 or s[2] == dh) and (Hkv == 1 or s[1] == P * dh), "what is in a page is contiguous"
+    return shape
+
+
+def page_extend(seq_len: torch.Tensor, n_rows: torch.Tensor, table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor, page_size: int,
+                start: Optional[torch.Tensor] = None, rows: Optional[int] = None, out=None):
+    """Pages for the n_rows[b] rows that each request computes next, at positions start[b] .. (None: behind its seq_len[b] tokens); table is written.
+    Returns (seq_len, n_free, cu_rows [B + 1], admitted [B], place [B + 1], pos [rows], slot [rows]), or writes them into `out`, such a tuple;
+    `rows` counts the rows in all and is needed without `out`.  seq_len and n_free of `out` may be the inputs themselves."""
+    dev, B = seq_len.get_device(), seq_len.numel()
+    if out is None:
+        assert rows is not None, "rows, or out, is needed"
+        new = lambda n: torch.empty(n, dtype=torch.int32, device=seq_len.device)  # noqa: E731
+        out = (new(B), new(1), new(B + 1), new(B), new(B + 1), new(rows), new(rows))
+    len_out, free_out, cu, admitted, place, pos, slot = out
+    M = pos.numel()
+    assert rows is None or rows == M, "rows of `out`"
+    _i32(dev, B, seq_len, n_rows, len_out, admitted)
+    _i32(dev, B + 1, cu, place)
+    _i32(dev, M, pos, slot)
+    _i32(dev, 1, n_free, free_out)
+    _i32(dev, free_pages.numel(), free_pages)
+    if start is not None:
+        _i32(dev, B, start)
+    width, stride = _table(table, dev, B)
+    _page_call(lib().pvf_page_extend, dev, seq_len.data_ptr(), _p(start), n_rows.data_ptr(), B, table.data_ptr(), width, stride, page_size, free_pages.data_ptr(),
+               free_pages.numel(), n_free.data_ptr(), M, len_out.data_ptr(), free_out.data_ptr(), cu.data_ptr(), admitted.data_ptr(), place.data_ptr(),
+               pos.data_ptr(), slot.data_ptr())
+    return out
+
+
+def page_trim(seq_len: torch.Tensor, keep: torch.Tensor, table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor, page_size: int, out=None):
+    """Pages behind the first keep[b] tokens of each request go back to free_pages, which is written.  Returns (seq_len, n_free, place [B + 1]), or
+    writes them into `out`; seq_len (also keep) and n_free of `out` may be the inputs themselves."""
+    dev, B = seq_len.get_device(), seq_len.numel()
+    if out is None:
+        new = lambda n: torch.empty(n, dtype=torch.int32, device=seq_len.device)  # noqa: E731
+        out = (new(B), new(1), new(B + 1))
+    len_out, free_out, place = out
+    _i32(dev, B, seq_len, keep, len_out)
+    _i32(dev, B + 1, place)
+    _i32(dev, 1, n_free, free_out)
+    _i32(dev, free_pages.numel(), free_pages)
+    width, stride = _table(table, dev, B)
+    _page_call(lib().pvf_page_trim, dev, seq_len.data_ptr(), keep.data_ptr(), B, table.data_ptr(), width, stride, page_size, free_pages.data_ptr(),
+               free_pages.numel(), n_free.data_ptr(), len_out.data_ptr(), free_out.data_ptr(), place.data_ptr())
+    return out
+
+
+def page_store(qkv: torch.Tensor, pos: torch.Tensor, slot: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, rope_theta: float,
+               q_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Rotated q [M, H, d_head] of qkv [M, (H + 2 Hkv) * d_head] (rows may lie apart), whose rotated keys and values go to their slots; H follows from the
+    caches.  q_out may be strided by rows, also the q part of qkv itself."""
+    dev, (M, wide) = qkv.get_device(), qkv.shape
+    n_pages, Hkv, P, dh = _cache(k_cache, v_cache, qkv.dtype, dev)
+    H = wide // dh - 2 * Hkv
+    assert H >= 0 and wide == (H + 2 * Hkv) * dh and (wide == 1 or qkv.stride(1) == 1), "rows are q | k | v of whole heads"
+    _i32(dev, M, pos, slot)
+    if q_out is None:
+        q_out = torch.empty(M, H, dh, dtype=qkv.dtype, device=qkv.device)
+    assert q_out.shape == (M, H, dh) and q_out.dtype is qkv.dtype and q_out.get_device() == dev and (dh == 1 or q_out.stride(2) == 1) and \
+        (H <= 1 or q_out.stride(1) == dh), "q_out is [M, H, d_head] of qkv's type, heads contiguous"
+    _page_call(lib().pvf_page_store, dev, _dtype_code(qkv.dtype), qkv.data_ptr(), qkv.stride(0) if M > 1 else 0, pos.data_ptr(), slot.data_ptr(), M, H, Hkv, dh,
+               rope_theta, q_out.data_ptr(), q_out.stride(0) if M > 1 else 0, k_cache.data_ptr(), v_cache.data_ptr(), n_pages, P,
+               k_cache.stride(0) if n_pages > 1 else 0, v_cache.stride(0) if n_pages > 1 else 0)
+    return q_out
+
+
+def page_attention_workspace(q: torch.Tensor, k_cache: torch.Tensor, table: torch.Tensor) -> int:
+    """Bytes of workspace that page_attention wants for such tensors (PAGE_WORKSPACE suffices for any)."""
+    M, H, dh = q.shape
+    n = lib().pvf_page_attention_workspace(_dtype_code(q.dtype), table.shape[0], M, H, k_cache.shape[1], dh, table.shape[1], k_cache.shape[2])
+    if n < 0:
+        _check(n)
+    return n
+
+
+def page_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, seq_len: torch.Tensor,
+                   cu_rows: Optional[torch.Tensor] = None, causal: bool = False, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """softmax(scale * q k^T) v of rows q [M, H, d_head] against the seq_len[b] tokens of their request: rows cu_rows[b] .. cu_rows[b + 1] - 1 are request b's
+    (None: one row each).  causal: a request's rows are its last tokens and see no later ones.  scale: d_head^-0.5 by default.  q and out may be strided
+    by rows.  workspace: uint8, for callers who keep one (PAGE_WORKSPACE bytes); calls that overlap need one each."""
+    dev, (M, H, dh), B = q.get_device(), q.shape, seq_len.numel()
+    n_pages, Hkv, P, cdh = _cache(k_cache, v_cache, q.dtype, dev)
+    assert cdh == dh and (dh == 1 or q.stride(2) == 1) and (H <= 1 or q.stride(1) == dh), "q is [M, H, d_head], heads contiguous, d_head the caches'"
+    if out is None:
+        out = torch.empty(M, H, dh, dtype=q.dtype, device=q.device)
+    assert out.shape == (M, H, dh) and out.dtype is q.dtype and out.get_device() == dev and (dh == 1 or out.stride(2) == 1) and (H <= 1 or out.stride(1) == dh), \
+        "out is like q"
+    _i32(dev, B, seq_len)
+    if cu_rows is not None:
+        _i32(dev, B + 1, cu_rows)
+    width, stride = _table(table, dev, B)
+    if workspace is None:
+        workspace = torch.empty(page_attention_workspace(q, k_cache, table), dtype=torch.uint8, device=q.device)
+    assert workspace.dtype is torch.uint8 and workspace.is_contiguous() and workspace.get_device() == dev, "the workspace is uint8, beside q"
+    _page_call(lib().pvf_page_attention, dev, _dtype_code(q.dtype), q.data_ptr(), q.stride(0) if M > 1 else 0, k_cache.data_ptr(), v_cache.data_ptr(), n_pages, P,
+               k_cache.stride(0) if n_pages > 1 else 0, v_cache.stride(0) if n_pages > 1 else 0, table.data_ptr(), width, stride, seq_len.data_ptr(),
+               _p(cu_rows), B, M, H, Hkv, dh, int(causal), dh ** -0.5 if scale is None else scale, out.data_ptr(), out.stride(0) if M > 1 else 0,
+               workspace.data_ptr(), workspace.numel())
+    return out
 
 
 def rope_attention(qkv: torch.Tensor, S: int, T: int, n_heads: int, d_head: int,

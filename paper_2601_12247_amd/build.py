@@ -24,6 +24,8 @@ SOURCES = [
     "gemm_mfma.hip",
     "gemm_mx.hip",
     "mx_rows.hip",
+    "pages.hip",
+    "paged_attention.hip",
     "attention_simple.hip",
     "attention_f32.hip",
     "attention_mfma.hip",

@@ -2,6 +2,7 @@
 // one PVF round (Algorithm 1 with one batched forward per round) and of the decode loop.
 #include "common.h"
 #include "mx.h"
+#include "paged.h"
 
 #include <chrono>
 #include <cmath>
@@ -1143,6 +1144,133 @@ extern "C" pvf_status pvf_gemm_mx_instance(int32_t call, int32_t w_fmt, int32_t 
   *index = chosen.index;
   *count = chosen.count;
   return PVF_OK;
+}
+
+// ---- keys and values in pages --------------------------------------------------------------------
+static bool at_16(const void *p) { return (uintptr_t)p % 16 == 0; }
+static bool at_4(const void *p) { return (uintptr_t)p % 4 == 0; }
+
+static pvf_status check_pages(const char *call, int32_t B, int32_t width, int64_t table_stride, int32_t page_size) {
+  PVF_REQUIRE(nullptr, B >= 0 && width >= 0 && page_size > 0, PVF_EINVAL, "%s: bad size (B=%d, width=%d, page_size=%d)", call, B, width, page_size);
+  PVF_REQUIRE(nullptr, B <= 1 << 20 && (int64_t)width * page_size <= 1 << 30, PVF_ESHAPE, "%s: %d requests of %d pages of %d: at most 2^20 requests of 2^30 tokens",
+              call, B, width, page_size);
+  PVF_REQUIRE(nullptr, table_stride >= width && table_stride <= INT32_MAX, PVF_EINVAL, "%s: rows of the table are %lld apart and %d wide", call,
+              (long long)table_stride, width);
+  return PVF_OK;
+}
+
+extern "C" pvf_status pvf_page_extend(void *stream, const int32_t *seq_len, const int32_t *start, const int32_t *n_rows, int32_t B, int32_t *table,
+                                      int32_t width, int64_t table_stride, int32_t page_size, const int32_t *free_pages, int32_t free_cap,
+                                      const int32_t *n_free, int32_t M, int32_t *seq_len_out, int32_t *n_free_out, int32_t *cu_rows, int32_t *admitted,
+                                      int32_t *place, int32_t *pos, int32_t *slot) {
+  if (const pvf_status st = check_pages("pvf_page_extend", B, width, table_stride, page_size)) return st;
+  PVF_REQUIRE(nullptr, M >= 0 && free_cap >= 0, PVF_EINVAL, "pvf_page_extend: bad size (M=%d, free_cap=%d)", M, free_cap);
+  PVF_REQUIRE(nullptr, M <= 1 << 24, PVF_ESHAPE, "pvf_page_extend: M=%d beyond 2^24", M);
+  PVF_REQUIRE(nullptr, n_free && n_free_out && cu_rows && place && (B == 0 || (seq_len && n_rows && seq_len_out && admitted)) &&
+              (B == 0 || width == 0 || table) && (free_cap == 0 || free_pages) && (M == 0 || (pos && slot)), PVF_EINVAL, "pvf_page_extend: a tensor is NULL");
+  const void *all[] = {seq_len, start, n_rows, table, free_pages, n_free, seq_len_out, n_free_out, cu_rows, admitted, place, pos, slot};
+  for (const void *p : all) PVF_REQUIRE(nullptr, at_4(p), PVF_EINVAL, "pvf_page_extend: a tensor begins between elements");
+  PageExtend a;
+  a.seq_len = seq_len; a.start = start; a.n_rows = n_rows; a.n_free = n_free; a.free_pages = free_pages; a.table = table;
+  a.B = B; a.M = M; a.width = width; a.table_stride = (int32_t)table_stride; a.page_size = page_size; a.free_cap = free_cap;
+  a.seq_len_out = seq_len_out; a.n_free_out = n_free_out; a.cu_rows = cu_rows; a.admitted = admitted; a.place = place; a.pos = pos; a.slot = slot;
+  return launch_page_extend((hipStream_t)stream, a);
+}
+
+extern "C" pvf_status pvf_page_trim(void *stream, const int32_t *seq_len, const int32_t *keep, int32_t B, const int32_t *table, int32_t width,
+                                    int64_t table_stride, int32_t page_size, int32_t *free_pages, int32_t free_cap, const int32_t *n_free,
+                                    int32_t *seq_len_out, int32_t *n_free_out, int32_t *place) {
+  if (const pvf_status st = check_pages("pvf_page_trim", B, width, table_stride, page_size)) return st;
+  PVF_REQUIRE(nullptr, free_cap >= 0, PVF_EINVAL, "pvf_page_trim: free_cap=%d", free_cap);
+  PVF_REQUIRE(nullptr, n_free && n_free_out && place && (B == 0 || (seq_len && keep && seq_len_out)) && (B == 0 || width == 0 || table) &&
+              (free_cap == 0 || free_pages), PVF_EINVAL, "pvf_page_trim: a tensor is NULL");
+  const void *all[] = {seq_len, keep, table, free_pages, n_free, seq_len_out, n_free_out, place};
+  for (const void *p : all) PVF_REQUIRE(nullptr, at_4(p), PVF_EINVAL, "pvf_page_trim: a tensor begins between elements");
+  PageTrim a;
+  a.seq_len = seq_len; a.keep = keep; a.table = table; a.n_free = n_free; a.free_pages = free_pages;
+  a.B = B; a.width = width; a.table_stride = (int32_t)table_stride; a.page_size = page_size; a.free_cap = free_cap;
+  a.seq_len_out = seq_len_out; a.n_free_out = n_free_out; a.place = place;
+  return launch_page_trim((hipStream_t)stream, a);
+}
+
+// what a paged cache and rows against it have to be
+static pvf_status check_cache(const char *call, int32_t dtype, int32_t M, int32_t H, int32_t Hkv, int32_t dh, int32_t n_pages, int32_t page_size,
+                              const void *k_cache, const void *v_cache, int64_t k_page_stride, int64_t v_page_stride) {
+  const int per_16 = dtype == PVF_F32 ? 4 : 8;
+  PVF_REQUIRE(nullptr, M >= 0 && H >= 0 && Hkv > 0 && dh > 0 && n_pages >= 0 && page_size > 0, PVF_EINVAL, "%s: bad size (M=%d, H=%d, Hkv=%d, d_head=%d, n_pages=%d, page_size=%d)",
+              call, M, H, Hkv, dh, n_pages, page_size);
+  PVF_REQUIRE(nullptr, dh % 8 == 0 && dh <= 256 && page_size % 8 == 0 && page_size <= 1 << 16, PVF_ENOTIMPL,
+              "%s: d_head=%d, page_size=%d: multiples of 8, up to 256 and 65536", call, dh, page_size);
+  PVF_REQUIRE(nullptr, M <= 1 << 24 && H <= 1 << 12 && Hkv <= 1 << 12 && (int64_t)M * H <= 1 << 30, PVF_ESHAPE, "%s: %d rows of %d and %d heads: at most 2^24 rows, 2^12 heads, 2^30 of both",
+              call, M, H, Hkv);
+  PVF_REQUIRE(nullptr, (int64_t)n_pages * page_size <= INT32_MAX, PVF_ESHAPE, "%s: %d pages of %d tokens: slots are 31 bits", call, n_pages, page_size);
+  PVF_REQUIRE(nullptr, n_pages == 0 || (k_cache && v_cache && at_16(k_cache) && at_16(v_cache)), PVF_EINVAL, "%s: a cache is NULL or begins between 16 bytes", call);
+  const int64_t page = (int64_t)Hkv * page_size * dh;
+  PVF_REQUIRE(nullptr, k_page_stride % per_16 == 0 && v_page_stride % per_16 == 0 && (n_pages <= 1 || (k_page_stride >= page && v_page_stride >= page)),
+              PVF_EINVAL, "%s: pages of %lld elements are %lld and %lld apart", call, (long long)page, (long long)k_page_stride, (long long)v_page_stride);
+  return PVF_OK;
+}
+
+extern "C" pvf_status pvf_page_store(void *stream, int32_t dtype, const void *qkv, int64_t qkv_stride, const int32_t *pos, const int32_t *slot, int32_t M,
+                                     int32_t H, int32_t Hkv, int32_t d_head, float rope_theta, void *q_out, int64_t q_stride, void *k_cache, void *v_cache,
+                                     int32_t n_pages, int32_t page_size, int64_t k_page_stride, int64_t v_page_stride) {
+  if (check_dtype(dtype) != PVF_OK) return PVF_EINVAL;
+  if (const pvf_status st = check_cache("pvf_page_store", dtype, M, H, Hkv, d_head, n_pages, page_size, k_cache, v_cache, k_page_stride, v_page_stride)) return st;
+  PVF_REQUIRE(nullptr, rope_theta > 0.f && rope_theta < INFINITY, PVF_EINVAL, "pvf_page_store: rope_theta=%g", rope_theta);
+  if (M == 0) return PVF_OK;
+  const int per_16 = dtype == PVF_F32 ? 4 : 8;
+  PVF_REQUIRE(nullptr, qkv && pos && slot && (H == 0 || q_out) && at_16(qkv) && at_16(q_out) && at_4(pos) && at_4(slot), PVF_EINVAL,
+              "pvf_page_store: a tensor is NULL, rows begin between 16 bytes or positions between elements");
+  PVF_REQUIRE(nullptr, qkv_stride % per_16 == 0 && q_stride % per_16 == 0 && (M == 1 || (qkv_stride >= (int64_t)(H + 2 * Hkv) * d_head && (H == 0 || q_stride >= (int64_t)H * d_head))),
+              PVF_EINVAL, "pvf_page_store: rows are %lld and %lld elements apart", (long long)qkv_stride, (long long)q_stride);
+  PageStore a;
+  a.qkv = qkv; a.pos = pos; a.slot = slot; a.q_out = q_out; a.k_cache = k_cache; a.v_cache = v_cache;
+  a.qkv_stride = qkv_stride; a.q_stride = q_stride; a.k_page_stride = k_page_stride; a.v_page_stride = v_page_stride;
+  a.M = M; a.H = H; a.Hkv = Hkv; a.dh = d_head; a.n_pages = n_pages; a.page_size = page_size;
+  a.log2_theta = std::log2((double)rope_theta);
+  return launch_page_store((hipStream_t)stream, dtype, a);
+}
+
+// the checks that pvf_page_attention and its workspace share
+static pvf_status check_attention(const char *call, int32_t B, int32_t M, int32_t H, int32_t Hkv, int32_t width, int64_t table_stride, int32_t page_size) {
+  if (const pvf_status st = check_pages(call, B, width, table_stride, page_size)) return st;
+  PVF_REQUIRE(nullptr, H > 0 && H % Hkv == 0, PVF_EINVAL, "%s: %d heads share %d key heads", call, H, Hkv);
+  return PVF_OK;
+}
+
+extern "C" int64_t pvf_page_attention_workspace(int32_t dtype, int32_t B, int32_t M, int32_t H, int32_t Hkv, int32_t d_head, int32_t width, int32_t page_size) {
+  if (check_dtype(dtype) != PVF_OK) return PVF_EINVAL;
+  if (const pvf_status st = check_cache("pvf_page_attention_workspace", dtype, M, H, Hkv, d_head, 0, page_size, nullptr, nullptr, 0, 0)) return st;
+  if (const pvf_status st = check_attention("pvf_page_attention_workspace", B, M, H, Hkv, width, width, page_size)) return st;
+  return B == 0 || M == 0 ? 0 : page_attention_workspace(dtype, B, M, H, Hkv, d_head, width, page_size);
+}
+
+extern "C" pvf_status pvf_page_attention(void *stream, int32_t dtype, const void *q, int64_t q_stride, const void *k_cache, const void *v_cache,
+                                         int32_t n_pages, int32_t page_size, int64_t k_page_stride, int64_t v_page_stride, const int32_t *table,
+                                         int32_t width, int64_t table_stride, const int32_t *seq_len, const int32_t *cu_rows, int32_t B, int32_t M,
+                                         int32_t H, int32_t Hkv, int32_t d_head, int32_t causal, float scale, void *out, int64_t out_stride,
+                                         void *workspace, int64_t workspace_bytes) {
+  if (check_dtype(dtype) != PVF_OK) return PVF_EINVAL;
+  if (const pvf_status st = check_cache("pvf_page_attention", dtype, M, H, Hkv, d_head, n_pages, page_size, k_cache, v_cache, k_page_stride, v_page_stride)) return st;
+  if (const pvf_status st = check_attention("pvf_page_attention", B, M, H, Hkv, width, table_stride, page_size)) return st;
+  PVF_REQUIRE(nullptr, (causal == 0 || causal == 1) && std::isfinite(scale), PVF_EINVAL, "pvf_page_attention: causal=%d, scale=%g", causal, scale);
+  PVF_REQUIRE(nullptr, cu_rows || B == M, PVF_EINVAL, "pvf_page_attention: without cu_rows there is one row a request, not %d of %d", M, B);
+  if (M == 0 || B == 0) return PVF_OK;
+  const int per_16 = dtype == PVF_F32 ? 4 : 8;
+  PVF_REQUIRE(nullptr, n_pages > 0, PVF_EINVAL, "pvf_page_attention: a cache without pages");
+  PVF_REQUIRE(nullptr, q && out && seq_len && (table || width == 0) && at_16(q) && at_16(out) && at_4(table) && at_4(seq_len) && at_4(cu_rows), PVF_EINVAL,
+              "pvf_page_attention: a tensor is NULL, rows begin between 16 bytes or tables between elements");
+  PVF_REQUIRE(nullptr, q_stride % per_16 == 0 && out_stride % per_16 == 0 && (M == 1 || (q_stride >= (int64_t)H * d_head && out_stride >= (int64_t)H * d_head)),
+              PVF_EINVAL, "pvf_page_attention: rows are %lld and %lld elements apart", (long long)q_stride, (long long)out_stride);
+  const int64_t need = page_attention_workspace(dtype, B, M, H, Hkv, d_head, width, page_size);
+  PVF_REQUIRE(nullptr, need == 0 || (workspace && at_16(workspace) && workspace_bytes >= need), PVF_ESHAPE,
+              "pvf_page_attention: %lld bytes of workspace at a multiple of 16 wanted, %lld given", (long long)need, (long long)(workspace ? workspace_bytes : 0));
+  PageAttention a;
+  a.q = q; a.k_cache = k_cache; a.v_cache = v_cache; a.table = table; a.seq_len = seq_len; a.cu_rows = cu_rows; a.out = out; a.ws = (float *)workspace;
+  a.q_stride = q_stride; a.out_stride = out_stride; a.k_page_stride = k_page_stride; a.v_page_stride = v_page_stride;
+  a.B = B; a.M = M; a.H = H; a.Hkv = Hkv; a.dh = d_head; a.n_pages = n_pages; a.page_size = page_size; a.width = width;
+  a.table_stride = (int32_t)table_stride; a.causal = causal; a.scale = scale;
+  return launch_page_attention((hipStream_t)stream, dtype, a);
 }
 
 // Builds the rotary table on the host for this call, so it synchronises the stream and
