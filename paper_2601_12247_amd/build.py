@@ -26,6 +26,7 @@ SOURCES = [
     "mx_rows.hip",
     "pages.hip",
     "paged_attention.hip",
+    "paged_attention_wide.hip",
     "attention_simple.hip",
     "attention_f32.hip",
     "attention_mfma.hip",

@@ -1,0 +1,319 @@
+// Attention over pages for many rows a request (paged_attention.h): bf16, more than 32 (row, head) pairs a key head.
+//
+// One workgroup = 128 columns of one (request, key head), 32 a wave, or 64, with the waves in two pairs that take alternate halves of the keys.
+// 64 keys and their values at a time go from the pages into LDS (no detour over registers), one buffer ahead; S^T = K Q^T and O^T = V^T P^T on
+// 32 x 32 x 16 matrix instructions.  A lane of S^T holds one column and keys 8 (e / 4) + 4 (lane / 32) + e % 4; P^T is multiplied as it is held, with V^T's
+// keys in that order: transposing reads give a lane four keys of one dimension.
+//
+// LDS rows are keys, in 16-byte chunks; chunk x of a key lies at x ^ turn(key), so that 16 keys' equal chunks (the operand K) and 8 keys' neighbouring
+// ones (V^T) fall on all banks.
+#include "paged_attention.h"
+
+namespace pvf {
+namespace page {
+namespace {
+
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(1))) const void gptr_t;
+typedef __attribute__((address_space(3))) void lptr_t;
+typedef __attribute__((address_space(3))) short4v *trptr_t;
+
+// CW: waves beside each other over columns; the 4 / CW groups of them share out the keys of a step.
+template <int DH, int CW>
+struct WideInst {
+  static constexpr int kDh = DH, QT = 32 * CW, KW = 4 / CW, kStep = 64, kSubs = 2 / KW, kSnap = 4, kWholeSteps = 16, kPerCu = 2;
+  static constexpr int NT = DH / 32, KJ = DH / 16;
+  static constexpr int kRow = DH * 2, kChunks = DH / 8, kTile = kStep * kRow;   // bytes of a key, its chunks, bytes of 64 keys
+  static constexpr int kLoads = kTile / 4096;                                 // loads of 1 KB a wave and tile
+  static constexpr int kSlotFloats = QT * (DH + 2);
+  static_assert(CW * KW == 4 && kSubs * KW == 2, "four waves, two groups of 32 keys");
+};
+
+template <int DH, int CW, bool kWhole>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
+page_attention_wide_kernel(Args a) {
+  typedef WideInst<DH, CW> I;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * I::kTile];   // keys, values; twice
+  __shared__ int32_t s_pages[kPageSlots];
+  const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int cw = wid % CW, kw = wid / CW, fr = lane & 31, fh = lane >> 5;
+  int worker;
+  Place w = place_of<I>(a, blockIdx.x, gridDim.x, &worker);
+  if (!a.whole && tid == 0) a.joins[(int64_t)worker * kJoinInts] = 0;
+  if (w.at >= w.end) return;
+  Request r = request<I>(a, w.b);
+  Piece piece;
+
+  auto turn = [](int key) { return I::kChunks == 16 ? (key & 3) << 2 | (key >> 2 & 3) : (key >> 1 & 1) << 2 | (key >> 2 & 3); };
+  // operand K: key fr of 32, chunk 2 j + fh.  Operand V^T: of 16 lanes, lane 4 k + x reads dimensions 4 x .. of key k; keys 4 fh .. (and 8 behind
+  // them), dimensions 32 t + 16 (lane / 16 % 2) + ..
+  int k_rd[I::KJ], v_rd[I::NT][2];
+#pragma unroll
+  for (int j = 0; j < I::KJ; ++j) k_rd[j] = fr * I::kRow + (((2 * j + fh) ^ turn(fr)) << 4);
+#pragma unroll
+  for (int t = 0; t < I::NT; ++t)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int s = lane & 15, key = 8 * e + 4 * fh + s / 4, dim = 32 * t + 16 * (lane >> 4 & 1) + 4 * (s & 3);
+      v_rd[t][e] = key * I::kRow + ((dim / 8 ^ turn(key)) << 4) + dim % 8 * 2;
+    }
+
+  while (next_piece<I>(a, w, r, piece)) {
+    const int cols = piece.cols, len = r.len, col = 32 * cw + fr;
+    const bf16_t *kbase = (const bf16_t *)a.p.k_cache + (int64_t)piece.head * a.p.page_size * a.p.dh;
+    const bf16_t *vbase = (const bf16_t *)a.p.v_cache + (int64_t)piece.head * a.p.page_size * a.p.dh;
+    int row;
+    const int64_t q_at = row_place(a, r.row0, piece.head, (int64_t)piece.tile * I::QT + col, a.p.q_stride, &row);
+    const int limit = col < cols ? limit_of(a, len, r.n, row) : INT32_MAX;
+    const int least = limit_of(a, len, r.n, (int)((int64_t)piece.tile * I::QT / a.group));      // of the tile's columns: the first row's
+    bf16x8 q[I::KJ];
+#pragma unroll
+    for (int j = 0; j < I::KJ; ++j) {
+      uint4 x = make_uint4(0, 0, 0, 0);
+      if (col < cols && (kWhole || 16 * j + 8 * fh < a.p.dh)) x = *(const uint4 *)((const bf16_t *)a.p.q + q_at + 16 * j + 8 * fh);
+      q[j] = __builtin_bit_cast(bf16x8, make_uint4(x.x ^ a.q_xor, x.y ^ a.q_xor, x.z ^ a.q_xor, x.w ^ a.q_xor));
+    }
+    floatx16 o[I::NT];
+#pragma unroll
+    for (int t = 0; t < I::NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[t][e] = 0.f;
+    float m = -INFINITY, l = 0.f;
+    __syncthreads();                      // the last piece's results have been read
+    if (!kWhole) {                        // chunks behind d_head: nothing is loaded there, and q is zero beside them
+      for (int i = tid; i < 4 * I::kTile / 16; i += 256) *(uint4 *)(lds + 16 * i) = make_uint4(0, 0, 0, 0);
+    }
+
+    for (int s0 = piece.step0; s0 < piece.step1; s0 += a.chunk_steps) {
+      const int s1 = min(piece.step1, s0 + min(a.chunk_steps, piece.step1 - s0));
+      const int k0 = s0 * I::kStep, k1 = (int)min((int64_t)len, (int64_t)s1 * I::kStep);
+      __syncthreads();                    // the last chunk's pages and tiles have been read
+      const int first_page = page_of(a, k0);
+      const bool bad = __syncthreads_or(load_pages(a, w.b, k0, k1, first_page, s_pages)) != 0 || r.over;
+      if (k1 <= k0) continue;             // a request without keys
+
+      auto load = [&](int kb, int buf) {  // 64 keys from kb on and their values; the ones behind the last as copies of it
+        unsigned char *dst = lds + buf * 2 * I::kTile;
+#pragma unroll
+        for (int i = 0; i < I::kLoads; ++i) {
+          const int at = (i * 4 + wid) * 1024 + lane * 16, in = at / I::kRow, chunk = at / 16 % I::kChunks ^ turn(in);
+          const int key = min(kb + in, len - 1), page = page_of(a, key), id = max(s_pages[page - first_page], 0);
+          const int off = (key - page * a.p.page_size) * a.p.dh + chunk * 8;
+          if (kWhole || chunk * 8 < a.p.dh) {
+            __builtin_amdgcn_global_load_lds((gptr_t *)(kbase + (int64_t)id * a.p.k_page_stride + off), (lptr_t *)(dst + (i * 4 + wid) * 1024), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((gptr_t *)(vbase + (int64_t)id * a.p.v_page_stride + off), (lptr_t *)(dst + I::kTile + (i * 4 + wid) * 1024), 16, 0, 0);
+          }
+        }
+      };
+
+      auto step = [&](int kb, auto buf_c) {
+        constexpr int kBuf = decltype(buf_c)::value;
+        unsigned char *ks = lds + kBuf * 2 * I::kTile, *vs = ks + I::kTile;
+        __builtin_amdgcn_s_waitcnt(0x0f70);                    // vmcnt(0): this wave's part of the tile is there
+        __syncthreads();
+        if (kb < k1 - I::kStep) load(kb + I::kStep, kBuf ^ 1);
+        bool odd = false;
+        if (kb + I::kStep > least) {
+          // The tile holds keys that a row does not see, or copies of the last one.  0 times an infinity is no zero: values that are not finite
+          // leave it and are added to the columns that see them, by themselves.
+          bool mine = false;
+          for (int i = tid; i < I::kTile / 16; i += 256) {
+            uint4 x = *(uint4 *)(vs + 16 * i);
+            if (bf16s_not_finite(x.x) | bf16s_not_finite(x.y) | bf16s_not_finite(x.z) | bf16s_not_finite(x.w)) {
+              mine = true;
+              *(uint4 *)(vs + 16 * i) = make_uint4(bf16s_finite(x.x), bf16s_finite(x.y), bf16s_finite(x.z), bf16s_finite(x.w));
+            }
+          }
+          odd = __syncthreads_or(mine) != 0;
+        }
+        floatx16 s[I::kSubs];
+#pragma unroll
+        for (int u = 0; u < I::kSubs; ++u)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[u][e] = 0.f;
+#pragma unroll
+        for (int j = 0; j < I::KJ; ++j)
+#pragma unroll
+          for (int u = 0; u < I::kSubs; ++u) {
+            const bf16x8 kf = *(const bf16x8 *)(ks + (u * I::KW + kw) * 32 * I::kRow + k_rd[j]);
+            s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[j], s[u], 0, 0, 0);
+          }
+        auto key_of = [&](int u, int e) { return kb + 32 * (u * I::KW + kw) + 8 * (e / 4) + 4 * fh + e % 4; };
+        if (bad) {
+#pragma unroll
+          for (int u = 0; u < I::kSubs; ++u)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int key = min(key_of(u, e), len - 1);
+              if (r.over || s_pages[page_of(a, key) - first_page] < 0) s[u][e] = NAN;
+            }
+        }
+        if (kb + I::kStep > least) {
+#pragma unroll
+          for (int u = 0; u < I::kSubs; ++u)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (key_of(u, e) >= min(limit, len)) s[u][e] = -INFINITY;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int u = 0; u < I::kSubs; ++u)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) top = fmaxf(top, s[u][e]);
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        // the maximum in use follows when it is passed by 2^8: sums stay far from overflow and are rarely scaled
+        const bool up = (top - m) * a.c > 8.0f;                // the first time m = -inf
+        const float now = up ? top : m, ref = reference(now), alpha = up ? weight(a, m, now) : 1.0f, less = -ref * a.c;
+        m = now;
+        float sum = 0.f;
+#pragma unroll
+        for (int u = 0; u < I::kSubs; ++u)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            s[u][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e], a.c, less));
+            sum += s[u][e];
+          }
+        l = l * alpha + sum;
+        if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
+#pragma unroll
+          for (int t = 0; t < I::NT; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[t][e] *= alpha;
+        }
+        if (odd) {
+#pragma unroll 1
+          for (int x = 0; x < 64 && kb + x < len; ++x) {
+            if (I::KW == 2 && x / 32 != kw) continue;
+            const int key = kb + x, page = page_of(a, key), id = max(s_pages[page - first_page], 0);
+            const bf16_t *v = vbase + (int64_t)id * a.p.v_page_stride + (key - page * a.p.page_size) * a.p.dh + 4 * fh;
+#pragma unroll
+            for (int t = 0; t < I::NT; ++t)
+#pragma unroll
+              for (int e = 0; e < 16; e += 4) {
+                const int d = 32 * t + 2 * e;
+                uint2 y = make_uint2(0, 0);
+                if (key < limit && (kWhole || d + 4 * fh < a.p.dh)) y = *(const uint2 *)(v + d);
+                o[t][e] += odd_part(y.x << 16);
+                o[t][e + 1] += odd_part(y.x & 0xffff0000u);
+                o[t][e + 2] += odd_part(y.y << 16);
+                o[t][e + 3] += odd_part(y.y & 0xffff0000u);
+              }
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < I::kSubs; ++u)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {                        // 16 keys
+            auto p = [&](int i) { return s[u][8 * h + i]; };
+            const bf16x8 hi = __builtin_bit_cast(bf16x8, make_uint4(upper_parts(p(0), p(1)), upper_parts(p(2), p(3)), upper_parts(p(4), p(5)), upper_parts(p(6), p(7))));
+            const bf16x8 lo = __builtin_bit_cast(bf16x8, make_uint4(lower_parts(p(0), p(1)), lower_parts(p(2), p(3)), lower_parts(p(4), p(5)), lower_parts(p(6), p(7))));
+            const int at = (32 * (u * I::KW + kw) + 16 * h) * I::kRow;
+#pragma unroll
+            for (int t = 0; t < I::NT; ++t) {
+              const short4v v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((trptr_t)(vs + at + v_rd[t][0]));
+              const short4v v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((trptr_t)(vs + at + v_rd[t][1]));
+              const bf16x8 vt = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+              o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, hi, o[t], 0, 0, 0);
+              o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, lo, o[t], 0, 0, 0);
+            }
+          }
+      };
+      load(k0, 0);
+      for (int kb = k0;;) {               // two steps a turn, so that a buffer's place is a constant
+        step(kb, std::integral_constant<int, 0>{});
+        if (kb >= k1 - I::kStep) break;
+        kb += I::kStep;
+        step(kb, std::integral_constant<int, 1>{});
+        if (kb >= k1 - I::kStep) break;
+        kb += I::kStep;
+      }
+    }
+
+    l += __shfl_xor(l, 32, kWave);
+    if (I::KW == 2) {                     // the second pair's results, to the first
+      __syncthreads();
+      float *x = reinterpret_cast<float *>(lds) + cw * (I::NT * 16 + 2) * 64 + lane;
+      if (kw == 1) {
+#pragma unroll
+        for (int t = 0; t < I::NT; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[(t * 16 + e) * 64] = o[t][e];
+        x[I::NT * 16 * 64] = m;
+        x[(I::NT * 16 + 1) * 64] = l;
+      }
+      __syncthreads();
+      if (kw == 0) {
+        const float m1 = x[I::NT * 16 * 64], l1 = x[(I::NT * 16 + 1) * 64], top = fmaxf(m, m1), ref = reference(top);
+        const float f0 = weight(a, m, ref), f1 = weight(a, m1, ref);
+#pragma unroll
+        for (int t = 0; t < I::NT; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[t][e] = f0 * o[t][e] + f1 * x[(t * 16 + e) * 64];
+        l = f0 * l + f1 * l1;
+        m = top;
+      }
+    }
+    if (col < cols && kw == 0) {
+      if (piece.done) {
+        int r_;
+        bf16_t *dst = (bf16_t *)a.p.out + row_place(a, r.row0, piece.head, (int64_t)piece.tile * I::QT + col, a.p.out_stride, &r_);
+#pragma unroll
+        for (int t = 0; t < I::NT; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            const int d = 32 * t + 2 * e + 4 * fh;
+            if (kWhole || d < a.p.dh) store4(dst + d, floatx4{o[t][e], o[t][e + 1], o[t][e + 2], o[t][e + 3]}, l, limit <= 0);
+          }
+      } else {
+        float *slot = partial<I>(a, worker, piece.begun);
+        if (fh == 0) {
+          slot[col] = m;
+          slot[I::QT + col] = l;
+        }
+#pragma unroll
+        for (int t = 0; t < I::NT; ++t)
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            const int d = 32 * t + 2 * e + 4 * fh;
+            if (kWhole || d < a.p.dh) *(floatx4 *)(slot + 2 * I::QT + col * DH + d) = floatx4{o[t][e], o[t][e + 1], o[t][e + 2], o[t][e + 3]};
+          }
+      }
+    }
+    if (!piece.done && piece.begun && tid == 0) note_join<I>(a, worker, w, r, piece);
+  }
+}
+
+template <class F>
+auto with_wide(int64_t pairs, int dh, F f) {
+  if (dh <= 64) return pairs <= 64 ? f(WideInst<64, 2>{}) : f(WideInst<64, 4>{});
+  return pairs <= 64 ? f(WideInst<128, 2>{}) : f(WideInst<128, 4>{});
+}
+
+template <int DH, int CW>
+pvf_status launch(WideInst<DH, CW>, hipStream_t s, Args &a) {
+  typedef WideInst<DH, CW> I;
+  const Plan p = prepare<I>(a);
+  if (a.p.dh == DH) page_attention_wide_kernel<DH, CW, true><<<p.workers, 256, 0, s>>>(a);
+  else page_attention_wide_kernel<DH, CW, false><<<p.workers, 256, 0, s>>>(a);
+  PVF_LAUNCH_CHECK(nullptr, "page_attention_wide");
+  if (!a.whole) {
+    page_attention_join_kernel<bf16_t, I><<<p.workers - 1, kJoinThreads, 0, s>>>(a);
+    PVF_LAUNCH_CHECK(nullptr, "page_attention_join");
+  }
+  return PVF_OK;
+}
+
+}  // namespace
+
+pvf_status launch_wide(hipStream_t s, Args &a, int64_t pairs) {
+  return with_wide(pairs, a.p.dh, [&](auto inst) { return launch(inst, s, a); });
+}
+int64_t wide_workspace(int B, int M, int Hkv, int group, int dh, int width, int page_size, int64_t pairs) {
+  return with_wide(pairs, dh, [&](auto inst) {
+    typedef decltype(inst) I;
+    return workspace_bytes<I>(plan<I>(B, M, Hkv, group, width, page_size));
+  });
+}
+
+}  // namespace page
+}  // namespace pvf

@@ -1253,7 +1253,7 @@ extern "C" pvf_status pvf_page_attention(void *stream, int32_t dtype, const void
   if (check_dtype(dtype) != PVF_OK) return PVF_EINVAL;
   if (const pvf_status st = check_cache("pvf_page_attention", dtype, M, H, Hkv, d_head, n_pages, page_size, k_cache, v_cache, k_page_stride, v_page_stride)) return st;
   if (const pvf_status st = check_attention("pvf_page_attention", B, M, H, Hkv, width, table_stride, page_size)) return st;
-  PVF_REQUIRE(nullptr, (causal == 0 || causal == 1) && std::isfinite(scale), PVF_EINVAL, "pvf_page_attention: causal=%d, scale=%g", causal, scale);
+  PVF_REQUIRE(nullptr, (causal == 0 || causal == 1) && std::fabs(scale) <= 0x1p100f, PVF_EINVAL, "pvf_page_attention: causal=%d, scale=%g", causal, scale);
   PVF_REQUIRE(nullptr, cu_rows || B == M, PVF_EINVAL, "pvf_page_attention: without cu_rows there is one row a request, not %d of %d", M, B);
   if (M == 0 || B == 0) return PVF_OK;
   const int per_16 = dtype == PVF_F32 ? 4 : 8;
