@@ -31,11 +31,11 @@ constexpr int kJoinInts = 8;              // workers that took it (0: none), its
 struct Request {
   int row0, n, len, steps, tiles;         // its rows, visible keys, steps of keys and tiles of columns
   bool over;                              // longer than its table
-  int64_t items;
+  int64_t triples, items;                 // items: its length on the line, triples or steps of them
 };
 
 template <class I>
-__device__ __forceinline__ Request request(const Args &a, int b) {
+__device__ __forceinline__ Request request(const Args &a, int b, bool whole) {
   Request r;
   const int raw = a.p.seq_len[b];
   if (a.p.cu_rows) {
@@ -50,8 +50,9 @@ __device__ __forceinline__ Request request(const Args &a, int b) {
   r.len = min(len, most);
   r.over = len > most;
   r.steps = max((r.len - 1) / I::kStep + 1, 1);
-  r.tiles = (int)(((int64_t)r.n * a.group + I::QT - 1) / I::QT);
-  r.items = (int64_t)r.tiles * a.p.Hkv * (a.whole ? 1 : r.steps);
+  r.tiles = (int)(((uint32_t)(r.n * a.group) + I::QT - 1) / I::QT);
+  r.triples = (int64_t)r.tiles * a.p.Hkv;
+  r.items = whole ? r.triples : r.triples * r.steps;
   return r;
 }
 
@@ -71,21 +72,30 @@ __device__ __forceinline__ int64_t uniform64(int64_t x) {
   return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
 }
 
+// a / b, and *rest: exact below 2^52.
+__device__ __forceinline__ int64_t divide(int64_t a, int b, int64_t *rest) {
+  int64_t q = (int64_t)((double)a / (double)b), r = a - q * b;   // at most one off
+  if (r < 0) { --q; r += b; }
+  if (r >= b) { ++q; r -= b; }
+  *rest = r;
+  return q;
+}
+
 // A worker's place: items [at, end) of the line, `at` in request b, whose first item is `first`.
 struct Place {
   int64_t at, end, first, share;
   int b;
-  bool all;                               // every worker has a share
+  bool whole;                             // the line is of triples
 };
 
 // The request that item `at` belongs to, and its first item.
 template <class I>
-__device__ __forceinline__ int find_request(const Args &a, int64_t at, int64_t *first) {
+__device__ __forceinline__ int find_request(const Args &a, int64_t at, bool whole, int64_t *first) {
   const int lane = threadIdx.x & 63;
   int64_t base = 0;
   for (int b0 = 0;; b0 += kWave) {
     const int b = b0 + lane;
-    const int64_t items = b < a.p.B ? request<I>(a, b).items : 0, upto = base + wave_scan(items);
+    const int64_t items = b < a.p.B ? request<I>(a, b, whole).items : 0, upto = base + wave_scan(items);
     const uint64_t beyond = __builtin_amdgcn_ballot_w64(upto > at);
     if (beyond || b0 + kWave >= a.p.B) {
       const int l = beyond ? __builtin_ctzll(beyond) : 63;
@@ -96,46 +106,43 @@ __device__ __forceinline__ int find_request(const Args &a, int64_t at, int64_t *
   }
 }
 
-// kSnap instances have wide partial results: while no triple is longer than kSnap shares, triples stay whole, and a border inside of one
-// moves to its nearer end.
-template <class I>
-__device__ __forceinline__ int64_t snapped(const Args &a, int64_t border, int64_t items) {
-  if (border >= items) return items;
-  int64_t first;
-  const Request r = request<I>(a, find_request<I>(a, border, &first));
-  const int64_t off = (border - first) % r.steps;
-  return 2 * off < r.steps ? border - off : border - off + r.steps;
-}
-
+// Triples stay whole where the host says so, and on kSnap instances, whose partial results are large, where that divides the work well enough:
+// none is longer than kSnap shares, and there are no more of them than workers, or several for each.
 template <class I>
 __device__ __forceinline__ Place place_of(const Args &a, int block, int workers, int *worker) {
   const int lane = threadIdx.x & 63;
-  int64_t items = 0;
+  int64_t items = 0, triples = 0;
   int longest = 0;
   for (int b = lane; b < a.p.B; b += kWave) {
-    const Request r = request<I>(a, b);
+    const Request r = request<I>(a, b, a.whole);
     items += r.items;
+    triples += r.triples;
     longest = max(longest, r.n > 0 ? r.steps : 0);
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
     items += __shfl_xor(items, o, kWave);
-    longest = max(longest, __shfl_xor(longest, o, kWave));
+    if (I::kSnap > 0) triples += __shfl_xor(triples, o, kWave);
+    if (I::kSnap > 0) longest = max(longest, __shfl_xor(longest, o, kWave));
   }
   items = uniform64(items);
-  longest = __builtin_amdgcn_readfirstlane(longest);
   Place w;
-  w.share = (items + workers - 1) / workers;
-  w.all = w.share * (workers - 1) < items;
+  int64_t rest;
+  w.share = divide(items + workers - 1, workers, &rest);
+  w.whole = a.whole;
+  if (I::kSnap > 0 && !a.whole) {
+    triples = uniform64(triples);
+    if (__builtin_amdgcn_readfirstlane(longest) <= I::kSnap * w.share && (triples <= workers || triples >= 4 * (int64_t)workers)) {
+      w.whole = true;
+      items = triples;
+      w.share = divide(items + workers - 1, workers, &rest);
+    }
+  }
   // workers that follow each other read the same keys for other columns: where all take part, neighbours run on one XCD and share its L2
-  *worker = workers % 8 == 0 && w.all ? block % 8 * (workers / 8) + block / 8 : block;
+  *worker = workers % 8 == 0 && w.share * (workers - 1) < items ? block % 8 * (workers / 8) + block / 8 : block;
   w.at = w.share * *worker;
   w.end = min(w.at + w.share, items);
-  if (I::kSnap > 0 && !a.whole && longest <= I::kSnap * w.share) {
-    w.at = snapped<I>(a, w.at, items);
-    w.end = snapped<I>(a, w.end, items);
-  }
-  if (w.at < w.end) w.b = find_request<I>(a, w.at, &w.first);
+  if (w.at < w.end) w.b = find_request<I>(a, w.at, w.whole, &w.first);
   return w;
 }
 
@@ -152,34 +159,35 @@ __device__ __forceinline__ bool next_piece(const Args &a, Place &w, Request &r, 
   while (w.at - w.first >= r.items) {
     w.first += r.items;
     if (++w.b >= a.p.B) return false;
-    r = request<I>(a, w.b);
+    r = request<I>(a, w.b, w.whole);
   }
   int64_t triple = w.at - w.first;
-  if (a.whole) {
+  if (w.whole) {
     p.step0 = 0;
     p.step1 = r.steps;
     ++w.at;
   } else {
-    const int64_t rel = triple;
-    triple = rel / r.steps;
-    p.step0 = (int)(rel - triple * r.steps);
+    int64_t step0;
+    triple = divide(triple, r.steps, &step0);
+    p.step0 = (int)step0;
     p.step1 = (int)min((int64_t)r.steps, p.step0 + (w.end - w.at));
     w.at += p.step1 - p.step0;
   }
-  p.head = (int)(triple / r.tiles);
-  p.tile = (int)(triple - (int64_t)p.head * r.tiles);
-  p.cols = (int)min((int64_t)I::QT, (int64_t)r.n * a.group - (int64_t)p.tile * I::QT);
+  p.head = (int)((uint32_t)triple / (uint32_t)r.tiles);        // rows and heads together are below 2^31
+  p.tile = (int)((uint32_t)triple - (uint32_t)p.head * r.tiles);
+  if (p.head >= a.p.Hkv) return false;                         // cannot be, unless lengths change under the call
+  p.cols = min(I::QT, r.n * a.group - p.tile * I::QT);
   p.begun = p.step0 == 0;
   p.done = p.begun && p.step1 == r.steps;
   return true;
 }
 
 // Where a column's row and head begin in q or out.
-__device__ __forceinline__ int64_t row_place(const Args &a, int row0, int head, int64_t pair, int64_t stride, int *row) {
-  const int64_t m = pair / a.group;
-  const int sub = (int)(pair - m * a.group);
+__device__ __forceinline__ int64_t row_place(const Args &a, int row0, int head, int pair, int64_t stride, int *row) {
+  const uint32_t m = (uint32_t)pair / (uint32_t)a.group;
+  const int sub = (int)((uint32_t)pair - m * (uint32_t)a.group);
   *row = (int)m;
-  return (row0 + m) * stride + (int64_t)(head * a.group + sub) * a.p.dh;
+  return (int64_t)(row0 + (int)m) * stride + (int64_t)(head * a.group + sub) * a.p.dh;
 }
 
 // Partial results: worker w has two, 2 w: of the triple that an earlier worker began, 2 w + 1: of the one that it begins itself.
@@ -189,17 +197,18 @@ __device__ __forceinline__ float *partial(const Args &a, int worker, bool begun)
 // How many workers take a triple that this one begins.
 template <class I>
 __device__ __forceinline__ void note_join(const Args &a, int worker, const Place &w, const Request &r, const Piece &p) {
-  const int64_t last = (w.at - 1) + (r.steps - p.step1);       // its last item
+  const int64_t behind = r.steps - p.step1;                    // items that other workers take, w.share each
   int32_t *j = a.joins + (int64_t)worker * kJoinInts;
+  int64_t rest;
   *(int4 *)(j + 4) = make_int4(p.head, p.tile, 0, 0);
-  *(int4 *)j = make_int4((int)(last / w.share) - worker + 1, r.row0, r.n, r.len);
+  *(int4 *)j = make_int4((int)divide(behind + w.share - 1, (int)w.share, &rest) + 1, r.row0, r.n, r.len);
 }
 
 template <typename T>
-__device__ __forceinline__ void store4(T *dst, floatx4 x, float total, bool none) {
+__device__ __forceinline__ void store4(T *dst, floatx4 x, float inv_total, bool none) {
   struct alignas(4 * sizeof(T)) { T v[4]; } y;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) y.v[i] = from_float<T>(none ? 0.f : x[i] / total);
+  for (int i = 0; i < 4; ++i) y.v[i] = from_float<T>(none ? 0.f : x[i] * inv_total);
   *(decltype(y) *)dst = y;
 }
 
@@ -235,11 +244,11 @@ __device__ __forceinline__ uint32_t bf16s_finite(uint32_t w) {   // what is not 
 // y (float32 bits) where it is not finite, else zero: what a key adds whose probability is not zero
 __device__ __forceinline__ float odd_part(uint32_t y) { return (y & 0x7f800000u) == 0x7f800000u ? __uint_as_float(y) : 0.f; }
 
-// Two probabilities as bf16 in two parts: the upper halves, and the rest of 16 bits.  The rest is never zero beside p > 0: zero times an
-// infinite value would make NaN of infinity (2^-23 of p is added; for p = 0 the lowest bit is lost in the conversion).
+// Two probabilities as bf16 in two parts: the upper halves, and the rest of 16 bits.  The rest is never zero beside p > 0 (2^-23 of p is added): zero
+// times an infinite value would make NaN of infinity.
 __device__ __forceinline__ uint32_t upper_parts(float x, float y) { return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302); }
 __device__ __forceinline__ uint32_t lower_parts(float x, float y) {
-  auto low = [](float p) { return (bf16_t)(__uint_as_float(__float_as_uint(p) | 1u) - __uint_as_float(__float_as_uint(p) & 0xffff0000u)); };
+  auto low = [](float p) { return (bf16_t)__builtin_fmaf(p, 1.0f + 0x1p-23f, -__uint_as_float(__float_as_uint(p) & 0xffff0000u)); };
   const bf16x2 r = {low(x), low(y)};
   return __builtin_bit_cast(uint32_t, r);
 }
@@ -258,7 +267,7 @@ page_attention_join_kernel(Args a) {
   const int n = j[0];
   if (n == 0) return;
   const int row0 = j[1], rows = j[2], len = j[3], head = j[4], tile = j[5];
-  const int cols = (int)min((int64_t)QT, (int64_t)rows * a.group - (int64_t)tile * QT);
+  const int cols = min(QT, rows * a.group - tile * QT);
   const float *first = partial<I>(a, blockIdx.x, true);
   auto slot = [&](int i) { return i == 0 ? first : first + (int64_t)(2 * i - 1) * I::kSlotFloats; };
   // a thread takes four dimensions of a column; where the workgroup has more threads than that, groups of them take every parts-th result
@@ -318,8 +327,8 @@ page_attention_join_kernel(Args a) {
     }
     if (live && part == 0) {
       int row;
-      const int64_t at = row_place(a, row0, head, (int64_t)tile * QT + col, a.p.out_stride, &row);
-      store4((T *)a.p.out + at + d, sum, s_total[col], limit_of(a, len, rows, row) <= 0);
+      const int64_t at = row_place(a, row0, head, tile * QT + col, a.p.out_stride, &row);
+      store4((T *)a.p.out + at + d, sum, 1.0f / s_total[col], limit_of(a, len, rows, row) <= 0);
     }
   }
 }

@@ -273,7 +273,7 @@ page_attention_kernel(Args a) {
   Place w = place_of<I>(a, blockIdx.x, gridDim.x, &worker);
   if (!a.whole && tid == 0) a.joins[(int64_t)worker * kJoinInts] = 0;
   if (w.at >= w.end) return;
-  Request r = request<I>(a, w.b);
+  Request r = request<I>(a, w.b, w.whole);
   Piece piece;
   Pass<T, DH, NQ, kWhole> pass(a, s_pages);
   while (next_piece<I>(a, w, r, piece)) {
@@ -287,7 +287,7 @@ page_attention_kernel(Args a) {
     for (int nq = 0; nq < NQ; ++nq) {
       const int col = 16 * nq + pass.c;
       int row;
-      const T *src = (const T *)a.p.q + row_place(a, r.row0, piece.head, (int64_t)piece.tile * I::QT + col, a.p.q_stride, &row) + I::KE * pass.g;
+      const T *src = (const T *)a.p.q + row_place(a, r.row0, piece.head, piece.tile * I::QT + col, a.p.q_stride, &row) + I::KE * pass.g;
       pass.limit[nq] = col < cols ? limit_of(a, r.len, r.n, row) : INT32_MAX;
       pass.least = min(pass.least, pass.limit[nq]);
 #pragma unroll
@@ -361,8 +361,8 @@ page_attention_kernel(Args a) {
         }
         if (piece.done) {
           int row;
-          const int64_t at = row_place(a, r.row0, piece.head, (int64_t)piece.tile * I::QT + col, a.p.out_stride, &row);
-          store4((T *)a.p.out + at + d, sum, total, limit_of(a, r.len, r.n, row) <= 0);
+          const int64_t at = row_place(a, r.row0, piece.head, piece.tile * I::QT + col, a.p.out_stride, &row);
+          store4((T *)a.p.out + at + d, sum, 1.0f / total, limit_of(a, r.len, r.n, row) <= 0);
         } else {
           *(floatx4 *)(slot + 2 * I::QT + col * DH + d) = sum;
           if (d == 0) {

@@ -14,9 +14,23 @@ namespace page {
 namespace {
 
 typedef short short4v __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(1))) const void gptr_t;
 typedef __attribute__((address_space(3))) void lptr_t;
 typedef __attribute__((address_space(3))) short4v *trptr_t;
+
+// 16 bytes a lane from global memory to LDS, lane after lane from `at` on, counted by vmcnt alone: written out because the compiler, which cannot
+// tell the tile on its way from the one that is read, waits for the builtin's loads before the next read of LDS.  There is no register that a load
+// writes.  Every wait for them stands below.
+__device__ __forceinline__ void load_to_lds(const void *src, uint32_t lane_bytes, uint32_t at) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(lane_bytes), "s"(src) : "memory", "m0");
+}
+// at most N of this wave's loads are on the way; its LDS reads are done; then every wave's
+template <int N>
+__device__ __forceinline__ void wait_and_meet() {
+  __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4) << 14);   // vmcnt(N) lgkmcnt(0)
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 
 // CW: waves beside each other over columns; the 4 / CW groups of them share out the keys of a step.
 template <int DH, int CW>
@@ -24,7 +38,7 @@ struct WideInst {
   static constexpr int kDh = DH, QT = 32 * CW, KW = 4 / CW, kStep = 64, kSubs = 2 / KW, kSnap = 4, kWholeSteps = 16, kPerCu = 2;
   static constexpr int NT = DH / 32, KJ = DH / 16;
   static constexpr int kRow = DH * 2, kChunks = DH / 8, kTile = kStep * kRow;   // bytes of a key, its chunks, bytes of 64 keys
-  static constexpr int kLoads = kTile / 4096;                                 // loads of 1 KB a wave and tile
+  static constexpr int kLoads = kTile / 4096, kKeys = 1024 / kRow;             // loads of 1 KB a wave and tile, keys of one
   static constexpr int kSlotFloats = QT * (DH + 2);
   static_assert(CW * KW == 4 && kSubs * KW == 2, "four waves, two groups of 32 keys");
 };
@@ -41,7 +55,7 @@ page_attention_wide_kernel(Args a) {
   Place w = place_of<I>(a, blockIdx.x, gridDim.x, &worker);
   if (!a.whole && tid == 0) a.joins[(int64_t)worker * kJoinInts] = 0;
   if (w.at >= w.end) return;
-  Request r = request<I>(a, w.b);
+  Request r = request<I>(a, w.b, w.whole);
   Piece piece;
 
   auto turn = [](int key) { return I::kChunks == 16 ? (key & 3) << 2 | (key >> 2 & 3) : (key >> 1 & 1) << 2 | (key >> 2 & 3); };
@@ -58,14 +72,18 @@ page_attention_wide_kernel(Args a) {
       v_rd[t][e] = key * I::kRow + ((dim / 8 ^ turn(key)) << 4) + dim % 8 * 2;
     }
 
+  // a lane's part of a load: a chunk of one of its kKeys keys (turn() of a key is the same for every load of a wave)
+  const int lane_key = wid * I::kKeys + lane / I::kChunks, lane_chunk = lane % I::kChunks ^ turn(lane_key);
+  const uint32_t lane_bytes = (uint32_t)((lane / I::kChunks) * a.p.dh + lane_chunk * 8) * 2;
+
   while (next_piece<I>(a, w, r, piece)) {
     const int cols = piece.cols, len = r.len, col = 32 * cw + fr;
     const bf16_t *kbase = (const bf16_t *)a.p.k_cache + (int64_t)piece.head * a.p.page_size * a.p.dh;
     const bf16_t *vbase = (const bf16_t *)a.p.v_cache + (int64_t)piece.head * a.p.page_size * a.p.dh;
     int row;
-    const int64_t q_at = row_place(a, r.row0, piece.head, (int64_t)piece.tile * I::QT + col, a.p.q_stride, &row);
+    const int64_t q_at = row_place(a, r.row0, piece.head, piece.tile * I::QT + col, a.p.q_stride, &row);
     const int limit = col < cols ? limit_of(a, len, r.n, row) : INT32_MAX;
-    const int least = limit_of(a, len, r.n, (int)((int64_t)piece.tile * I::QT / a.group));      // of the tile's columns: the first row's
+    const int least = limit_of(a, len, r.n, (int)((uint32_t)(piece.tile * I::QT) / (uint32_t)a.group));      // of the tile's columns: the first row's
     bf16x8 q[I::KJ];
 #pragma unroll
     for (int j = 0; j < I::KJ; ++j) {
@@ -92,26 +110,53 @@ page_attention_wide_kernel(Args a) {
       const bool bad = __syncthreads_or(load_pages(a, w.b, k0, k1, first_page, s_pages)) != 0 || r.over;
       if (k1 <= k0) continue;             // a request without keys
 
-      auto load = [&](int kb, int buf) {  // 64 keys from kb on and their values; the ones behind the last as copies of it
-        unsigned char *dst = lds + buf * 2 * I::kTile;
+      // 64 keys from kb on (or their values), kKeys neighbouring ones a load: they share a page, which is looked up once a wave.  What lies behind the
+      // last key comes along.
+      auto load = [&](const bf16_t *base, int64_t page_stride, int kb, uint32_t dst) {
 #pragma unroll
         for (int i = 0; i < I::kLoads; ++i) {
-          const int at = (i * 4 + wid) * 1024 + lane * 16, in = at / I::kRow, chunk = at / 16 % I::kChunks ^ turn(in);
-          const int key = min(kb + in, len - 1), page = page_of(a, key), id = max(s_pages[page - first_page], 0);
-          const int off = (key - page * a.p.page_size) * a.p.dh + chunk * 8;
-          if (kWhole || chunk * 8 < a.p.dh) {
-            __builtin_amdgcn_global_load_lds((gptr_t *)(kbase + (int64_t)id * a.p.k_page_stride + off), (lptr_t *)(dst + (i * 4 + wid) * 1024), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((gptr_t *)(vbase + (int64_t)id * a.p.v_page_stride + off), (lptr_t *)(dst + I::kTile + (i * 4 + wid) * 1024), 16, 0, 0);
-          }
+          const int key = min(kb + (i * 4 + wid) * I::kKeys, (len - 1) & ~(I::kKeys - 1)), page = page_of(a, key);
+          const int id = max(__builtin_amdgcn_readfirstlane(s_pages[page - first_page]), 0);
+          const bf16_t *src = base + (int64_t)id * page_stride + (key - page * a.p.page_size) * a.p.dh;
+          if (kWhole || lane_chunk * 8 < a.p.dh) load_to_lds(src, lane_bytes, dst + (i * 4 + wid) * 1024);
         }
       };
+      const uint32_t lds_at = (uint32_t)(uintptr_t)(lptr_t *)lds;
+      auto load_keys = [&](int kb, int buf) { load(kbase, a.p.k_page_stride, kb, lds_at + buf * 2 * I::kTile); };
+      auto load_values = [&](int kb, int buf) { load(vbase, a.p.v_page_stride, kb, lds_at + (buf * 2 + 1) * I::kTile); };
 
+      // Keys and values of a step are asked for two steps ahead, each when its buffer has been read: three tiles are on the way at most, and waits are
+      // for the oldest (the last two steps': for all).  The keys of this step are awaited before it begins.
       auto step = [&](int kb, auto buf_c) {
         constexpr int kBuf = decltype(buf_c)::value;
-        unsigned char *ks = lds + kBuf * 2 * I::kTile, *vs = ks + I::kTile;
-        __builtin_amdgcn_s_waitcnt(0x0f70);                    // vmcnt(0): this wave's part of the tile is there
-        __syncthreads();
-        if (kb < k1 - I::kStep) load(kb + I::kStep, kBuf ^ 1);
+        const unsigned char *ks = lds + kBuf * 2 * I::kTile;
+        unsigned char *vs = lds + (kBuf * 2 + 1) * I::kTile;
+        const bool more = kb < k1 - 2 * I::kStep;
+        floatx16 s[I::kSubs];
+#pragma unroll
+        for (int u = 0; u < I::kSubs; ++u)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[u][e] = 0.f;
+        // operands of half a row are read while the other half is multiplied
+        constexpr int kHalf = I::KJ / 2;
+        bf16x8 kf[2][kHalf][I::kSubs];
+        auto read_keys = [&](int half) {
+#pragma unroll
+          for (int j = 0; j < kHalf; ++j)
+#pragma unroll
+            for (int u = 0; u < I::kSubs; ++u) kf[half][j][u] = *(const bf16x8 *)(ks + (u * I::KW + kw) * 32 * I::kRow + k_rd[half * kHalf + j]);
+          __builtin_amdgcn_sched_barrier(0);
+        };
+        read_keys(0);
+        read_keys(1);
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int j = 0; j < kHalf; ++j)
+#pragma unroll
+            for (int u = 0; u < I::kSubs; ++u) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[half][j][u], q[half * kHalf + j], s[u], 0, 0, 0);
+        if (more) wait_and_meet<2 * I::kLoads>(); else wait_and_meet<0>();     // its values are there, its keys have been read
+        if (more) load_keys(kb + 2 * I::kStep, kBuf);
         bool odd = false;
         if (kb + I::kStep > least) {
           // The tile holds keys that a row does not see, or copies of the last one.  0 times an infinity is no zero: values that are not finite
@@ -126,26 +171,15 @@ page_attention_wide_kernel(Args a) {
           }
           odd = __syncthreads_or(mine) != 0;
         }
-        floatx16 s[I::kSubs];
-#pragma unroll
-        for (int u = 0; u < I::kSubs; ++u)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) s[u][e] = 0.f;
-#pragma unroll
-        for (int j = 0; j < I::KJ; ++j)
-#pragma unroll
-          for (int u = 0; u < I::kSubs; ++u) {
-            const bf16x8 kf = *(const bf16x8 *)(ks + (u * I::KW + kw) * 32 * I::kRow + k_rd[j]);
-            s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[j], s[u], 0, 0, 0);
-          }
         auto key_of = [&](int u, int e) { return kb + 32 * (u * I::KW + kw) + 8 * (e / 4) + 4 * fh + e % 4; };
-        if (bad) {
+        if (bad) {                                             // four keys from a multiple of four on share a page
 #pragma unroll
           for (int u = 0; u < I::kSubs; ++u)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int key = min(key_of(u, e), len - 1);
-              if (r.over || s_pages[page_of(a, key) - first_page] < 0) s[u][e] = NAN;
+            for (int e = 0; e < 16; e += 4) {
+              const bool none = (s_pages[page_of(a, min(key_of(u, e), len - 1)) - first_page] < 0) | r.over;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) s[u][e + i] = none ? NAN : s[u][e + i];
             }
         }
         if (kb + I::kStep > least) {
@@ -200,31 +234,60 @@ page_attention_wide_kernel(Args a) {
               }
           }
         }
+        // 16 keys at a time, the next ones' operands read ahead
+        bf16x8 vt[2][I::NT];
+        auto read_values = [&](int k) {
+          const int at = (32 * (k / 2 * I::KW + kw) + 16 * (k % 2)) * I::kRow;
 #pragma unroll
-        for (int u = 0; u < I::kSubs; ++u)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {                        // 16 keys
-            auto p = [&](int i) { return s[u][8 * h + i]; };
-            const bf16x8 hi = __builtin_bit_cast(bf16x8, make_uint4(upper_parts(p(0), p(1)), upper_parts(p(2), p(3)), upper_parts(p(4), p(5)), upper_parts(p(6), p(7))));
-            const bf16x8 lo = __builtin_bit_cast(bf16x8, make_uint4(lower_parts(p(0), p(1)), lower_parts(p(2), p(3)), lower_parts(p(4), p(5)), lower_parts(p(6), p(7))));
-            const int at = (32 * (u * I::KW + kw) + 16 * h) * I::kRow;
-#pragma unroll
-            for (int t = 0; t < I::NT; ++t) {
-              const short4v v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((trptr_t)(vs + at + v_rd[t][0]));
-              const short4v v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((trptr_t)(vs + at + v_rd[t][1]));
-              const bf16x8 vt = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-              o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, hi, o[t], 0, 0, 0);
-              o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, lo, o[t], 0, 0, 0);
-            }
+          for (int t = 0; t < I::NT; ++t) {
+            const short4v v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((trptr_t)(vs + at + v_rd[t][0]));
+            const short4v v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((trptr_t)(vs + at + v_rd[t][1]));
+            vt[k % 2][t] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
           }
+          __builtin_amdgcn_sched_barrier(0);
+        };
+        read_values(0);
+#pragma unroll
+        for (int k = 0; k < 2 * I::kSubs; ++k) {
+          if (k + 1 < 2 * I::kSubs) read_values(k + 1);
+          auto p = [&](int i) { return s[k / 2][8 * (k % 2) + i]; };
+          const bf16x8 hi = __builtin_bit_cast(bf16x8, make_uint4(upper_parts(p(0), p(1)), upper_parts(p(2), p(3)), upper_parts(p(4), p(5)), upper_parts(p(6), p(7))));
+          const bf16x8 lo = __builtin_bit_cast(bf16x8, make_uint4(lower_parts(p(0), p(1)), lower_parts(p(2), p(3)), lower_parts(p(4), p(5)), lower_parts(p(6), p(7))));
+#pragma unroll
+          for (int t = 0; t < I::NT; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt[k % 2][t], hi, o[t], 0, 0, 0);
+#pragma unroll
+          for (int t = 0; t < I::NT; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt[k % 2][t], lo, o[t], 0, 0, 0);
+        }
       };
-      load(k0, 0);
+      __builtin_amdgcn_s_waitcnt(0x0f70);                      // vmcnt(0): nothing else is counted from here on
+      load_keys(k0, 0);
+      load_values(k0, 0);
+      const bool two = k0 < k1 - I::kStep;
+      if (two) {
+        load_keys(k0 + I::kStep, 1);
+        load_values(k0 + I::kStep, 1);
+        wait_and_meet<3 * I::kLoads>();
+      } else {
+        wait_and_meet<I::kLoads>();
+      }
       for (int kb = k0;;) {               // two steps a turn, so that a buffer's place is a constant
         step(kb, std::integral_constant<int, 0>{});
         if (kb >= k1 - I::kStep) break;
+        if (kb < k1 - 2 * I::kStep) {
+          wait_and_meet<2 * I::kLoads>(); // the next step's keys are there, this one's values have been read
+          load_values(kb + 2 * I::kStep, 0);
+        } else {
+          wait_and_meet<0>();
+        }
         kb += I::kStep;
         step(kb, std::integral_constant<int, 1>{});
         if (kb >= k1 - I::kStep) break;
+        if (kb < k1 - 2 * I::kStep) {
+          wait_and_meet<2 * I::kLoads>();
+          load_values(kb + 2 * I::kStep, 1);
+        } else {
+          wait_and_meet<0>();
+        }
         kb += I::kStep;
       }
     }
@@ -256,13 +319,14 @@ page_attention_wide_kernel(Args a) {
     if (col < cols && kw == 0) {
       if (piece.done) {
         int r_;
-        bf16_t *dst = (bf16_t *)a.p.out + row_place(a, r.row0, piece.head, (int64_t)piece.tile * I::QT + col, a.p.out_stride, &r_);
+        const float inv = 1.0f / l;
+        bf16_t *dst = (bf16_t *)a.p.out + row_place(a, r.row0, piece.head, piece.tile * I::QT + col, a.p.out_stride, &r_);
 #pragma unroll
         for (int t = 0; t < I::NT; ++t)
 #pragma unroll
           for (int e = 0; e < 16; e += 4) {
             const int d = 32 * t + 2 * e + 4 * fh;
-            if (kWhole || d < a.p.dh) store4(dst + d, floatx4{o[t][e], o[t][e + 1], o[t][e + 2], o[t][e + 3]}, l, limit <= 0);
+            if (kWhole || d < a.p.dh) store4(dst + d, floatx4{o[t][e], o[t][e + 1], o[t][e + 2], o[t][e + 3]}, inv, limit <= 0);
           }
       } else {
         float *slot = partial<I>(a, worker, piece.begun);
