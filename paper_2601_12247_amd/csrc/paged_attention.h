@@ -16,6 +16,8 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 constexpr int kPageSlots = 1024;          // table entries in LDS
+template <int N>
+struct Const { static constexpr int value = N; };
 
 struct Args {
   PageAttention p;
@@ -28,123 +30,28 @@ struct Args {
 };
 constexpr int kJoinInts = 8;              // workers that took it (0: none), its first row, rows, length, key head, tile
 
+// A wave's sums over lanes 0 .. i, at most 2^32 - 1.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+  auto behind = [&](auto ctrl, auto rows) {
+    x = __builtin_elementwise_add_sat(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
+  };
+  behind(Const<0x111>{}, Const<0xf>{});   // rows of 16: one, two, four, eight lanes back
+  behind(Const<0x112>{}, Const<0xf>{});
+  behind(Const<0x114>{}, Const<0xf>{});
+  behind(Const<0x118>{}, Const<0xf>{});
+  behind(Const<0x142>{}, Const<0xa>{});   // the row in front, both rows in front
+  behind(Const<0x143>{}, Const<0xc>{});
+  return x;
+}
+__device__ __forceinline__ uint32_t last_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, 63); }
+
 struct Request {
   int row0, n, len, steps, tiles;         // its rows, visible keys, steps of keys and tiles of columns
   bool over;                              // longer than its table
-  int64_t triples, items;                 // items: its length on the line, triples or steps of them
 };
 
-template <class I>
-__device__ __forceinline__ Request request(const Args &a, int b, bool whole) {
-  Request r;
-  const int raw = a.p.seq_len[b];
-  if (a.p.cu_rows) {
-    const int from = a.p.cu_rows[b], to = a.p.cu_rows[b + 1];
-    r.row0 = min(max(from, 0), a.p.M);
-    r.n = max(min(to, a.p.M) - r.row0, 0);
-  } else {
-    r.row0 = b;
-    r.n = 1;
-  }
-  const int len = max(raw, 0), most = a.p.width * a.p.page_size;
-  r.len = min(len, most);
-  r.over = len > most;
-  r.steps = max((r.len - 1) / I::kStep + 1, 1);
-  r.tiles = (int)(((uint32_t)(r.n * a.group) + I::QT - 1) / I::QT);
-  r.triples = (int64_t)r.tiles * a.p.Hkv;
-  r.items = whole ? r.triples : r.triples * r.steps;
-  return r;
-}
-
-// Keys that row `row` of the request sees.
+// Keys that row `row` of a request sees.
 __device__ __forceinline__ int limit_of(const Args &a, int len, int n, int row) { return a.p.causal ? len - n + row + 1 : len; }
-
-__device__ __forceinline__ int64_t wave_scan(int64_t x) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const int64_t y = __shfl_up(x, o, kWave);
-    if (lane >= o) x += y;
-  }
-  return x;
-}
-__device__ __forceinline__ int64_t uniform64(int64_t x) {
-  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
-}
-
-// a / b, and *rest: exact below 2^52.
-__device__ __forceinline__ int64_t divide(int64_t a, int b, int64_t *rest) {
-  int64_t q = (int64_t)((double)a / (double)b), r = a - q * b;   // at most one off
-  if (r < 0) { --q; r += b; }
-  if (r >= b) { ++q; r -= b; }
-  *rest = r;
-  return q;
-}
-
-// A worker's place: items [at, end) of the line, `at` in request b, whose first item is `first`.
-struct Place {
-  int64_t at, end, first, share;
-  int b;
-  bool whole;                             // the line is of triples
-};
-
-// The request that item `at` belongs to, and its first item.
-template <class I>
-__device__ __forceinline__ int find_request(const Args &a, int64_t at, bool whole, int64_t *first) {
-  const int lane = threadIdx.x & 63;
-  int64_t base = 0;
-  for (int b0 = 0;; b0 += kWave) {
-    const int b = b0 + lane;
-    const int64_t items = b < a.p.B ? request<I>(a, b, whole).items : 0, upto = base + wave_scan(items);
-    const uint64_t beyond = __builtin_amdgcn_ballot_w64(upto > at);
-    if (beyond || b0 + kWave >= a.p.B) {
-      const int l = beyond ? __builtin_ctzll(beyond) : 63;
-      *first = uniform64(__shfl(upto - items, l, kWave));
-      return __builtin_amdgcn_readfirstlane(min(b0 + l, a.p.B - 1));
-    }
-    base = uniform64(__shfl(upto, 63, kWave));
-  }
-}
-
-// Triples stay whole where the host says so, and on kSnap instances, whose partial results are large, where that divides the work well enough:
-// none is longer than kSnap shares, and there are no more of them than workers, or several for each.
-template <class I>
-__device__ __forceinline__ Place place_of(const Args &a, int block, int workers, int *worker) {
-  const int lane = threadIdx.x & 63;
-  int64_t items = 0, triples = 0;
-  int longest = 0;
-  for (int b = lane; b < a.p.B; b += kWave) {
-    const Request r = request<I>(a, b, a.whole);
-    items += r.items;
-    triples += r.triples;
-    longest = max(longest, r.n > 0 ? r.steps : 0);
-  }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    items += __shfl_xor(items, o, kWave);
-    if (I::kSnap > 0) triples += __shfl_xor(triples, o, kWave);
-    if (I::kSnap > 0) longest = max(longest, __shfl_xor(longest, o, kWave));
-  }
-  items = uniform64(items);
-  Place w;
-  int64_t rest;
-  w.share = divide(items + workers - 1, workers, &rest);
-  w.whole = a.whole;
-  if (I::kSnap > 0 && !a.whole) {
-    triples = uniform64(triples);
-    if (__builtin_amdgcn_readfirstlane(longest) <= I::kSnap * w.share && (triples <= workers || triples >= 4 * (int64_t)workers)) {
-      w.whole = true;
-      items = triples;
-      w.share = divide(items + workers - 1, workers, &rest);
-    }
-  }
-  // workers that follow each other read the same keys for other columns: where all take part, neighbours run on one XCD and share its L2
-  *worker = workers % 8 == 0 && w.share * (workers - 1) < items ? block % 8 * (workers / 8) + block / 8 : block;
-  w.at = w.share * *worker;
-  w.end = min(w.at + w.share, items);
-  if (w.at < w.end) w.b = find_request<I>(a, w.at, w.whole, &w.first);
-  return w;
-}
 
 // The part of a triple that a worker takes next.
 struct Piece {
@@ -152,35 +59,120 @@ struct Piece {
   bool done, begun;                       // all of it; from its first step on
 };
 
-// False: nothing is left (or lengths changed under the call).  b and r follow.
+// The line, 64 requests at a time, one a lane, and a worker's place on it.  Triples are below 2^31 (rows and heads together are); a line of that many
+// steps is one of whole triples.
 template <class I>
-__device__ __forceinline__ bool next_piece(const Args &a, Place &w, Request &r, Piece &p) {
-  if (w.at >= w.end) return false;
-  while (w.at - w.first >= r.items) {
-    w.first += r.items;
-    if (++w.b >= a.p.B) return false;
-    r = request<I>(a, w.b, w.whole);
+struct Line {
+  const Args &a;
+  int row0, n, len;                       // this lane's; row0 with kOver set: longer than its table
+  uint32_t upto, base;                    // items up to it and its own; in front of these 64
+  int b0, b;                              // the first of these 64; the request of the last piece
+  bool whole;                             // items are triples, not steps of them
+  uint32_t at, end, share;
+
+  static constexpr int kOver = 1 << 30;
+
+  __device__ __forceinline__ static int steps_of(int len) { return max((len + I::kStep - 1) / I::kStep, 1); }
+  __device__ __forceinline__ int tiles_of(int rows) const { return (int)(((uint32_t)(rows * a.group) + I::QT - 1) / I::QT); }
+  __device__ __forceinline__ uint32_t triples_of(int rows) const { return (uint32_t)tiles_of(rows) * (uint32_t)a.p.Hkv; }
+  __device__ __forceinline__ uint32_t items_of(int rows, int keys) const { return triples_of(rows) * (whole ? 1u : (uint32_t)steps_of(keys)); }
+
+  __device__ __forceinline__ void load(int from) {
+    b0 = from;
+    const int i = from + (threadIdx.x & 63);
+    row0 = n = len = 0;
+    if (i < a.p.B) {
+      const int raw = a.p.seq_len[i], most = a.p.width * a.p.page_size;
+      int r0 = i, r1 = i + 1;
+      if (a.p.cu_rows) {
+        r0 = a.p.cu_rows[i];
+        r1 = a.p.cu_rows[i + 1];
+      }
+      row0 = min(max(r0, 0), a.p.M);
+      n = max(min(r1, a.p.M) - row0, 0);
+      len = min(max(raw, 0), most);
+      if (raw > most) row0 |= kOver;
+    }
   }
-  int64_t triple = w.at - w.first;
-  if (w.whole) {
+
+  // Triples stay whole where the host says so, and on kSnap instances, whose partial results are large, where that divides the work well enough:
+  // none is longer than kSnap shares, and there are no more of them than workers, or several for each.
+  __device__ __forceinline__ Line(const Args &args, int block, int workers, int *worker) : a(args) {
+    whole = a.whole;
+    uint32_t sum = 0, all_triples = 0;
+    int longest = 0;
+    for (int from = 0; from < a.p.B; from += kWave) {
+      load(from);
+      const uint32_t mine = items_of(n, len);
+      sum = __builtin_elementwise_add_sat(sum, !whole && __umulhi(triples_of(n), (uint32_t)steps_of(len)) ? 0xffffffffu : mine);
+      if (I::kSnap > 0) {
+        longest = max(longest, n > 0 ? steps_of(len) : 0);
+      }
+      all_triples += triples_of(n);
+    }
+    uint32_t all = last_lane(wave_scan(sum));
+    share = (all + workers - 1) / (uint32_t)workers;
+    if (!whole && (I::kSnap > 0 || all >> 31)) {
+      const uint32_t t = last_lane(wave_scan(all_triples));
+      if (all >> 31 || (__builtin_amdgcn_ballot_w64((uint32_t)longest > I::kSnap * share) == 0 && (t <= (uint32_t)workers || t / 4 >= (uint32_t)workers))) {
+        whole = true;
+        all = t;
+        share = (all + workers - 1) / (uint32_t)workers;
+      }
+    }
+    // workers that follow each other read the same keys for other columns: where all take part, neighbours run on one XCD and share its L2
+    *worker = workers % 8 == 0 && share * (uint32_t)(workers - 1) < all ? block % 8 * (workers / 8) + block / 8 : block;
+    at = min(share * (uint32_t)*worker, all);
+    end = min(at + share, all);
+    base = 0;
+    if (a.p.B > kWave) load(0);
+    upto = wave_scan(items_of(n, len));
+  }
+
+  // False: nothing is left.  (A b that leaves the requests, or a head: lengths have changed under the call.)
+  __device__ __forceinline__ bool next(Request &r, Piece &p) {
+    if (at >= end) return false;
+    uint64_t beyond;
+    while (beyond = __builtin_amdgcn_ballot_w64(upto > at), beyond == 0) {
+      base = last_lane(upto);
+      if (b0 + kWave >= a.p.B) return false;
+      load(b0 + kWave);
+      upto = base + wave_scan(items_of(n, len));
+    }
+    const int l = __builtin_ctzll(beyond);
+    auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
+    b = b0 + l;
+    r.row0 = of(row0) & ~kOver;
+    r.over = (of(row0) & kOver) != 0;
+    r.n = of(n);
+    r.len = of(len);
+    r.steps = steps_of(r.len);
+    r.tiles = tiles_of(r.n);
+    const uint32_t rel = at - ((uint32_t)of((int)upto) - items_of(r.n, r.len));
+    uint32_t triple = rel;
     p.step0 = 0;
     p.step1 = r.steps;
-    ++w.at;
-  } else {
-    int64_t step0;
-    triple = divide(triple, r.steps, &step0);
-    p.step0 = (int)step0;
-    p.step1 = (int)min((int64_t)r.steps, p.step0 + (w.end - w.at));
-    w.at += p.step1 - p.step0;
+    if (!whole) {
+      triple = rel / (uint32_t)r.steps;
+      p.step0 = (int)(rel - triple * (uint32_t)r.steps);
+      p.step1 = (int)min((uint32_t)r.steps, p.step0 + (end - at));
+    }
+    at += whole ? 1 : p.step1 - p.step0;
+    p.head = (int)(triple / (uint32_t)r.tiles);
+    p.tile = (int)(triple - (uint32_t)p.head * (uint32_t)r.tiles);
+    p.cols = min(I::QT, r.n * a.group - p.tile * I::QT);
+    p.begun = p.step0 == 0;
+    p.done = p.begun && p.step1 == r.steps;
+    return p.head < a.p.Hkv;
   }
-  p.head = (int)((uint32_t)triple / (uint32_t)r.tiles);        // rows and heads together are below 2^31
-  p.tile = (int)((uint32_t)triple - (uint32_t)p.head * r.tiles);
-  if (p.head >= a.p.Hkv) return false;                         // cannot be, unless lengths change under the call
-  p.cols = min(I::QT, r.n * a.group - p.tile * I::QT);
-  p.begun = p.step0 == 0;
-  p.done = p.begun && p.step1 == r.steps;
-  return true;
-}
+
+  // Notes how many workers take a triple that this one begins: others end it, `share` steps each.
+  __device__ __forceinline__ void note_join(int worker, const Request &r, const Piece &p) const {
+    int32_t *j = a.joins + (int64_t)worker * kJoinInts;
+    *(int4 *)(j + 4) = make_int4(p.head, p.tile, 0, 0);
+    *(int4 *)j = make_int4((int)((r.steps - p.step1 + share - 1) / share) + 1, r.row0, r.n, r.len);
+  }
+};
 
 // Where a column's row and head begin in q or out.
 __device__ __forceinline__ int64_t row_place(const Args &a, int row0, int head, int pair, int64_t stride, int *row) {
@@ -193,16 +185,6 @@ __device__ __forceinline__ int64_t row_place(const Args &a, int row0, int head, 
 // Partial results: worker w has two, 2 w: of the triple that an earlier worker began, 2 w + 1: of the one that it begins itself.
 template <class I>
 __device__ __forceinline__ float *partial(const Args &a, int worker, bool begun) { return a.p.ws + (int64_t)(2 * worker + begun) * I::kSlotFloats; }
-
-// How many workers take a triple that this one begins.
-template <class I>
-__device__ __forceinline__ void note_join(const Args &a, int worker, const Place &w, const Request &r, const Piece &p) {
-  const int64_t behind = r.steps - p.step1;                    // items that other workers take, w.share each
-  int32_t *j = a.joins + (int64_t)worker * kJoinInts;
-  int64_t rest;
-  *(int4 *)(j + 4) = make_int4(p.head, p.tile, 0, 0);
-  *(int4 *)j = make_int4((int)divide(behind + w.share - 1, (int)w.share, &rest) + 1, r.row0, r.n, r.len);
-}
 
 template <typename T>
 __device__ __forceinline__ void store4(T *dst, floatx4 x, float inv_total, bool none) {
@@ -219,19 +201,24 @@ __device__ __forceinline__ float weight(const Args &a, float m, float ref) { ret
 // Where a key lies, from the table entries in LDS; *none: on no page (page 0 is read).
 __device__ __forceinline__ int page_of(const Args &a, int key) { return (int)(__umulhi((uint32_t)(key >> 3) << 1, a.div_mul) >> a.div_shift); }
 
-// Table entries of keys k0 .. k1 - 1 into LDS, -1 for what is no page; every thread's answer: whether one of its entries is.
-__device__ __forceinline__ bool load_pages(const Args &a, int b, int k0, int k1, int first_page, int32_t *s_pages) {
+// Table entries of keys k0 .. k1 - 1 into LDS, -1 for what is no page; *s_bad (zero before) becomes one if there is such.
+__device__ __forceinline__ void load_pages(const Args &a, int b, int k0, int k1, int first_page, int32_t *s_pages, int32_t *s_bad) {
   const int n = k1 > k0 ? page_of(a, k1 - 1) - first_page + 1 : 0;
-  bool bad = false;
+  const int32_t *row = a.p.table + (int64_t)b * a.p.table_stride + first_page;
   for (int i = threadIdx.x; i < n; i += 256) {
-    const int j = first_page + i;
     int id = -1;
-    if (j < a.p.width) id = a.p.table[(int64_t)b * a.p.table_stride + j];
-    const bool there = id >= 0 && id < a.p.n_pages;
+    if (first_page + i < a.p.width) id = row[i];
+    const bool there = (uint32_t)id < (uint32_t)a.p.n_pages;
     s_pages[i] = there ? id : -1;
-    bad |= !there;
+    if (!there) *s_bad = 1;
   }
-  return bad;
+}
+// Every wave's LDS accesses so far are done; loads from global memory stay on their way.
+__device__ __forceinline__ void meet() {
+  __builtin_amdgcn_s_waitcnt(0xc07f);     // lgkmcnt(0)
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
 }
 
 __device__ __forceinline__ bool bf16s_not_finite(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
@@ -352,7 +339,8 @@ Plan plan(int B, int M, int Hkv, int group, int width, int page_size) {
   return p;
 }
 template <class I>
-int64_t workspace_bytes(const Plan &p) {
+int64_t workspace_bytes(int B, int M, int Hkv, int group, int width, int page_size) {
+  const Plan p = plan<I>(B, M, Hkv, group, width, page_size);
   return p.whole || p.workers == 1 ? 0 : p.workers * kPartialBytes<I>;
 }
 

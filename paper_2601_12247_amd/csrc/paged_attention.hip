@@ -269,14 +269,14 @@ page_attention_kernel(Args a) {
   __shared__ float s_m[4][I::QT], s_l[4][I::QT];
   __shared__ alignas(16) float s_o[4][16][I::kOPad];
   const int tid = threadIdx.x, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
+  __shared__ int32_t s_bad;
   int worker;
-  Place w = place_of<I>(a, blockIdx.x, gridDim.x, &worker);
+  Line<I> line(a, blockIdx.x, gridDim.x, &worker);
   if (!a.whole && tid == 0) a.joins[(int64_t)worker * kJoinInts] = 0;
-  if (w.at >= w.end) return;
-  Request r = request<I>(a, w.b, w.whole);
+  Request r;
   Piece piece;
   Pass<T, DH, NQ, kWhole> pass(a, s_pages);
-  while (next_piece<I>(a, w, r, piece)) {
+  while (line.next(r, piece)) {
     const int cols = piece.cols;
     pass.len = r.len;
     pass.over = r.over;
@@ -308,10 +308,10 @@ page_attention_kernel(Args a) {
     for (int s0 = piece.step0; s0 < piece.step1; s0 += a.chunk_steps) {
       const int s1 = min(piece.step1, s0 + min(a.chunk_steps, piece.step1 - s0));
       const int k0 = s0 * I::kStep, k1 = (int)min((int64_t)r.len, (int64_t)s1 * I::kStep);
-      __syncthreads();                    // the last chunk's pages, or the last piece's results, have been read
+      meet();                             // the last chunk's pages, or the last piece's results, have been read
       pass.first_page = page_of(a, k0);
-      load_pages(a, w.b, k0, k1, pass.first_page, s_pages);
-      __syncthreads();
+      load_pages(a, line.b, k0, k1, pass.first_page, s_pages, &s_bad);
+      meet();
       int kb = k0 + wid * I::KT;
       if (kb < k1) {
         pass.load_keys(kb);
@@ -372,7 +372,7 @@ page_attention_kernel(Args a) {
         }
       }
     }
-    if (!piece.done && piece.begun && tid == 0) note_join<I>(a, worker, w, r, piece);
+    if (!piece.done && piece.begun && tid == 0) line.note_join(worker, r, piece);
   }
 }
 
@@ -415,7 +415,7 @@ int64_t page_attention_workspace(int dtype, int B, int M, int H, int Hkv, int dh
   if (page::is_wide(dtype, pairs, dh)) return page::wide_workspace(B, M, Hkv, group, dh, width, page_size, pairs);
   return page::with_instance(dtype, pairs, dh, [&](auto inst) {
     typedef decltype(inst) I;
-    return page::workspace_bytes<I>(page::plan<I>(B, M, Hkv, group, width, page_size));
+    return page::workspace_bytes<I>(B, M, Hkv, group, width, page_size);
   });
 }
 

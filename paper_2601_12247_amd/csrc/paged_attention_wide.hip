@@ -5,8 +5,8 @@
 // 32 x 32 x 16 matrix instructions.  A lane of S^T holds one column and keys 8 (e / 4) + 4 (lane / 32) + e % 4; P^T is multiplied as it is held, with V^T's
 // keys in that order: transposing reads give a lane four keys of one dimension.
 //
-// LDS rows are keys, in 16-byte chunks; chunk x of a key lies at x ^ turn(key), so that 16 keys' equal chunks (the operand K) and 8 keys' neighbouring
-// ones (V^T) fall on all banks.
+// LDS rows are keys, in 16-byte chunks; chunk x of a key lies at x ^ turn(key), so that equal chunks of 8 keys (the operand K) and pairs of chunks of 4 keys
+// (V^T) fall on different banks.
 #include "paged_attention.h"
 
 namespace pvf {
@@ -51,14 +51,14 @@ page_attention_wide_kernel(Args a) {
   __shared__ int32_t s_pages[kPageSlots];
   const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int cw = wid % CW, kw = wid / CW, fr = lane & 31, fh = lane >> 5;
+  __shared__ int32_t s_bad;
   int worker;
-  Place w = place_of<I>(a, blockIdx.x, gridDim.x, &worker);
+  Line<I> line(a, blockIdx.x, gridDim.x, &worker);
   if (!a.whole && tid == 0) a.joins[(int64_t)worker * kJoinInts] = 0;
-  if (w.at >= w.end) return;
-  Request r = request<I>(a, w.b, w.whole);
+  Request r;
   Piece piece;
 
-  auto turn = [](int key) { return I::kChunks == 16 ? (key & 3) << 2 | (key >> 2 & 3) : (key >> 1 & 1) << 2 | (key >> 2 & 3); };
+  auto turn = [](int key) { return (key & 3) << 1 | (key >> 2 & 1) | (I::kChunks == 16 ? key & 8 : 0); };
   // operand K: key fr of 32, chunk 2 j + fh.  Operand V^T: of 16 lanes, lane 4 k + x reads dimensions 4 x .. of key k; keys 4 fh .. (and 8 behind
   // them), dimensions 32 t + 16 (lane / 16 % 2) + ..
   int k_rd[I::KJ], v_rd[I::NT][2];
@@ -76,7 +76,7 @@ page_attention_wide_kernel(Args a) {
   const int lane_key = wid * I::kKeys + lane / I::kChunks, lane_chunk = lane % I::kChunks ^ turn(lane_key);
   const uint32_t lane_bytes = (uint32_t)((lane / I::kChunks) * a.p.dh + lane_chunk * 8) * 2;
 
-  while (next_piece<I>(a, w, r, piece)) {
+  while (line.next(r, piece)) {
     const int cols = piece.cols, len = r.len, col = 32 * cw + fr;
     const bf16_t *kbase = (const bf16_t *)a.p.k_cache + (int64_t)piece.head * a.p.page_size * a.p.dh;
     const bf16_t *vbase = (const bf16_t *)a.p.v_cache + (int64_t)piece.head * a.p.page_size * a.p.dh;
@@ -97,7 +97,7 @@ page_attention_wide_kernel(Args a) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[t][e] = 0.f;
     float m = -INFINITY, l = 0.f;
-    __syncthreads();                      // the last piece's results have been read
+    meet();                               // the last piece's results have been read
     if (!kWhole) {                        // chunks behind d_head: nothing is loaded there, and q is zero beside them
       for (int i = tid; i < 4 * I::kTile / 16; i += 256) *(uint4 *)(lds + 16 * i) = make_uint4(0, 0, 0, 0);
     }
@@ -105,25 +105,32 @@ page_attention_wide_kernel(Args a) {
     for (int s0 = piece.step0; s0 < piece.step1; s0 += a.chunk_steps) {
       const int s1 = min(piece.step1, s0 + min(a.chunk_steps, piece.step1 - s0));
       const int k0 = s0 * I::kStep, k1 = (int)min((int64_t)len, (int64_t)s1 * I::kStep);
-      __syncthreads();                    // the last chunk's pages and tiles have been read
+      if (tid == 0) s_bad = 0;
+      meet();                             // the last chunk's pages and tiles have been read
       const int first_page = page_of(a, k0);
-      const bool bad = __syncthreads_or(load_pages(a, w.b, k0, k1, first_page, s_pages)) != 0 || r.over;
+      load_pages(a, line.b, k0, k1, first_page, s_pages, &s_bad);
+      meet();
+      const bool bad = __builtin_amdgcn_readfirstlane(s_bad) != 0 || r.over;
       if (k1 <= k0) continue;             // a request without keys
 
-      // 64 keys from kb on (or their values), kKeys neighbouring ones a load: they share a page, which is looked up once a wave.  What lies behind the
-      // last key comes along.
-      auto load = [&](const bf16_t *base, int64_t page_stride, int kb, uint32_t dst) {
+      // 64 keys from kb on, or their values, kKeys neighbouring ones a load: they share a page.  Lane i finds where the wave's i-th load begins, for
+      // keys and values at once.  What lies behind the last key comes along.
+      const uint32_t lds_at = (uint32_t)(uintptr_t)(lptr_t *)lds + wid * 1024;
+      int64_t values_at = 0;
+      auto load = [&](int64_t at, uint32_t dst) {
 #pragma unroll
         for (int i = 0; i < I::kLoads; ++i) {
-          const int key = min(kb + (i * 4 + wid) * I::kKeys, (len - 1) & ~(I::kKeys - 1)), page = page_of(a, key);
-          const int id = max(__builtin_amdgcn_readfirstlane(s_pages[page - first_page]), 0);
-          const bf16_t *src = base + (int64_t)id * page_stride + (key - page * a.p.page_size) * a.p.dh;
-          if (kWhole || lane_chunk * 8 < a.p.dh) load_to_lds(src, lane_bytes, dst + (i * 4 + wid) * 1024);
+          const uint32_t lo = __builtin_amdgcn_readlane((int)at, i), hi = __builtin_amdgcn_readlane((int)(at >> 32), i);
+          if (kWhole || lane_chunk * 8 < a.p.dh) load_to_lds((const void *)((uint64_t)hi << 32 | lo), lane_bytes, dst + i * 4096);
         }
       };
-      const uint32_t lds_at = (uint32_t)(uintptr_t)(lptr_t *)lds;
-      auto load_keys = [&](int kb, int buf) { load(kbase, a.p.k_page_stride, kb, lds_at + buf * 2 * I::kTile); };
-      auto load_values = [&](int kb, int buf) { load(vbase, a.p.v_page_stride, kb, lds_at + (buf * 2 + 1) * I::kTile); };
+      auto load_keys = [&](int kb, int buf) {
+        const int key = min(kb + (lane % I::kLoads * 4 + wid) * I::kKeys, (len - 1) & ~(I::kKeys - 1)), page = page_of(a, key);
+        const int id = max(s_pages[page - first_page], 0), off = (key - page * a.p.page_size) * a.p.dh;
+        values_at = (int64_t)(vbase + (int64_t)id * a.p.v_page_stride + off);
+        load((int64_t)(kbase + (int64_t)id * a.p.k_page_stride + off), lds_at + buf * 2 * I::kTile);
+      };
+      auto load_values = [&](int buf) { load(values_at, lds_at + (buf * 2 + 1) * I::kTile); };   // of the keys asked for last
 
       // Keys and values of a step are asked for two steps ahead, each when its buffer has been read: three tiles are on the way at most, and waits are
       // for the oldest (the last two steps': for all).  The keys of this step are awaited before it begins.
@@ -158,7 +165,7 @@ page_attention_wide_kernel(Args a) {
         if (more) wait_and_meet<2 * I::kLoads>(); else wait_and_meet<0>();     // its values are there, its keys have been read
         if (more) load_keys(kb + 2 * I::kStep, kBuf);
         bool odd = false;
-        if (kb + I::kStep > least) {
+        if (__builtin_expect(kb + I::kStep > least, 0)) {
           // The tile holds keys that a row does not see, or copies of the last one.  0 times an infinity is no zero: values that are not finite
           // leave it and are added to the columns that see them, by themselves.
           bool mine = false;
@@ -172,7 +179,7 @@ page_attention_wide_kernel(Args a) {
           odd = __syncthreads_or(mine) != 0;
         }
         auto key_of = [&](int u, int e) { return kb + 32 * (u * I::KW + kw) + 8 * (e / 4) + 4 * fh + e % 4; };
-        if (bad) {                                             // four keys from a multiple of four on share a page
+        if (__builtin_expect(bad, 0)) {                                             // four keys from a multiple of four on share a page
 #pragma unroll
           for (int u = 0; u < I::kSubs; ++u)
 #pragma unroll
@@ -182,7 +189,7 @@ page_attention_wide_kernel(Args a) {
               for (int i = 0; i < 4; ++i) s[u][e + i] = none ? NAN : s[u][e + i];
             }
         }
-        if (kb + I::kStep > least) {
+        if (__builtin_expect(kb + I::kStep > least, 0)) {
 #pragma unroll
           for (int u = 0; u < I::kSubs; ++u)
 #pragma unroll
@@ -199,22 +206,14 @@ page_attention_wide_kernel(Args a) {
         const bool up = (top - m) * a.c > 8.0f;                // the first time m = -inf
         const float now = up ? top : m, ref = reference(now), alpha = up ? weight(a, m, now) : 1.0f, less = -ref * a.c;
         m = now;
-        float sum = 0.f;
-#pragma unroll
-        for (int u = 0; u < I::kSubs; ++u)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            s[u][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][e], a.c, less));
-            sum += s[u][e];
-          }
-        l = l * alpha + sum;
+        l *= alpha;
         if (__builtin_amdgcn_ballot_w64(alpha != 1.0f) != 0) {
 #pragma unroll
           for (int t = 0; t < I::NT; ++t)
 #pragma unroll
             for (int e = 0; e < 16; ++e) o[t][e] *= alpha;
         }
-        if (odd) {
+        if (__builtin_expect(odd, 0)) {
 #pragma unroll 1
           for (int x = 0; x < 64 && kb + x < len; ++x) {
             if (I::KW == 2 && x / 32 != kw) continue;
@@ -234,7 +233,9 @@ page_attention_wide_kernel(Args a) {
               }
           }
         }
-        // 16 keys at a time, the next ones' operands read ahead
+        // 16 keys at a time: while their values are multiplied, the next ones' operands are read and their probabilities computed, which takes the vector
+        // unit as long as the products take the matrix unit
+        constexpr int kBlocks = 2 * I::kSubs;
         bf16x8 vt[2][I::NT];
         auto read_values = [&](int k) {
           const int at = (32 * (k / 2 * I::KW + kw) + 16 * (k % 2)) * I::kRow;
@@ -244,28 +245,51 @@ page_attention_wide_kernel(Args a) {
             const short4v v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((trptr_t)(vs + at + v_rd[t][1]));
             vt[k % 2][t] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
           }
-          __builtin_amdgcn_sched_barrier(0);
+        };
+        float p[8];
+        auto exponential = [&](int k, int i) { p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k / 2][8 * (k % 2) + i], a.c, less)); };
+        struct Parts { uint32_t w[4]; } hi[2], lo[2];          // P^T's two operands of 16 keys
+        auto take = [&](int k, int i) {                        // the i-th of 8
+          l += p[i];
+          if (i % 2) {
+            hi[k % 2].w[i / 2] = upper_parts(p[i - 1], p[i]);
+            lo[k % 2].w[i / 2] = lower_parts(p[i - 1], p[i]);
+          }
         };
         read_values(0);
 #pragma unroll
-        for (int k = 0; k < 2 * I::kSubs; ++k) {
-          if (k + 1 < 2 * I::kSubs) read_values(k + 1);
-          auto p = [&](int i) { return s[k / 2][8 * (k % 2) + i]; };
-          const bf16x8 hi = __builtin_bit_cast(bf16x8, make_uint4(upper_parts(p(0), p(1)), upper_parts(p(2), p(3)), upper_parts(p(4), p(5)), upper_parts(p(6), p(7))));
-          const bf16x8 lo = __builtin_bit_cast(bf16x8, make_uint4(lower_parts(p(0), p(1)), lower_parts(p(2), p(3)), lower_parts(p(4), p(5)), lower_parts(p(6), p(7))));
+        for (int i = 0; i < 8; ++i) exponential(0, i);
 #pragma unroll
-          for (int t = 0; t < I::NT; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt[k % 2][t], hi, o[t], 0, 0, 0);
+        for (int i = 0; i < 8; ++i) take(0, i);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int t = 0; t < I::NT; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt[k % 2][t], lo, o[t], 0, 0, 0);
+        for (int k = 0; k < kBlocks; ++k) {
+          const bool more_blocks = k + 1 < kBlocks;
+          if (more_blocks) read_values(k + 1);
+          constexpr int kProducts = 2 * I::NT, kEach = 8 / kProducts;   // probabilities beside a product
+#pragma unroll
+          for (int i = 0; i < kProducts; ++i) {
+            const int t = i % I::NT;
+            o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt[k % 2][t], __builtin_bit_cast(bf16x8, i < I::NT ? hi[k % 2] : lo[k % 2]), o[t], 0, 0, 0);
+            if (more_blocks) {
+#pragma unroll
+              for (int x = kEach * i; x < kEach * (i + 1); ++x) {
+                exponential(k + 1, x);
+                if (x > 0) take(k + 1, x - 1);
+              }
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          }
+          if (more_blocks) take(k + 1, 7);
         }
       };
       __builtin_amdgcn_s_waitcnt(0x0f70);                      // vmcnt(0): nothing else is counted from here on
       load_keys(k0, 0);
-      load_values(k0, 0);
+      load_values(0);
       const bool two = k0 < k1 - I::kStep;
       if (two) {
         load_keys(k0 + I::kStep, 1);
-        load_values(k0 + I::kStep, 1);
+        load_values(1);
         wait_and_meet<3 * I::kLoads>();
       } else {
         wait_and_meet<I::kLoads>();
@@ -275,7 +299,7 @@ page_attention_wide_kernel(Args a) {
         if (kb >= k1 - I::kStep) break;
         if (kb < k1 - 2 * I::kStep) {
           wait_and_meet<2 * I::kLoads>(); // the next step's keys are there, this one's values have been read
-          load_values(kb + 2 * I::kStep, 0);
+          load_values(0);
         } else {
           wait_and_meet<0>();
         }
@@ -284,7 +308,7 @@ page_attention_wide_kernel(Args a) {
         if (kb >= k1 - I::kStep) break;
         if (kb < k1 - 2 * I::kStep) {
           wait_and_meet<2 * I::kLoads>();
-          load_values(kb + 2 * I::kStep, 1);
+          load_values(1);
         } else {
           wait_and_meet<0>();
         }
@@ -343,7 +367,7 @@ page_attention_wide_kernel(Args a) {
           }
       }
     }
-    if (!piece.done && piece.begun && tid == 0) note_join<I>(a, worker, w, r, piece);
+    if (!piece.done && piece.begun && tid == 0) line.note_join(worker, r, piece);
   }
 }
 
@@ -375,7 +399,7 @@ pvf_status launch_wide(hipStream_t s, Args &a, int64_t pairs) {
 int64_t wide_workspace(int B, int M, int Hkv, int group, int dh, int width, int page_size, int64_t pairs) {
   return with_wide(pairs, dh, [&](auto inst) {
     typedef decltype(inst) I;
-    return workspace_bytes<I>(plan<I>(B, M, Hkv, group, width, page_size));
+    return workspace_bytes<I>(B, M, Hkv, group, width, page_size);
   });
 }
 
