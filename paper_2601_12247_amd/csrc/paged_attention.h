@@ -16,6 +16,7 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 constexpr int kPageSlots = 1024;          // table entries in LDS
+constexpr int kCus = 256;
 template <int N>
 struct Const { static constexpr int value = N; };
 
@@ -69,6 +70,7 @@ struct Line {
   int b0, b;                              // the first of these 64; the request of the last piece
   bool whole;                             // items are triples, not steps of them
   uint32_t at, end, share;
+  uint32_t rest_at, rest_end;             // the worker's items of steps behind those, of triples that are divided
 
   static constexpr int kOver = 1 << 30;
 
@@ -95,8 +97,9 @@ struct Line {
     }
   }
 
-  // Triples stay whole where the host says so, and on kSnap instances, whose partial results are large, where that divides the work well enough:
-  // none is longer than kSnap shares, and there are no more of them than workers, or several for each.
+  // Triples stay whole where the host says so, and on instances with large partial results as far as they can be dealt out evenly: unless one is longer
+  // than a CU's part of all steps by more than kSplit (what dividing costs, in steps), each CU takes one, or every worker the same number; the
+  // others are divided, between the workers that have none, or all.
   __device__ __forceinline__ Line(const Args &args, int block, int workers, int *worker) : a(args) {
     whole = a.whole;
     uint32_t sum = 0, all_triples = 0;
@@ -105,25 +108,62 @@ struct Line {
       load(from);
       const uint32_t mine = items_of(n, len);
       sum = __builtin_elementwise_add_sat(sum, !whole && __umulhi(triples_of(n), (uint32_t)steps_of(len)) ? 0xffffffffu : mine);
-      if (I::kSnap > 0) {
-        longest = max(longest, n > 0 ? steps_of(len) : 0);
-      }
+      if (I::kSplit > 0) longest = max(longest, n > 0 ? steps_of(len) : 0);
       all_triples += triples_of(n);
     }
     uint32_t all = last_lane(wave_scan(sum));
     share = (all + workers - 1) / (uint32_t)workers;
-    if (!whole && (I::kSnap > 0 || all >> 31)) {
-      const uint32_t t = last_lane(wave_scan(all_triples));
-      if (all >> 31 || (__builtin_amdgcn_ballot_w64((uint32_t)longest > I::kSnap * share) == 0 && (t <= (uint32_t)workers || t / 4 >= (uint32_t)workers))) {
+    *worker = block;
+    base = rest_at = rest_end = 0;
+    const bool counted = whole || all >> 31;
+    if (!counted && I::kSplit > 0 && __builtin_amdgcn_ballot_w64((uint32_t)longest > all / kCus + I::kSplit) == 0) {
+      const uint32_t t = last_lane(wave_scan(all_triples)), takers = t < (uint32_t)(workers - workers / 8) ? min(workers, kCus) : workers, each = t < takers ? 1 : t / takers;
+      const uint32_t dealt = min(t, takers * each), others = dealt == t ? 0 : takers < (uint32_t)workers ? workers - takers : takers;
+      if (others == 0 || dealt >= t / 2) {
+        if (others > 0) {                 // steps of the triples that are dealt out lie in front of the others'
+          whole = false;
+          if (a.p.B > kWave) load(0);
+          uint32_t t0 = 0, s0 = 0;
+          for (;;) {
+            const uint32_t t1 = t0 + wave_scan(triples_of(n)), s1 = s0 + wave_scan(items_of(n, len));
+            const uint64_t beyond = __builtin_amdgcn_ballot_w64(t1 > dealt);
+            if (beyond || b0 + kWave >= a.p.B) {
+              const int l = beyond ? __builtin_ctzll(beyond) : 63;
+              const uint32_t behind = (uint32_t)__builtin_amdgcn_readlane((int)t1, l) - dealt;      // of this request's triples
+              s0 = (uint32_t)__builtin_amdgcn_readlane((int)s1, l) - behind * (uint32_t)steps_of(__builtin_amdgcn_readlane(len, l));
+              break;
+            }
+            t0 = last_lane(t1);
+            s0 = last_lane(s1);
+            load(b0 + kWave);
+          }
+          share = (all - s0 + others - 1) / others;
+          const uint32_t k = takers < (uint32_t)workers ? (uint32_t)block - takers : (uint32_t)block;   // which of the others; takers have none where that wraps
+          if (k < others) {
+            rest_at = min(s0 + share * k, all);
+            rest_end = min(rest_at + share, all);
+          }
+        }
         whole = true;
-        all = t;
-        share = (all + workers - 1) / (uint32_t)workers;
+        at = (uint32_t)block < takers ? min((uint32_t)block * each, dealt) : dealt;
+        end = min(at + each, dealt);
+        begin();
+        return;
       }
     }
+    if (counted && !whole) {
+      whole = true;
+      all = last_lane(wave_scan(all_triples));
+      share = (all + workers - 1) / (uint32_t)workers;
+    }
     // workers that follow each other read the same keys for other columns: where all take part, neighbours run on one XCD and share its L2
-    *worker = workers % 8 == 0 && share * (uint32_t)(workers - 1) < all ? block % 8 * (workers / 8) + block / 8 : block;
+    if (workers % 8 == 0 && share * (uint32_t)(workers - 1) < all) *worker = block % 8 * (workers / 8) + block / 8;
     at = min(share * (uint32_t)*worker, all);
     end = min(at + share, all);
+    begin();
+  }
+
+  __device__ __forceinline__ void begin() {
     base = 0;
     if (a.p.B > kWave) load(0);
     upto = wave_scan(items_of(n, len));
@@ -131,7 +171,14 @@ struct Line {
 
   // False: nothing is left.  (A b that leaves the requests, or a head: lengths have changed under the call.)
   __device__ __forceinline__ bool next(Request &r, Piece &p) {
-    if (at >= end) return false;
+    if (at >= end) {
+      if (rest_at >= rest_end) return false;
+      at = rest_at;
+      end = rest_end;
+      rest_end = 0;
+      whole = false;
+      begin();
+    }
     uint64_t beyond;
     while (beyond = __builtin_amdgcn_ballot_w64(upto > at), beyond == 0) {
       base = last_lane(upto);
@@ -241,47 +288,57 @@ __device__ __forceinline__ uint32_t lower_parts(float x, float y) {
 }
 
 // ---- the join: block w joins the triple that worker w begins, if others end it ----------------------
-constexpr int kJoinThreads = 512;
+constexpr int kJoinThreads = 1024;
+template <class I>
+constexpr int kJoinCols = I::QT < 32 ? I::QT : 32;   // columns of a block
 
 template <typename T, class I>
 __global__ void __launch_bounds__(kJoinThreads)
 page_attention_join_kernel(Args a) {
-  constexpr int DH = I::kDh, QT = I::QT, kLanes = kJoinThreads / QT < 64 ? kJoinThreads / QT : 64;
-  __shared__ float s_top[QT], s_total[QT];
+  constexpr int DH = I::kDh, QT = I::QT, kCols = kJoinCols<I>, kLanes = kJoinThreads / kCols;
+  __shared__ float s_top[kCols], s_total[kCols];
   __shared__ alignas(16) floatx4 s_part[kJoinThreads];
   const int tid = threadIdx.x;
   const int32_t *j = a.joins + (int64_t)blockIdx.x * kJoinInts;
   const int n = j[0];
   if (n == 0) return;
-  const int row0 = j[1], rows = j[2], len = j[3], head = j[4], tile = j[5];
-  const int cols = min(QT, rows * a.group - tile * QT);
-  const float *first = partial<I>(a, blockIdx.x, true);
-  auto slot = [&](int i) { return i == 0 ? first : first + (int64_t)(2 * i - 1) * I::kSlotFloats; };
-  // a thread takes four dimensions of a column; where the workgroup has more threads than that, groups of them take every parts-th result
-  const int per_col = a.p.dh / 4, elems = cols * per_col;
+  const int row0 = j[1], rows = j[2], len = j[3], head = j[4], tile = j[5], col0 = blockIdx.y * kCols;
+  const int cols = min(kCols, rows * a.group - tile * QT - col0);
+  if (cols <= 0) return;
+  const float *first = partial<I>(a, blockIdx.x, true) + col0;
+  auto slot = [&](int i) { return i == 0 ? first : first + (int64_t)(2 * i - 1) * I::kSlotFloats; };       // m; l lies QT, O 2 QT + col0 (DH - 1) behind it
+  // A thread takes four dimensions of a column; where the workgroup has more threads than that, groups of them take every parts-th result.  Eight
+  // results at a time are on their way, the first eight while the maxima are found.
+  const int per_col = a.p.dh / 4, elems = cols * per_col;      // at most kJoinThreads where d_head is at most 128
   int parts = 1;
   while (2 * parts * elems <= kJoinThreads && parts < n) parts *= 2;
   const int part = parts > 1 ? tid / elems : 0, e_first = parts > 1 ? tid - part * elems : tid;
-  constexpr int kAhead = 4;
-  floatx4 ahead[kAhead];                                       // the first results are on their way while the maxima are found
-  {
-    const int col = min(e_first / per_col, QT - 1), d = e_first % per_col * 4;
+  constexpr int kAhead = 8;
+  floatx4 o[kAhead];
+  float m[kAhead];
+  auto fetch = [&](int i, int e) {
+    const int col = e / per_col;
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k)
-      ahead[k] = e_first < elems && part + k * parts < n ? *(const floatx4 *)(slot(part + k * parts) + 2 * QT + col * DH + d) : floatx4{0.f, 0.f, 0.f, 0.f};
-  }
+    for (int k = 0; k < kAhead; ++k) {
+      const float *p = slot(min(i + k * parts, n - 1));
+      m[k] = p[col];
+      o[k] = *(const floatx4 *)(p + 2 * QT + col0 * (DH - 1) + col * DH + e % per_col * 4);
+    }
+  };
+  const bool any = e_first < elems && part < parts;
+  if (any) fetch(part, e_first);
   {
     const int col = tid / kLanes;
     float top = -INFINITY, total = 0.f;
-    auto merge = [&](float m, float l) {
-      const float t = fmaxf(top, m), ref = reference(t);
-      total = total * weight(a, top, ref) + l * weight(a, m, ref);
+    auto merge = [&](float m1, float l1) {
+      const float t = fmaxf(top, m1), ref = reference(t);
+      total = total * weight(a, top, ref) + l1 * weight(a, m1, ref);
       top = t;
     };
     if (col < cols)
       for (int i = tid % kLanes; i < n; i += kLanes) merge(slot(i)[col], slot(i)[QT + col]);
 #pragma unroll
-    for (int o = 1; o < kLanes; o <<= 1) merge(__shfl_xor(top, o, kWave), __shfl_xor(total, o, kWave));
+    for (int off = 1; off < kLanes; off <<= 1) merge(__shfl_xor(top, off, kWave), __shfl_xor(total, off, kWave));
     if (col < cols && tid % kLanes == 0) {
       s_top[col] = reference(top);
       s_total[col] = total;
@@ -291,19 +348,14 @@ page_attention_join_kernel(Args a) {
   for (int e0 = 0; e0 < elems; e0 += kJoinThreads) {
     const int e = e0 + e_first;
     const bool live = e < elems && part < parts;
-    const int col = live ? e / per_col : 0, d = live ? e % per_col * 4 : 0;
+    const int col = live ? e / per_col : 0;
     floatx4 sum = {0.f, 0.f, 0.f, 0.f};
     if (live) {
-      int i = part;
-      if (e0 == 0) {
+      for (int i = part; i < n; i += kAhead * parts) {
+        if (e0 > 0 || i > part) fetch(i, e);
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k, i += parts)
-          if (i < n) sum += weight(a, slot(i)[col], s_top[col]) * ahead[k];
-      }
-#pragma unroll 4
-      for (; i < n; i += parts) {
-        const float *p = slot(i);
-        sum += weight(a, p[col], s_top[col]) * *(const floatx4 *)(p + 2 * QT + col * DH + d);
+        for (int k = 0; k < kAhead; ++k)
+          if (i + k * parts < n) sum += weight(a, m[k], s_top[col]) * o[k];
       }
     }
     if (parts > 1) {
@@ -314,8 +366,8 @@ page_attention_join_kernel(Args a) {
     }
     if (live && part == 0) {
       int row;
-      const int64_t at = row_place(a, row0, head, tile * QT + col, a.p.out_stride, &row);
-      store4((T *)a.p.out + at + d, sum, 1.0f / s_total[col], limit_of(a, len, rows, row) <= 0);
+      const int64_t to = row_place(a, row0, head, tile * QT + col0 + col, a.p.out_stride, &row);
+      store4((T *)a.p.out + to + e % per_col * 4, sum, 1.0f / s_total[col], limit_of(a, len, rows, row) <= 0);
     }
   }
 }
@@ -331,7 +383,7 @@ Plan plan(int B, int M, int Hkv, int group, int width, int page_size) {
   const int64_t tiles = (int64_t)M * group / I::QT + (B < M ? B : M), triples = tiles * Hkv;
   const int64_t steps = ((int64_t)width * page_size + I::kStep - 1) / I::kStep;
   // what fits the chip, and PVF_PAGE_WORKSPACE: a number that 8 divides, for the order of workers on the XCDs
-  constexpr int64_t kRoom = PVF_PAGE_WORKSPACE / kPartialBytes<I> / 8 * 8, most = 256 * I::kPerCu < kRoom ? 256 * I::kPerCu : kRoom;
+  constexpr int64_t kRoom = PVF_PAGE_WORKSPACE / kPartialBytes<I> / 8 * 8, most = kCus * I::kPerCu < kRoom ? kCus * I::kPerCu : kRoom;
   Plan p;
   p.whole = steps <= I::kWholeSteps;
   const int64_t want = p.whole ? triples : triples * steps;

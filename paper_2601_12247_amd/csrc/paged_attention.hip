@@ -27,7 +27,7 @@ struct Inst {
   static constexpr int VE = kBf16 && DH >= 128 ? 8 : 4;
   static constexpr int NB = DH / (16 * VE), NT = DH / 16;
   static constexpr int kStep = 4 * KT;                  // keys a workgroup takes at once
-  static constexpr int QT = 16 * NQ, kDh = DH, kSnap = 0, kWholeSteps = 4;
+  static constexpr int QT = 16 * NQ, kDh = DH, kSplit = 0, kWholeSteps = 4;
   static constexpr int kOPad = DH + 4;
   static constexpr int kSlotFloats = QT * (DH + 2);     // a partial result: m[QT], l[QT], O[QT][DH]
   static constexpr int kRegs = (NT + KJ + 2) * 4 * NQ + NU * KJ * 4 + NU * 4 * NB * VE * (int)sizeof(T) / 4 + 64;   // about
@@ -400,7 +400,7 @@ pvf_status launch(Inst<T, DH, NQ>, hipStream_t s, Args &a) {
   else page_attention_kernel<T, DH, NQ, false><<<p.workers, 256, 0, s>>>(a);
   PVF_LAUNCH_CHECK(nullptr, "page_attention");
   if (!a.whole) {
-    page_attention_join_kernel<T, I><<<p.workers - 1, kJoinThreads, 0, s>>>(a);
+    page_attention_join_kernel<T, I><<<dim3(p.workers - 1, I::QT / kJoinCols<I>), kJoinThreads, 0, s>>>(a);
     PVF_LAUNCH_CHECK(nullptr, "page_attention_join");
   }
   return PVF_OK;

@@ -35,7 +35,7 @@ __device__ __forceinline__ void wait_and_meet() {
 // CW: waves beside each other over columns; the 4 / CW groups of them share out the keys of a step.
 template <int DH, int CW>
 struct WideInst {
-  static constexpr int kDh = DH, QT = 32 * CW, KW = 4 / CW, kStep = 64, kSubs = 2 / KW, kSnap = 4, kWholeSteps = 16, kPerCu = 2;
+  static constexpr int kDh = DH, QT = 32 * CW, KW = 4 / CW, kStep = 64, kSubs = 2 / KW, kSplit = 8, kWholeSteps = 16, kPerCu = 2;
   static constexpr int NT = DH / 32, KJ = DH / 16;
   static constexpr int kRow = DH * 2, kChunks = DH / 8, kTile = kStep * kRow;   // bytes of a key, its chunks, bytes of 64 keys
   static constexpr int kLoads = kTile / 4096, kKeys = 1024 / kRow;             // loads of 1 KB a wave and tile, keys of one
@@ -89,7 +89,14 @@ page_attention_wide_kernel(Args a) {
     for (int j = 0; j < I::KJ; ++j) {
       uint4 x = make_uint4(0, 0, 0, 0);
       if (col < cols && (kWhole || 16 * j + 8 * fh < a.p.dh)) x = *(const uint4 *)((const bf16_t *)a.p.q + q_at + 16 * j + 8 * fh);
-      q[j] = __builtin_bit_cast(bf16x8, make_uint4(x.x ^ a.q_xor, x.y ^ a.q_xor, x.z ^ a.q_xor, x.w ^ a.q_xor));
+      q[j] = __builtin_bit_cast(bf16x8, x);
+    }
+    if (a.q_xor) {                        // not before it is needed: the rows are on their way
+#pragma unroll
+      for (int j = 0; j < I::KJ; ++j) {
+        const uint4 x = __builtin_bit_cast(uint4, q[j]);
+        q[j] = __builtin_bit_cast(bf16x8, make_uint4(x.x ^ a.q_xor, x.y ^ a.q_xor, x.z ^ a.q_xor, x.w ^ a.q_xor));
+      }
     }
     floatx16 o[I::NT];
 #pragma unroll
@@ -124,13 +131,15 @@ page_attention_wide_kernel(Args a) {
           if (kWhole || lane_chunk * 8 < a.p.dh) load_to_lds((const void *)((uint64_t)hi << 32 | lo), lane_bytes, dst + i * 4096);
         }
       };
-      auto load_keys = [&](int kb, int buf) {
-        const int key = min(kb + (lane % I::kLoads * 4 + wid) * I::kKeys, (len - 1) & ~(I::kKeys - 1)), page = page_of(a, key);
+      int64_t keys_at = 0;
+      auto find = [&](int kb) {
+        const int key = min(kb + (lane % I::kLoads * 4 + wid) * I::kKeys, (k1 - 1) & ~(I::kKeys - 1)), page = page_of(a, key);
         const int id = max(s_pages[page - first_page], 0), off = (key - page * a.p.page_size) * a.p.dh;
+        keys_at = (int64_t)(kbase + (int64_t)id * a.p.k_page_stride + off);
         values_at = (int64_t)(vbase + (int64_t)id * a.p.v_page_stride + off);
-        load((int64_t)(kbase + (int64_t)id * a.p.k_page_stride + off), lds_at + buf * 2 * I::kTile);
       };
-      auto load_values = [&](int buf) { load(values_at, lds_at + (buf * 2 + 1) * I::kTile); };   // of the keys asked for last
+      auto load_keys = [&](int buf) { load(keys_at, lds_at + buf * 2 * I::kTile); };             // found last
+      auto load_values = [&](int buf) { load(values_at, lds_at + (buf * 2 + 1) * I::kTile); };
 
       // Keys and values of a step are asked for two steps ahead, each when its buffer has been read: three tiles are on the way at most, and waits are
       // for the oldest (the last two steps': for all).  The keys of this step are awaited before it begins.
@@ -156,6 +165,7 @@ page_attention_wide_kernel(Args a) {
         };
         read_keys(0);
         read_keys(1);
+        find(kb + 2 * I::kStep);                               // beside the products
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -163,7 +173,7 @@ page_attention_wide_kernel(Args a) {
 #pragma unroll
             for (int u = 0; u < I::kSubs; ++u) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[half][j][u], q[half * kHalf + j], s[u], 0, 0, 0);
         if (more) wait_and_meet<2 * I::kLoads>(); else wait_and_meet<0>();     // its values are there, its keys have been read
-        if (more) load_keys(kb + 2 * I::kStep, kBuf);
+        if (more) load_keys(kBuf);
         bool odd = false;
         if (__builtin_expect(kb + I::kStep > least, 0)) {
           // The tile holds keys that a row does not see, or copies of the last one.  0 times an infinity is no zero: values that are not finite
@@ -284,11 +294,13 @@ page_attention_wide_kernel(Args a) {
         }
       };
       __builtin_amdgcn_s_waitcnt(0x0f70);                      // vmcnt(0): nothing else is counted from here on
-      load_keys(k0, 0);
+      find(k0);
+      load_keys(0);
       load_values(0);
       const bool two = k0 < k1 - I::kStep;
       if (two) {
-        load_keys(k0 + I::kStep, 1);
+        find(k0 + I::kStep);
+        load_keys(1);
         load_values(1);
         wait_and_meet<3 * I::kLoads>();
       } else {
@@ -385,7 +397,7 @@ pvf_status launch(WideInst<DH, CW>, hipStream_t s, Args &a) {
   else page_attention_wide_kernel<DH, CW, false><<<p.workers, 256, 0, s>>>(a);
   PVF_LAUNCH_CHECK(nullptr, "page_attention_wide");
   if (!a.whole) {
-    page_attention_join_kernel<bf16_t, I><<<p.workers - 1, kJoinThreads, 0, s>>>(a);
+    page_attention_join_kernel<bf16_t, I><<<dim3(p.workers - 1, I::QT / kJoinCols<I>), kJoinThreads, 0, s>>>(a);
     PVF_LAUNCH_CHECK(nullptr, "page_attention_join");
   }
   return PVF_OK;
