@@ -361,7 +361,7 @@ pvf_status pvf_gemm_mx_instance(int32_t call, int32_t w_fmt, int32_t dtype, int3
  * order: the token at position p lies on page table[b][p / page_size], and its slot is that page * page_size + p % page_size.
  * All arrays here are dev, int32 ones among them; lengths and counts stay on the GPU.  The calls allocate nothing and may be captured into a graph;
  * what they keep between their launches is in their outputs or the workspace, so calls on different streams may overlap if those differ.
- * Sizes: B <= 2^20, M <= 2^24, width * page_size <= 2^30; caches d_head and page_size multiples of 8, up to 256 and 65536, rows and caches at
+ * Sizes: B <= 2^20, M <= 2^24, width <= 2^24, width * page_size <= 2^30; caches d_head and page_size multiples of 8, up to 256 and 65536, rows and caches at
  * multiples of 16 bytes with strides of such. */
 
 /* Pages for rows that requests are about to add or write again: request b computes n_rows[b] rows, at positions start[b] .. (start NULL: behind

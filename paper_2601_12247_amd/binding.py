@@ -567,11 +567,22 @@ def gemm_mx_instance(call: int, M: int, N: int, K: int, w_fmt: int = MX_E4M3, dt
 
 # ---- keys and values in pages --------------------------------------------------------------
 # A cache is a pair of tensors [n_pages, Hkv, page_size, d_head], pages contiguous but for the distance between them (stride(0)); a table is
-# int32 [B, width]; lengths, counts, positions and slots are int32.
-def _page_call(fn, dev: int, *args) -> None:
+# int32 [B, width]; lengths, counts, positions and slots are int32.  These calls may stand in a loop of single tokens, where what a check costs counts:
+# conditions are written out in one expression, and what does not fit is looked at again to say what it was.
+_i32_t = torch.int32
+
+
+def _misfit(dev: int, sizes) -> None:
+    """Says which of the (name, tensor, elements) does not fit: contiguous int32 tensors on device dev."""
+    assert dev >= 0, "device-resident tensors required"
+    for name, t, n in sizes:
+        assert t.dtype is _i32_t and t.numel() == n and t.is_contiguous() and t.get_device() == dev, \
+            f"{name}: int32 [{n}] on device {dev} required, not {t.dtype} {tuple(t.shape)} on {t.device}"
+    raise AssertionError("the table is int32 [B, width] beside the lengths, its rows contiguous")
+
+
+def _page_call(fn, dev: int, args) -> None:
     """fn(stream, *args) on device dev."""
-    if dev < 0:
-        raise AssertionError("device-resident tensors required")
     if dev != torch._C._cuda_getDevice():
         with torch.cuda.device(dev):
             status = fn(torch._C._cuda_getCurrentRawStream(dev), *args)
@@ -581,31 +592,20 @@ def _page_call(fn, dev: int, *args) -> None:
         _check(status)
 
 
-def _i32(dev: int, n: int, *tensors) -> None:
-    """Contiguous int32 tensors of n elements on device dev."""
-    for t in tensors:
-        assert t.dtype is torch.int32 and t.numel() == n and t.is_contiguous() and t.get_device() == dev, \
-            f"int32 [{n}] on device {dev} required: {t.dtype} {tuple(t.shape)} on {t.device}"
-
-
-def _table(table: torch.Tensor, dev: int, B: int):
-    """(width, distance of rows) of a checked table."""
-    assert table.dtype is torch.int32 and table.dim() == 2 and table.shape[0] == B and table.get_device() == dev, "the table is int32 [B, width] beside the lengths"
-    width = table.shape[1]
-    assert width <= 1 or table.stride(1) == 1, "rows of the table are contiguous"
-    return width, max(table.stride(0), width) if B > 1 else width
-
-
-def _cache(k: torch.Tensor, v: torch.Tensor, dtype: torch.dtype, dev: int):
-    """(n_pages, Hkv, page_size, d_head) of checked caches."""
-    shape = k.shape
-    assert len(shape) == 4 and v.shape == shape and k.dtype is dtype and v.dtype is dtype and k.get_device() == dev and v.get_device() == dev, \
+def _check_cache(k: torch.Tensor, v: torch.Tensor, dtype: torch.dtype, dev: int) -> None:
+    assert dev >= 0, "device-resident tensors required"
+    assert k.dim() == 4 and v.shape == k.shape and k.dtype is dtype and v.dtype is dtype and k.get_device() == dev and v.get_device() == dev, \
         "caches are [n_pages, Hkv, page_size, d_head] of the rows' type, beside them"
-    _, Hkv, P, dh = shape
+    _, Hkv, P, dh = k.shape
     for c in (k, v):
         s = c.stride()
         assert (dh == 1 or s[3] == 1) and (P == 1 or s[2] == dh) and (Hkv == 1 or s[1] == P * dh), "what is in a page is contiguous"
-    return shape
+
+
+def _check_rows(x: torch.Tensor, shape, dtype: torch.dtype, dev: int, name: str) -> None:
+    """x [rows, heads, d_head], rows apart at will."""
+    assert tuple(x.shape) == tuple(shape) and x.dtype is dtype and x.get_device() == dev and (shape[2] == 1 or x.stride(2) == 1) and \
+        (shape[1] <= 1 or x.stride(1) == shape[2]), f"{name} is {tuple(shape)} of {dtype}, heads contiguous: {tuple(x.shape)} {x.dtype} {x.stride()}"
 
 
 def page_extend(seq_len: torch.Tensor, n_rows: torch.Tensor, table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor, page_size: int,
@@ -613,43 +613,57 @@ def page_extend(seq_len: torch.Tensor, n_rows: torch.Tensor, table: torch.Tensor
     """Pages for the n_rows[b] rows that each request computes next, at positions start[b] .. (None: behind its seq_len[b] tokens); table is written.
     Returns (seq_len, n_free, cu_rows [B + 1], admitted [B], place [B + 1], pos [rows], slot [rows]), or writes them into `out`, such a tuple;
     `rows` counts the rows in all and is needed without `out`.  seq_len and n_free of `out` may be the inputs themselves."""
-    dev, B = seq_len.get_device(), seq_len.numel()
+    dev, B, i32 = seq_len.get_device(), seq_len.numel(), _i32_t
     if out is None:
         assert rows is not None, "rows, or out, is needed"
-        new = lambda n: torch.empty(n, dtype=torch.int32, device=seq_len.device)  # noqa: E731
+        new = lambda n: torch.empty(n, dtype=i32, device=seq_len.device)  # noqa: E731
         out = (new(B), new(1), new(B + 1), new(B), new(B + 1), new(rows), new(rows))
     len_out, free_out, cu, admitted, place, pos, slot = out
-    M = pos.numel()
+    M, cap, (TB, width) = pos.numel(), free_pages.numel(), table.shape
     assert rows is None or rows == M, "rows of `out`"
-    _i32(dev, B, seq_len, n_rows, len_out, admitted)
-    _i32(dev, B + 1, cu, place)
-    _i32(dev, M, pos, slot)
-    _i32(dev, 1, n_free, free_out)
-    _i32(dev, free_pages.numel(), free_pages)
-    if start is not None:
-        _i32(dev, B, start)
-    width, stride = _table(table, dev, B)
-    _page_call(lib().pvf_page_extend, dev, seq_len.data_ptr(), _p(start), n_rows.data_ptr(), B, table.data_ptr(), width, stride, page_size, free_pages.data_ptr(),
-               free_pages.numel(), n_free.data_ptr(), M, len_out.data_ptr(), free_out.data_ptr(), cu.data_ptr(), admitted.data_ptr(), place.data_ptr(),
-               pos.data_ptr(), slot.data_ptr())
+    stride = table.stride(0) if B > 1 else width
+    if not (dev >= 0 and seq_len.dtype is i32 and n_rows.dtype is i32 and len_out.dtype is i32 and admitted.dtype is i32 and cu.dtype is i32 and
+            place.dtype is i32 and pos.dtype is i32 and slot.dtype is i32 and n_free.dtype is i32 and free_out.dtype is i32 and free_pages.dtype is i32 and
+            table.dtype is i32 and TB == B and (width <= 1 or table.stride(1) == 1) and table.get_device() == dev and
+            n_rows.numel() == B and len_out.numel() == B and admitted.numel() == B and cu.numel() == B + 1 and place.numel() == B + 1 and slot.numel() == M and
+            n_free.numel() == 1 and free_out.numel() == 1 and
+            seq_len.is_contiguous() and n_rows.is_contiguous() and len_out.is_contiguous() and admitted.is_contiguous() and cu.is_contiguous() and
+            place.is_contiguous() and pos.is_contiguous() and slot.is_contiguous() and free_pages.is_contiguous() and
+            n_rows.get_device() == dev and len_out.get_device() == dev and admitted.get_device() == dev and cu.get_device() == dev and
+            place.get_device() == dev and pos.get_device() == dev and slot.get_device() == dev and n_free.get_device() == dev and
+            free_out.get_device() == dev and free_pages.get_device() == dev):
+        _misfit(dev, (("seq_len", seq_len, B), ("n_rows", n_rows, B), ("seq_len of out", len_out, B), ("admitted", admitted, B), ("cu_rows", cu, B + 1),
+                      ("place", place, B + 1), ("pos", pos, M), ("slot", slot, M), ("n_free", n_free, 1), ("n_free of out", free_out, 1), ("free_pages", free_pages, cap)))
+    if start is not None and not (start.dtype is i32 and start.numel() == B and start.is_contiguous() and start.get_device() == dev):
+        _misfit(dev, (("start", start, B),))
+    _page_call(lib().pvf_page_extend, dev, (
+        seq_len.data_ptr(), None if start is None else start.data_ptr(), n_rows.data_ptr(), B, table.data_ptr(), width, stride if stride > width else width, page_size,
+        free_pages.data_ptr(), cap, n_free.data_ptr(), M, len_out.data_ptr(), free_out.data_ptr(), cu.data_ptr(), admitted.data_ptr(), place.data_ptr(),
+        pos.data_ptr(), slot.data_ptr()))
     return out
 
 
 def page_trim(seq_len: torch.Tensor, keep: torch.Tensor, table: torch.Tensor, free_pages: torch.Tensor, n_free: torch.Tensor, page_size: int, out=None):
     """Pages behind the first keep[b] tokens of each request go back to free_pages, which is written.  Returns (seq_len, n_free, place [B + 1]), or
     writes them into `out`; seq_len (also keep) and n_free of `out` may be the inputs themselves."""
-    dev, B = seq_len.get_device(), seq_len.numel()
+    dev, B, i32 = seq_len.get_device(), seq_len.numel(), _i32_t
     if out is None:
-        new = lambda n: torch.empty(n, dtype=torch.int32, device=seq_len.device)  # noqa: E731
+        new = lambda n: torch.empty(n, dtype=i32, device=seq_len.device)  # noqa: E731
         out = (new(B), new(1), new(B + 1))
     len_out, free_out, place = out
-    _i32(dev, B, seq_len, keep, len_out)
-    _i32(dev, B + 1, place)
-    _i32(dev, 1, n_free, free_out)
-    _i32(dev, free_pages.numel(), free_pages)
-    width, stride = _table(table, dev, B)
-    _page_call(lib().pvf_page_trim, dev, seq_len.data_ptr(), keep.data_ptr(), B, table.data_ptr(), width, stride, page_size, free_pages.data_ptr(),
-               free_pages.numel(), n_free.data_ptr(), len_out.data_ptr(), free_out.data_ptr(), place.data_ptr())
+    cap, (TB, width) = free_pages.numel(), table.shape
+    stride = table.stride(0) if B > 1 else width
+    if not (dev >= 0 and seq_len.dtype is i32 and keep.dtype is i32 and len_out.dtype is i32 and place.dtype is i32 and n_free.dtype is i32 and
+            free_out.dtype is i32 and free_pages.dtype is i32 and table.dtype is i32 and TB == B and (width <= 1 or table.stride(1) == 1) and
+            table.get_device() == dev and keep.numel() == B and len_out.numel() == B and place.numel() == B + 1 and n_free.numel() == 1 and
+            free_out.numel() == 1 and seq_len.is_contiguous() and keep.is_contiguous() and len_out.is_contiguous() and place.is_contiguous() and
+            free_pages.is_contiguous() and keep.get_device() == dev and len_out.get_device() == dev and place.get_device() == dev and
+            n_free.get_device() == dev and free_out.get_device() == dev and free_pages.get_device() == dev):
+        _misfit(dev, (("seq_len", seq_len, B), ("keep", keep, B), ("seq_len of out", len_out, B), ("place", place, B + 1), ("n_free", n_free, 1),
+                      ("n_free of out", free_out, 1), ("free_pages", free_pages, cap)))
+    _page_call(lib().pvf_page_trim, dev, (
+        seq_len.data_ptr(), keep.data_ptr(), B, table.data_ptr(), width, stride if stride > width else width, page_size, free_pages.data_ptr(), cap,
+        n_free.data_ptr(), len_out.data_ptr(), free_out.data_ptr(), place.data_ptr()))
     return out
 
 
@@ -657,18 +671,28 @@ def page_store(qkv: torch.Tensor, pos: torch.Tensor, slot: torch.Tensor, k_cache
                q_out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Rotated q [M, H, d_head] of qkv [M, (H + 2 Hkv) * d_head] (rows may lie apart), whose rotated keys and values go to their slots; H follows from the
     caches.  q_out may be strided by rows, also the q part of qkv itself."""
-    dev, (M, wide) = qkv.get_device(), qkv.shape
-    n_pages, Hkv, P, dh = _cache(k_cache, v_cache, qkv.dtype, dev)
+    dev, (M, wide), dtype, i32 = qkv.get_device(), qkv.shape, qkv.dtype, _i32_t
+    shape = k_cache.shape
+    assert len(shape) == 4, "caches are [n_pages, Hkv, page_size, d_head]"
+    n_pages, Hkv, P, dh = shape
     H = wide // dh - 2 * Hkv
-    assert H >= 0 and wide == (H + 2 * Hkv) * dh and (wide == 1 or qkv.stride(1) == 1), "rows are q | k | v of whole heads"
-    _i32(dev, M, pos, slot)
+    assert H >= 0 and wide == (H + 2 * Hkv) * dh, "rows are q | k | v of whole heads"
     if q_out is None:
-        q_out = torch.empty(M, H, dh, dtype=qkv.dtype, device=qkv.device)
-    assert q_out.shape == (M, H, dh) and q_out.dtype is qkv.dtype and q_out.get_device() == dev and (dh == 1 or q_out.stride(2) == 1) and \
-        (H <= 1 or q_out.stride(1) == dh), "q_out is [M, H, d_head] of qkv's type, heads contiguous"
-    _page_call(lib().pvf_page_store, dev, _dtype_code(qkv.dtype), qkv.data_ptr(), qkv.stride(0) if M > 1 else 0, pos.data_ptr(), slot.data_ptr(), M, H, Hkv, dh,
-               rope_theta, q_out.data_ptr(), q_out.stride(0) if M > 1 else 0, k_cache.data_ptr(), v_cache.data_ptr(), n_pages, P,
-               k_cache.stride(0) if n_pages > 1 else 0, v_cache.stride(0) if n_pages > 1 else 0)
+        q_out = torch.empty(M, H, dh, dtype=dtype, device=qkv.device)
+    (x0, x1), (q0, q1, q2), (k0, k1, k2, k3), (v0, v1, v2, v3) = qkv.stride(), q_out.stride(), k_cache.stride(), v_cache.stride()
+    if not (dev >= 0 and k3 == 1 and v3 == 1 and k2 == dh and v2 == dh and k1 == P * dh and v1 == k1 and v_cache.shape == shape and k_cache.dtype is dtype and
+            v_cache.dtype is dtype and k_cache.get_device() == dev and v_cache.get_device() == dev):
+        _check_cache(k_cache, v_cache, dtype, dev)
+    if not (q2 == 1 and q1 == dh and q_out.shape == (M, H, dh) and q_out.dtype is dtype and q_out.get_device() == dev):
+        _check_rows(q_out, (M, H, dh), dtype, dev, "q_out")
+    assert x1 == 1 or wide == 1, "rows are contiguous"
+    if not (pos.dtype is i32 and slot.dtype is i32 and pos.numel() == M and slot.numel() == M and pos.is_contiguous() and slot.is_contiguous() and
+            pos.get_device() == dev and slot.get_device() == dev):
+        _misfit(dev, (("pos", pos, M), ("slot", slot, M)))
+    one, few = M <= 1, n_pages <= 1
+    _page_call(lib().pvf_page_store, dev, (
+        _dtype_code(dtype), qkv.data_ptr(), 0 if one else x0, pos.data_ptr(), slot.data_ptr(), M, H, Hkv, dh, rope_theta, q_out.data_ptr(), 0 if one else q0,
+        k_cache.data_ptr(), v_cache.data_ptr(), n_pages, P, 0 if few else k0, 0 if few else v0))
     return q_out
 
 
@@ -687,24 +711,34 @@ def page_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor
     """softmax(scale * q k^T) v of rows q [M, H, d_head] against the seq_len[b] tokens of their request: rows cu_rows[b] .. cu_rows[b + 1] - 1 are request b's
     (None: one row each).  causal: a request's rows are its last tokens and see no later ones.  scale: d_head^-0.5 by default.  q and out may be strided
     by rows.  workspace: uint8, for callers who keep one (PAGE_WORKSPACE bytes); calls that overlap need one each."""
-    dev, (M, H, dh), B = q.get_device(), q.shape, seq_len.numel()
-    n_pages, Hkv, P, cdh = _cache(k_cache, v_cache, q.dtype, dev)
-    assert cdh == dh and (dh == 1 or q.stride(2) == 1) and (H <= 1 or q.stride(1) == dh), "q is [M, H, d_head], heads contiguous, d_head the caches'"
+    dev, (M, H, dh), dtype, B, i32, shape = q.get_device(), q.shape, q.dtype, seq_len.numel(), _i32_t, k_cache.shape
+    assert len(shape) == 4 and shape[3] == dh, "caches are [n_pages, Hkv, page_size, d_head], d_head that of q"
+    n_pages, Hkv, P, _ = shape
     if out is None:
-        out = torch.empty(M, H, dh, dtype=q.dtype, device=q.device)
-    assert out.shape == (M, H, dh) and out.dtype is q.dtype and out.get_device() == dev and (dh == 1 or out.stride(2) == 1) and (H <= 1 or out.stride(1) == dh), \
-        "out is like q"
-    _i32(dev, B, seq_len)
-    if cu_rows is not None:
-        _i32(dev, B + 1, cu_rows)
-    width, stride = _table(table, dev, B)
+        out = torch.empty(M, H, dh, dtype=dtype, device=q.device)
+    (q0, q1, q2), (o0, o1, o2), (k0, k1, k2, k3), (v0, v1, v2, v3) = q.stride(), out.stride(), k_cache.stride(), v_cache.stride()
+    if not (dev >= 0 and k3 == 1 and v3 == 1 and k2 == dh and v2 == dh and k1 == P * dh and v1 == k1 and v_cache.shape == shape and k_cache.dtype is dtype and
+            v_cache.dtype is dtype and k_cache.get_device() == dev and v_cache.get_device() == dev):
+        _check_cache(k_cache, v_cache, dtype, dev)
+    if not (q2 == 1 and q1 == dh):
+        _check_rows(q, (M, H, dh), dtype, dev, "q")
+    if not (o2 == 1 and o1 == dh and out.shape == (M, H, dh) and out.dtype is dtype and out.get_device() == dev):
+        _check_rows(out, (M, H, dh), dtype, dev, "out")
+    TB, width = table.shape
+    stride = table.stride(0) if B > 1 else width
+    if not (seq_len.dtype is i32 and seq_len.is_contiguous() and table.dtype is i32 and TB == B and (width <= 1 or table.stride(1) == 1) and table.get_device() == dev):
+        _misfit(dev, (("seq_len", seq_len, B),))
+    if cu_rows is not None and not (cu_rows.dtype is i32 and cu_rows.numel() == B + 1 and cu_rows.is_contiguous() and cu_rows.get_device() == dev):
+        _misfit(dev, (("cu_rows", cu_rows, B + 1),))
+    assert seq_len.get_device() == dev, "lengths lie beside q"
     if workspace is None:
         workspace = torch.empty(page_attention_workspace(q, k_cache, table), dtype=torch.uint8, device=q.device)
     assert workspace.dtype is torch.uint8 and workspace.is_contiguous() and workspace.get_device() == dev, "the workspace is uint8, beside q"
-    _page_call(lib().pvf_page_attention, dev, _dtype_code(q.dtype), q.data_ptr(), q.stride(0) if M > 1 else 0, k_cache.data_ptr(), v_cache.data_ptr(), n_pages, P,
-               k_cache.stride(0) if n_pages > 1 else 0, v_cache.stride(0) if n_pages > 1 else 0, table.data_ptr(), width, stride, seq_len.data_ptr(),
-               _p(cu_rows), B, M, H, Hkv, dh, int(causal), dh ** -0.5 if scale is None else scale, out.data_ptr(), out.stride(0) if M > 1 else 0,
-               workspace.data_ptr(), workspace.numel())
+    one, few = M <= 1, n_pages <= 1
+    _page_call(lib().pvf_page_attention, dev, (
+        _dtype_code(dtype), q.data_ptr(), 0 if one else q0, k_cache.data_ptr(), v_cache.data_ptr(), n_pages, P, 0 if few else k0, 0 if few else v0,
+        table.data_ptr(), width, stride if stride > width else width, seq_len.data_ptr(), None if cu_rows is None else cu_rows.data_ptr(), B, M, H, Hkv, dh,
+        1 if causal else 0, dh ** -0.5 if scale is None else scale, out.data_ptr(), 0 if one else o0, workspace.data_ptr(), workspace.numel()))
     return out
 
 

@@ -7,6 +7,27 @@
 #include "common.h"
 
 namespace pvf {
+namespace page {
+
+template <int N>
+struct Const { static constexpr int value = N; };
+
+// A wave's sums over lanes 0 .. i, at most 2^32 - 1.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+  auto behind = [&](auto ctrl, auto rows) {
+    x = __builtin_elementwise_add_sat(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
+  };
+  behind(Const<0x111>{}, Const<0xf>{});   // rows of 16: one, two, four, eight lanes back
+  behind(Const<0x112>{}, Const<0xf>{});
+  behind(Const<0x114>{}, Const<0xf>{});
+  behind(Const<0x118>{}, Const<0xf>{});
+  behind(Const<0x142>{}, Const<0xa>{});   // the row in front, both rows in front
+  behind(Const<0x143>{}, Const<0xc>{});
+  return x;
+}
+__device__ __forceinline__ uint32_t last_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, 63); }
+
+}  // namespace page
 
 struct PageExtend {
   const int32_t *seq_len, *start, *n_rows, *n_free, *free_pages;

@@ -17,8 +17,6 @@ typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 constexpr int kPageSlots = 1024;          // table entries in LDS
 constexpr int kCus = 256;
-template <int N>
-struct Const { static constexpr int value = N; };
 
 struct Args {
   PageAttention p;
@@ -30,21 +28,6 @@ struct Args {
   int32_t *joins;                         // [workers][kJoinInts]: the triple that worker w begins and others end
 };
 constexpr int kJoinInts = 8;              // workers that took it (0: none), its first row, rows, length, key head, tile
-
-// A wave's sums over lanes 0 .. i, at most 2^32 - 1.
-__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
-  auto behind = [&](auto ctrl, auto rows) {
-    x = __builtin_elementwise_add_sat(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
-  };
-  behind(Const<0x111>{}, Const<0xf>{});   // rows of 16: one, two, four, eight lanes back
-  behind(Const<0x112>{}, Const<0xf>{});
-  behind(Const<0x114>{}, Const<0xf>{});
-  behind(Const<0x118>{}, Const<0xf>{});
-  behind(Const<0x142>{}, Const<0xa>{});   // the row in front, both rows in front
-  behind(Const<0x143>{}, Const<0xc>{});
-  return x;
-}
-__device__ __forceinline__ uint32_t last_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, 63); }
 
 struct Request {
   int row0, n, len, steps, tiles;         // its rows, visible keys, steps of keys and tiles of columns

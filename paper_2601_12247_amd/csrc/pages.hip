@@ -11,33 +11,32 @@
 namespace pvf {
 namespace {
 
+using page::last_lane;
+using page::wave_scan;
+
 constexpr int kThreads = 1024, kWaves = kThreads / kWave;
 constexpr int kFusedRequests = 2048, kFusedRows = 8192;
 constexpr int64_t kFusedPages = 65536;
 
-// Inclusive prefix sum over the workgroup's threads; *total: the sum.  part: kWaves elements of LDS.
-__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t *part, int64_t *total) {
-  const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const int64_t y = __shfl_up(x, o, kWave);
-    if (lane >= o) x += y;
+// Inclusive prefix sum, at most 2^32 - 1, over the workgroup's threads, or where all requests fit a wave over each wave's lanes; *total: the sum.
+// part: kWaves words of LDS that the sum before this one did not use.
+template <bool kOneWave>
+__device__ __forceinline__ uint32_t scan(uint32_t x, uint32_t *part, uint32_t *total) {
+  x = wave_scan(x);
+  if (kOneWave) {
+    *total = last_lane(x);
+    return x;
   }
-  __syncthreads();                                            // the last scan's reads of part are done
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (lane == 63) part[wid] = x;
   __syncthreads();
-  int64_t before = 0, all = 0;
-#pragma unroll
-  for (int i = 0; i < kWaves; ++i) {
-    const int64_t p = part[i];
-    before += i < wid ? p : 0;
-    all += p;
-  }
-  *total = all;
-  return x + before;
+  const uint32_t upto = wave_scan(lane < kWaves ? part[lane] : 0);
+  *total = last_lane(upto);
+  return __builtin_elementwise_add_sat(x, wid > 0 ? (uint32_t)__builtin_amdgcn_readlane((int)upto, wid - 1) : 0u);
 }
 
-__device__ __forceinline__ int64_t pages_of(int64_t tokens, int P) { return (tokens + P - 1) / P; }
+// of at most 2^30 tokens
+__device__ __forceinline__ uint32_t few_pages(int tokens, int P) { return ((uint32_t)tokens + (uint32_t)P - 1) / (uint32_t)P; }
 
 // The request that owns item x: the last r with first[r] <= x (first does not decrease).
 __device__ __forceinline__ int owner(const int32_t *first, int B, int x) {
@@ -57,7 +56,7 @@ __device__ __forceinline__ void write_row(const PageExtend &a, int r, const Grow
   const int p = (int)((uint32_t)g.start + (uint32_t)t);
   int slot = -1;
   if (g.admitted) {
-    const int j = p / a.page_size;
+    const int j = (int)((uint32_t)p / (uint32_t)a.page_size);
     const int page = j < g.have ? a.table[(int64_t)r * a.table_stride + j] : a.free_pages[g.top - 1 - (j - g.have)];
     const int64_t at = (int64_t)page * a.page_size + (p - j * a.page_size);
     slot = page < 0 || at > INT32_MAX ? -1 : (int)at;          // a table's or free list's entry that is no page
@@ -70,63 +69,75 @@ __device__ __forceinline__ void write_page(const PageExtend &a, int r, const Gro
 }
 __device__ __forceinline__ void write_padding(const PageExtend &a, int m) { a.pos[m] = 0; a.slot[m] = -1; }
 
-template <bool kFused>
+// kMost requests at most: 64 (every wave makes the sums for itself), kFusedRequests, or 0 for any number and a second launch for the rows.
+template <int kMost>
 __global__ void __launch_bounds__(kThreads)
 page_extend_kernel(PageExtend a) {
-  __shared__ int64_t part[kWaves];
-  __shared__ int32_t s_cu[kFused ? kFusedRequests + 1 : 1], s_taken[kFused ? kFusedRequests + 1 : 1];
-  __shared__ int32_t s_start[kFused ? kFusedRequests : 1], s_have[kFused ? kFusedRequests : 1];   // s_have < 0: not admitted
-  const int tid = threadIdx.x, P = a.page_size;
-  const int64_t most = (int64_t)a.width * P;
-  const int n_free = min(max(*a.n_free, 0), a.free_cap);
-  int64_t rows_before = 0, asked_before = 0, given_before = 0;
-  for (int b0 = 0; b0 < a.B; b0 += kThreads) {
-    const int b = b0 + tid;
-    int64_t len = 0, start = 0, n = 0;
+  constexpr bool kOneWave = kMost == kWave, kFused = kMost > 0;
+  __shared__ uint32_t part[3][kWaves];
+  __shared__ int32_t s_cu[kMost + 1], s_taken[kMost + 1], s_start[kFused ? kMost : 1], s_have[kFused ? kMost : 1];   // s_have < 0: not admitted
+  const int tid = threadIdx.x, P = a.page_size, stride = kOneWave ? kWave : kThreads, me = kOneWave ? tid & 63 : tid, most = a.width * P;
+  const bool writes = !kOneWave || tid < kWave;
+  const uint32_t n_free = (uint32_t)min(max(*a.n_free, 0), a.free_cap);
+  uint32_t rows_before = 0, asked_before = 0, given_before = 0;
+  for (int b0 = 0; b0 < a.B; b0 += stride) {
+    const int b = b0 + me;
+    int len = 0, start = 0, n = 0;
     if (b < a.B) {
       len = a.seq_len[b];
-      start = a.start ? a.start[b] : len;
       n = a.n_rows[b];
+      start = a.start ? a.start[b] : len;
     }
-    const bool sound = b < a.B && n >= 0 && start >= 0 && start <= len && len <= most;
-    const int64_t rows = n > 0 ? n : 0, new_len = max(len, start + n);
-    int64_t all;
-    const int64_t upto = rows_before + block_scan(rows, part, &all);
-    rows_before += all;
-    const bool fits = sound && new_len <= most && upto <= a.M;
-    const int64_t need = fits ? pages_of(new_len, P) - pages_of(len, P) : 0;
-    const int64_t asked = asked_before + block_scan(need, part, &all);
-    asked_before += all;
+    if (kOneWave) __syncthreads();                             // every wave has read what the first may write
+    const bool sound = b < a.B && n >= 0 && start >= 0 && start <= len && len <= most && n <= most - start;
+    const int new_len = sound ? max(len, start + n) : len;
+    const uint32_t rows = (uint32_t)min(max(n, 0), a.M + 1);    // more than M is too many, however many
+    uint32_t all;
+    const uint32_t upto = __builtin_elementwise_add_sat(rows_before, scan<kOneWave>(rows, part[0], &all));
+    rows_before = __builtin_elementwise_add_sat(rows_before, all);
+    const bool fits = sound && upto <= (uint32_t)a.M;
+    const uint32_t have = sound ? few_pages(len, P) : 0, need = fits ? few_pages(new_len, P) - have : 0;
+    const uint32_t asked = __builtin_elementwise_add_sat(asked_before, scan<kOneWave>(need, part[1], &all));
+    asked_before = __builtin_elementwise_add_sat(asked_before, all);
     const bool admitted = fits && (need == 0 || asked <= n_free);
-    const int64_t given = admitted ? need : 0, taken = given_before + block_scan(given, part, &all);
-    given_before += all;
+    // what is asked for does not decrease, so the requests that get pages are the first of those that want some
+    uint32_t taken = asked;
+    if (asked_before <= n_free) {
+      given_before = asked_before;
+    } else {
+      const uint32_t given = admitted ? need : 0;
+      taken = given_before + scan<kOneWave>(given, part[2], &all);
+      given_before += all;
+    }
     if (b < a.B) {
-      const int row0 = (int)min((int64_t)a.M, upto - rows);
-      a.seq_len_out[b] = (int)(admitted ? new_len : len);
-      a.admitted[b] = admitted;
-      a.cu_rows[b + 1] = (int)min((int64_t)a.M, upto);
-      a.place[b + 1] = (int)(n_free - taken);
-      if (row0 < a.M && rows > 0) a.pos[row0] = (int)start;
-      if (kFused) {
-        s_cu[b + 1] = (int)min((int64_t)a.M, upto);
+      const int end = (int)min((uint32_t)a.M, upto), row0 = (int)min((uint32_t)a.M, upto - rows);
+      if (writes) {
+        a.seq_len_out[b] = admitted ? new_len : len;
+        a.admitted[b] = admitted;
+        a.cu_rows[b + 1] = end;
+        a.place[b + 1] = (int)(n_free - taken);
+        if (!kFused && row0 < a.M && rows > 0) a.pos[row0] = start;
+      }
+      if (kFused) {                                            // with one wave's requests, every wave writes the same
+        s_cu[b + 1] = end;
         s_taken[b + 1] = (int)taken;
-        s_start[b] = (int)start;
-        s_have[b] = admitted ? (int)pages_of(len, P) : -1;
+        s_start[b] = start;
+        s_have[b] = admitted ? (int)have : -1;
       }
     }
+    if (!kOneWave && b0 + stride < a.B) __syncthreads();       // part[] has been read
   }
-  __syncthreads();
   if (tid == 0) {
     a.cu_rows[0] = 0;
-    a.place[0] = n_free;
-    *a.n_free_out = (int)(n_free - given_before);
+    a.place[0] = (int)n_free;
     if (kFused) s_cu[0] = s_taken[0] = 0;
   }
+  __syncthreads();                                             // and every thread has read *n_free
+  if (tid == 0) *a.n_free_out = (int)(n_free - given_before);
   if (!kFused) return;
-  __syncthreads();
-  const int total_rows = s_cu[a.B], total_pages = s_taken[a.B];
+  const int total_rows = a.B > 0 ? s_cu[a.B] : 0, total_pages = (int)given_before;
   auto grown = [&](int r) {
-    return Grown{s_cu[r], s_cu[r + 1] - s_cu[r], s_taken[r + 1] - s_taken[r], n_free - s_taken[r], s_have[r], s_start[r], s_have[r] >= 0};
+    return Grown{s_cu[r], s_cu[r + 1] - s_cu[r], s_taken[r + 1] - s_taken[r], (int)n_free - s_taken[r], s_have[r], s_start[r], s_have[r] >= 0};
   };
   for (int m = tid; m < a.M; m += kThreads) {
     if (m >= total_rows) { write_padding(a, m); continue; }
@@ -154,52 +165,73 @@ page_extend_rows_kernel(PageExtend a) {
   g.top = a.place[r];
   g.given = g.top - a.place[r + 1];
   g.admitted = a.admitted[r] != 0;
-  g.have = (int)pages_of(a.seq_len_out[r], a.page_size) - g.given;
+  g.have = g.admitted ? (int)few_pages(a.seq_len_out[r], a.page_size) - g.given : 0;
   g.start = g.rows > 0 ? a.pos[g.row0] : 0;
   for (int t = first; t < g.rows; t += step) write_row(a, r, g, t);
   for (int j = first; j < g.given; j += step) write_page(a, r, g, j);
 }
 
 // ---- trim --------------------------------------------------------------------------------------
-template <bool kFused>
+constexpr int kTrimEach = 4;               // requests of a thread where there are many
+
+template <int kMost>
 __global__ void __launch_bounds__(kThreads)
 page_trim_kernel(PageTrim a) {
-  __shared__ int64_t part[kWaves];
-  __shared__ int32_t s_place[kFused ? kFusedRequests + 1 : 1], s_first[kFused ? kFusedRequests : 1];
-  const int tid = threadIdx.x, P = a.page_size;
-  const int64_t most = (int64_t)a.width * P;
-  const int n_free = min(max(*a.n_free, 0), a.free_cap);
-  int64_t before = 0;
-  for (int b0 = 0; b0 < a.B; b0 += kThreads) {
-    const int b = b0 + tid;
-    int64_t len = 0, keep = 0;
-    if (b < a.B) {
-      len = min(max((int64_t)a.seq_len[b], (int64_t)0), most);
-      keep = min(max((int64_t)a.keep[b], (int64_t)0), len);
+  constexpr bool kOneWave = kMost == kWave, kFused = kMost > 0;
+  constexpr int kEach = kOneWave ? 1 : kTrimEach;
+  __shared__ uint32_t part[2][kWaves];
+  __shared__ int32_t s_place[kMost + 1], s_first[kFused ? kMost : 1];
+  const int tid = threadIdx.x, P = a.page_size, me = kOneWave ? tid & 63 : tid, most = a.width * P, stride = (kOneWave ? kWave : kThreads) * kEach;
+  const bool writes = !kOneWave || tid < kWave;
+  const uint32_t n_free = (uint32_t)min(max(*a.n_free, 0), a.free_cap);
+  uint32_t before = n_free;
+  int turn = 0;
+  for (int b0 = 0; b0 < a.B; b0 += stride, turn ^= 1) {
+    int keep[kEach];
+    uint32_t first[kEach], back[kEach], sum = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int b = b0 + me * kEach + i;
+      int len = 0;
+      keep[i] = 0;
+      if (b < a.B) {
+        len = min(max(a.seq_len[b], 0), most);
+        keep[i] = min(max(a.keep[b], 0), len);
+      }
+      first[i] = few_pages(keep[i], P);
+      back[i] = few_pages(len, P) - first[i];
+      sum = __builtin_elementwise_add_sat(sum, back[i]);
     }
-    int64_t all;
-    const int64_t back = pages_of(len, P) - pages_of(keep, P), upto = before + block_scan(back, part, &all);
-    before += all;
-    if (b < a.B) {
-      const int behind = (int)min((int64_t)a.free_cap, n_free + upto);
-      a.seq_len_out[b] = (int)keep;
-      a.place[b + 1] = behind;
-      if (kFused) {
-        s_place[b + 1] = behind;
-        s_first[b] = (int)pages_of(keep, P);
+    if (kOneWave) __syncthreads();                             // every wave has read what the first may write
+    uint32_t all, upto = __builtin_elementwise_add_sat(before, scan<kOneWave>(sum, part[turn], &all));
+    before = __builtin_elementwise_add_sat(before, all);
+    upto = upto == 0xffffffffu ? upto : upto - sum;            // beyond the list either way
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int b = b0 + me * kEach + i;
+      upto = __builtin_elementwise_add_sat(upto, back[i]);
+      if (b < a.B) {
+        const int behind = (int)min((uint32_t)a.free_cap, upto);
+        if (writes) {
+          a.seq_len_out[b] = keep[i];
+          a.place[b + 1] = behind;
+        }
+        if (kFused) {
+          s_place[b + 1] = behind;
+          s_first[b] = (int)first[i];
+        }
       }
     }
   }
-  __syncthreads();
-  const int top = (int)min((int64_t)a.free_cap, n_free + before);
+  const int top = (int)min((uint32_t)a.free_cap, before);
   if (tid == 0) {
-    a.place[0] = n_free;
-    *a.n_free_out = top;
-    if (kFused) s_place[0] = n_free;
+    a.place[0] = (int)n_free;
+    if (kFused) s_place[0] = (int)n_free;
   }
+  __syncthreads();                                             // and every thread has read *n_free
+  if (tid == 0) *a.n_free_out = top;
   if (!kFused) return;
-  __syncthreads();
-  for (int x = n_free + tid; x < top; x += kThreads) {
+  for (int x = (int)n_free + tid; x < top; x += kThreads) {
     const int r = owner(s_place, a.B, x);
     a.free_pages[x] = a.table[(int64_t)r * a.table_stride + s_first[r] + (x - s_place[r])];
   }
@@ -209,7 +241,7 @@ __global__ void __launch_bounds__(256)
 page_trim_pages_kernel(PageTrim a) {
   const int r = blockIdx.x, at = a.place[r], n = a.place[r + 1] - at;
   if (n == 0) return;
-  const int32_t *src = a.table + (int64_t)r * a.table_stride + pages_of(a.seq_len_out[r], a.page_size);
+  const int32_t *src = a.table + (int64_t)r * a.table_stride + few_pages(a.seq_len_out[r], a.page_size);
   for (int j = blockIdx.y * 256 + threadIdx.x; j < n; j += gridDim.y * 256) a.free_pages[at + j] = src[j];
 }
 
@@ -289,11 +321,12 @@ void store_rows(hipStream_t s, const PageStore &a) {
 
 pvf_status launch_page_extend(hipStream_t s, const PageExtend &a) {
   if (a.M <= kFusedRows && a.B <= kFusedRequests) {
-    page_extend_kernel<true><<<1, kThreads, 0, s>>>(a);
+    if (a.B <= kWave) page_extend_kernel<kWave><<<1, kThreads, 0, s>>>(a);
+    else page_extend_kernel<kFusedRequests><<<1, kThreads, 0, s>>>(a);
     PVF_LAUNCH_CHECK(nullptr, "page_extend");
     return PVF_OK;
   }
-  page_extend_kernel<false><<<1, kThreads, 0, s>>>(a);
+  page_extend_kernel<0><<<1, kThreads, 0, s>>>(a);
   PVF_LAUNCH_CHECK(nullptr, "page_extend");
   const int y = (int)std::min<int64_t>(64, ((int64_t)a.M / 1024 + a.B) / (a.B + 1) + 1);
   page_extend_rows_kernel<<<dim3(a.B + 1, y), 256, 0, s>>>(a);
@@ -303,11 +336,12 @@ pvf_status launch_page_extend(hipStream_t s, const PageExtend &a) {
 
 pvf_status launch_page_trim(hipStream_t s, const PageTrim &a) {
   if ((int64_t)a.B * a.width <= kFusedPages && a.B <= kFusedRequests) {
-    page_trim_kernel<true><<<1, kThreads, 0, s>>>(a);
+    if (a.B <= kWave) page_trim_kernel<kWave><<<1, kThreads, 0, s>>>(a);
+    else page_trim_kernel<kFusedRequests><<<1, kThreads, 0, s>>>(a);
     PVF_LAUNCH_CHECK(nullptr, "page_trim");
     return PVF_OK;
   }
-  page_trim_kernel<false><<<1, kThreads, 0, s>>>(a);
+  page_trim_kernel<0><<<1, kThreads, 0, s>>>(a);
   PVF_LAUNCH_CHECK(nullptr, "page_trim");
   const int y = (int)std::min<int64_t>(64, ((int64_t)a.width / 1024) * 256 / std::max(a.B, 256) + 1);
   page_trim_pages_kernel<<<dim3(a.B, y), 256, 0, s>>>(a);

@@ -1152,7 +1152,7 @@ static bool at_4(const void *p) { return (uintptr_t)p % 4 == 0; }
 
 static pvf_status check_pages(const char *call, int32_t B, int32_t width, int64_t table_stride, int32_t page_size) {
   PVF_REQUIRE(nullptr, B >= 0 && width >= 0 && page_size > 0, PVF_EINVAL, "%s: bad size (B=%d, width=%d, page_size=%d)", call, B, width, page_size);
-  PVF_REQUIRE(nullptr, B <= 1 << 20 && (int64_t)width * page_size <= 1 << 30, PVF_ESHAPE, "%s: %d requests of %d pages of %d: at most 2^20 requests of 2^30 tokens",
+  PVF_REQUIRE(nullptr, B <= 1 << 20 && width <= 1 << 24 && (int64_t)width * page_size <= 1 << 30, PVF_ESHAPE, "%s: %d requests of %d pages of %d: at most 2^20 requests of 2^24 pages and 2^30 tokens",
               call, B, width, page_size);
   PVF_REQUIRE(nullptr, table_stride >= width && table_stride <= INT32_MAX, PVF_EINVAL, "%s: rows of the table are %lld apart and %d wide", call,
               (long long)table_stride, width);

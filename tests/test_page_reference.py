@@ -116,7 +116,7 @@ def test_extend_refuses(status, kw):
 @pytest.mark.parametrize("status,kw", [
     *[(EINVAL, {name: None}) for name in ("seq_len", "keep", "table", "free_pages", "n_free", "seq_len_out", "n_free_out", "place")],
     (EINVAL, {"B": -1}), (EINVAL, {"page_size": -3}), (EINVAL, {"table_stride": 4}), (EINVAL, {"free_cap": -1}), (EINVAL, {"keep": A + 2}),
-    (ESHAPE, {"B": (1 << 20) + 1}), (ESHAPE, {"page_size": 1 << 29}),
+    (ESHAPE, {"B": (1 << 20) + 1}), (ESHAPE, {"page_size": 1 << 29}), (ESHAPE, {"width": (1 << 24) + 1, "table_stride": 1 << 25, "page_size": 1}),
 ])
 def test_trim_refuses(status, kw):
     assert _trim(**kw) == status and b"pvf_page_trim" in B.lib().pvf_last_error(None)
