@@ -43,24 +43,28 @@ struct Piece {
   bool done, begun;                       // all of it; from its first step on
 };
 
-// The line, 64 requests at a time, one a lane, and a worker's place on it.  Triples are below 2^31 (rows and heads together are); a line of that many
-// steps is one of whole triples.
+// The line, 64 requests at a time, one a lane, and a worker's place on it.  Its items are `chunk` steps of a triple each, the last of a triple as many as are
+// left: single steps, whole triples, or what gives each worker one item.  Triples are below 2^31 (rows and heads together are); a line of that many steps
+// is one of whole triples.
 template <class I>
 struct Line {
   const Args &a;
   int row0, n, len;                       // this lane's; row0 with kOver set: longer than its table
   uint32_t upto, base;                    // items up to it and its own; in front of these 64
   int b0, b;                              // the first of these 64; the request of the last piece
-  bool whole;                             // items are triples, not steps of them
+  uint32_t chunk;
   uint32_t at, end, share;
   uint32_t rest_at, rest_end;             // the worker's items of steps behind those, of triples that are divided
+  uint32_t left;                          // items of the last piece's triple behind it
 
   static constexpr int kOver = 1 << 30;
+  static constexpr uint32_t kWhole = 1u << 30;                 // more steps than a triple has
 
   __device__ __forceinline__ static int steps_of(int len) { return max((len + I::kStep - 1) / I::kStep, 1); }
   __device__ __forceinline__ int tiles_of(int rows) const { return (int)(((uint32_t)(rows * a.group) + I::QT - 1) / I::QT); }
   __device__ __forceinline__ uint32_t triples_of(int rows) const { return (uint32_t)tiles_of(rows) * (uint32_t)a.p.Hkv; }
-  __device__ __forceinline__ uint32_t items_of(int rows, int keys) const { return triples_of(rows) * (whole ? 1u : (uint32_t)steps_of(keys)); }
+  __device__ __forceinline__ uint32_t chunks_of(int keys) const { return chunk == 1 ? (uint32_t)steps_of(keys) : ((uint32_t)steps_of(keys) + chunk - 1) / chunk; }
+  __device__ __forceinline__ uint32_t items_of(int rows, int keys) const { return triples_of(rows) * chunks_of(keys); }
 
   __device__ __forceinline__ void load(int from) {
     b0 = from;
@@ -84,13 +88,13 @@ struct Line {
   // than a CU's part of all steps by more than kSplit (what dividing costs, in steps), each CU takes one, or every worker the same number; the
   // others are divided, between the workers that have none, or all.
   __device__ __forceinline__ Line(const Args &args, int block, int workers, int *worker) : a(args) {
-    whole = a.whole;
+    chunk = a.whole ? kWhole : 1;
     uint32_t sum = 0, all_triples = 0;
     int longest = 0;
     for (int from = 0; from < a.p.B; from += kWave) {
       load(from);
       const uint32_t mine = items_of(n, len);
-      sum = __builtin_elementwise_add_sat(sum, !whole && __umulhi(triples_of(n), (uint32_t)steps_of(len)) ? 0xffffffffu : mine);
+      sum = __builtin_elementwise_add_sat(sum, chunk == 1 && __umulhi(triples_of(n), (uint32_t)steps_of(len)) ? 0xffffffffu : mine);
       if (I::kSplit > 0) longest = max(longest, n > 0 ? steps_of(len) : 0);
       all_triples += triples_of(n);
     }
@@ -98,13 +102,12 @@ struct Line {
     share = (all + workers - 1) / (uint32_t)workers;
     *worker = block;
     base = rest_at = rest_end = 0;
-    const bool counted = whole || all >> 31;
+    const bool counted = chunk != 1 || all >> 31;
     if (!counted && I::kSplit > 0 && __builtin_amdgcn_ballot_w64((uint32_t)longest > all / kCus + I::kSplit) == 0) {
       const uint32_t t = last_lane(wave_scan(all_triples)), takers = t < (uint32_t)(workers - workers / 8) ? min(workers, kCus) : workers, each = t < takers ? 1 : t / takers;
       const uint32_t dealt = min(t, takers * each), others = dealt == t ? 0 : takers < (uint32_t)workers ? workers - takers : takers;
       if (others == 0 || dealt >= t / 2) {
         if (others > 0) {                 // steps of the triples that are dealt out lie in front of the others'
-          whole = false;
           if (a.p.B > kWave) load(0);
           uint32_t t0 = 0, s0 = 0;
           for (;;) {
@@ -127,17 +130,31 @@ struct Line {
             rest_end = min(rest_at + share, all);
           }
         }
-        whole = true;
+        chunk = kWhole;
         at = (uint32_t)block < takers ? min((uint32_t)block * each, dealt) : dealt;
         end = min(at + each, dealt);
         begin();
         return;
       }
     }
-    if (counted && !whole) {
-      whole = true;
+    if (counted && chunk == 1) {
+      chunk = kWhole;
       all = last_lane(wave_scan(all_triples));
       share = (all + workers - 1) / (uint32_t)workers;
+    }
+    if (chunk == 1 && share > 1 && a.p.B <= kWave) {
+      // A second piece costs a worker some steps (rows anew, its first keys, another result): each has one, if parts an eighth longer do.
+      // 17 requests of up to 1411 keys, f32: 17.0 us, 19.8 with shares of steps that end anywhere.
+      for (uint32_t more = 0; more < 3; ++more) {
+        chunk = share + (more < 2 ? more : 1 + share / 8);
+        const uint32_t items = last_lane(wave_scan(items_of(n, len)));
+        if (items <= (uint32_t)workers) {
+          all = items;
+          share = 1;
+          break;
+        }
+        chunk = 1;
+      }
     }
     // workers that follow each other read the same keys for other columns: where all take part, neighbours run on one XCD and share its L2
     if (workers % 8 == 0 && share * (uint32_t)(workers - 1) < all) *worker = block % 8 * (workers / 8) + block / 8;
@@ -159,7 +176,7 @@ struct Line {
       at = rest_at;
       end = rest_end;
       rest_end = 0;
-      whole = false;
+      chunk = 1;
       begin();
     }
     uint64_t beyond;
@@ -178,16 +195,12 @@ struct Line {
     r.len = of(len);
     r.steps = steps_of(r.len);
     r.tiles = tiles_of(r.n);
-    const uint32_t rel = at - ((uint32_t)of((int)upto) - items_of(r.n, r.len));
-    uint32_t triple = rel;
-    p.step0 = 0;
-    p.step1 = r.steps;
-    if (!whole) {
-      triple = rel / (uint32_t)r.steps;
-      p.step0 = (int)(rel - triple * (uint32_t)r.steps);
-      p.step1 = (int)min((uint32_t)r.steps, p.step0 + (end - at));
-    }
-    at += whole ? 1 : p.step1 - p.step0;
+    const uint32_t rel = at - ((uint32_t)of((int)upto) - items_of(r.n, r.len)), chunks = chunks_of(r.len), triple = chunks == 1 ? rel : rel / chunks;
+    const uint32_t first = rel - triple * chunks, count = min(chunks - first, end - at);
+    p.step0 = (int)(first * chunk);
+    p.step1 = (int)min((uint32_t)r.steps, (first + count) * chunk);
+    at += count;
+    left = chunks - first - count;
     p.head = (int)(triple / (uint32_t)r.tiles);
     p.tile = (int)(triple - (uint32_t)p.head * (uint32_t)r.tiles);
     p.cols = min(I::QT, r.n * a.group - p.tile * I::QT);
@@ -196,11 +209,11 @@ struct Line {
     return p.head < a.p.Hkv;
   }
 
-  // Notes how many workers take a triple that this one begins: others end it, `share` steps each.
+  // Notes how many workers take a triple that this one begins: others end it, `share` items each.
   __device__ __forceinline__ void note_join(int worker, const Request &r, const Piece &p) const {
     int32_t *j = a.joins + (int64_t)worker * kJoinInts;
     *(int4 *)(j + 4) = make_int4(p.head, p.tile, 0, 0);
-    *(int4 *)j = make_int4((int)((r.steps - p.step1 + share - 1) / share) + 1, r.row0, r.n, r.len);
+    *(int4 *)j = make_int4((int)((left + share - 1) / share) + 1, r.row0, r.n, r.len);
   }
 };
 

@@ -286,6 +286,30 @@ def test_many_requests():
     Pool(lens, 4, 2, 64, 16, "f32", seed=5, width=64).rows(n).check(causal=True)
 
 
+# Requests x key heads of 128 rows (or 50, 64 columns): how triples are dealt to workers changes at 256 of them, at 7/8 of the workers and at all of them,
+# with more than 64 requests, and where one request is much longer than the others.
+@pytest.mark.parametrize("nreq,Hkv,n,dh,longest,causal", [
+    (10, 30, 128, 128, 0, False), (10, 30, 128, 64, 0, True), (47, 10, 128, 64, 0, False), (75, 8, 128, 128, 0, True), (110, 10, 128, 64, 0, False), (70, 8, 50, 128, 0, True),
+    (40, 7, 50, 64, 0, False), (130, 1, 128, 128, 0, True), (65, 4, 33, 72, 0, False), (9, 4, 128, 128, 9000, True), (70, 4, 128, 128, 9000, False), (66, 2, 64, 64, 5000, True),
+    (1, 1, 128, 128, 30000, False), (1, 2, 50, 128, 20000, True), (3, 5, 300, 96, 3000, True)])
+def test_windows_dealt_to_workers(nreq, Hkv, n, dh, longest, causal):
+    lens = [130 + (97 * b) % 331 for b in range(nreq)]
+    rows = [n - (b % 5 == 3) * (b % 17) for b in range(nreq)]
+    if longest:
+        lens[nreq // 2] = longest
+    pool = Pool(lens, Hkv, Hkv, dh, 16, "bf16", seed=nreq + n, width=max(80, -(-longest // 16)), spread=2.0).rows(rows)
+    first = pool.check(causal=causal, extra=2)
+    assert torch.equal(first, pool.run(causal=causal, extra=2))
+
+
+@pytest.mark.parametrize("nreq,H,Hkv,n,dh", [(17, 12, 3, 5, 128), (3, 4, 1, 1, 80), (64, 8, 2, 2, 64), (65, 8, 2, 2, 64), (2, 6, 6, 40, 136), (5, 2, 2, 1, 256)])
+def test_keys_divided_between_workers(nreq, H, Hkv, n, dh):
+    """Lengths around what gives each worker one part, several, and parts that end inside another request."""
+    for top in (700, 1411, 2600):
+        lens = [top - (131 * b) % top for b in range(nreq)]
+        Pool(lens, H, Hkv, dh, 24, "f32", seed=nreq + top, width=120).rows([n] * nreq).check(causal=top == 1411)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_scales(dtype):
     for scale in (0.0, 0.7, -0.2, 3.0):
