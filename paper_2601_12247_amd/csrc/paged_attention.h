@@ -25,6 +25,7 @@ struct Args {
   float c;                                // |scale| * log2(e), above zero: scores are compared before they are scaled,
   uint32_t q_xor;                         // and the sign of a negative scale goes into q
   int32_t whole;                          // 1: the line is of triples, not steps (host)
+  int32_t workers;                        // workgroups between which triples may be divided: the grid's first
   int32_t *joins;                         // [workers][kJoinInts]: the triple that worker w begins and others end
 };
 constexpr int kJoinInts = 8;              // workers that took it (0: none), its first row, rows, length, key head, tile
@@ -84,10 +85,15 @@ struct Line {
     }
   }
 
-  // Triples stay whole where the host says so, and on instances with large partial results as far as they can be dealt out evenly: unless one is longer
-  // than a CU's part of all steps by more than kSplit (what dividing costs, in steps), each CU takes one, or every worker the same number; the
-  // others are divided, between the workers that have none, or all.
-  __device__ __forceinline__ Line(const Args &args, int block, int workers, int *worker) : a(args) {
+  // Triples stay whole where the host says so.  Else, unless one is longer than its share of all steps by more than kSplit (what dividing costs, in steps):
+  // where they are fewer than workers, each CU takes one and the rest is divided between the workers that have none; where they are more, instances with
+  // large partial results leave them whole, for the grid's workgroups as they come (a longest one at the end then costs less than dividing).  On the others
+  // a few triples (half the CUs) are divided, too.
+  //   bf16, 9 x 32 triples of 128 columns, 1280 keys: 65.4 us; 70.6 if none is divided, 81 with equal shares of all steps
+  //   bf16, 20 x 32 of them: 121 us (90 with lengths from half of that on); 154 (124) with equal shares
+  //   bf16, 32 x 8 triples of one column, 2048 keys: 45.8 us; 49.8 with equal shares
+  __device__ __forceinline__ Line(const Args &args, int block, int grid, int *worker) : a(args) {
+    const uint32_t workers = (uint32_t)a.workers;
     chunk = a.whole ? kWhole : 1;
     uint32_t sum = 0, all_triples = 0;
     int longest = 0;
@@ -95,19 +101,20 @@ struct Line {
       load(from);
       const uint32_t mine = items_of(n, len);
       sum = __builtin_elementwise_add_sat(sum, chunk == 1 && __umulhi(triples_of(n), (uint32_t)steps_of(len)) ? 0xffffffffu : mine);
-      if (I::kSplit > 0) longest = max(longest, n > 0 ? steps_of(len) : 0);
+      longest = max(longest, n > 0 ? steps_of(len) : 0);
       all_triples += triples_of(n);
     }
     uint32_t all = last_lane(wave_scan(sum));
-    share = (all + workers - 1) / (uint32_t)workers;
+    share = (all + workers - 1) / workers;
     *worker = block;
     base = rest_at = rest_end = 0;
     const bool counted = chunk != 1 || all >> 31;
-    if (!counted && I::kSplit > 0 && __builtin_amdgcn_ballot_w64((uint32_t)longest > all / kCus + I::kSplit) == 0) {
-      const uint32_t t = last_lane(wave_scan(all_triples)), takers = t < (uint32_t)(workers - workers / 8) ? min(workers, kCus) : workers, each = t < takers ? 1 : t / takers;
-      const uint32_t dealt = min(t, takers * each), others = dealt == t ? 0 : takers < (uint32_t)workers ? workers - takers : takers;
-      if (others == 0 || dealt >= t / 2) {
-        if (others > 0) {                 // steps of the triples that are dealt out lie in front of the others'
+    if (!counted) {
+      const uint32_t t = last_lane(wave_scan(all_triples));
+      const bool many = t >= workers - workers / 8;
+      if ((I::kAsTheyCome || (t >= kCus / 2 && !many)) && __builtin_amdgcn_ballot_w64((uint32_t)longest > all / (many ? 2 * kCus : kCus) + I::kSplit) == 0) {
+        const uint32_t takers = many ? (uint32_t)grid : min(workers, (uint32_t)kCus), each = (t + takers - 1) / takers, dealt = many ? t : min(t, takers);
+        if (dealt < t) {                  // steps of the triples that are dealt out lie in front of the others'
           if (a.p.B > kWave) load(0);
           uint32_t t0 = 0, s0 = 0;
           for (;;) {
@@ -123,16 +130,17 @@ struct Line {
             s0 = last_lane(s1);
             load(b0 + kWave);
           }
+          const uint32_t others = workers - takers;                                                 // more triples than CUs, fewer than workers
           share = (all - s0 + others - 1) / others;
-          const uint32_t k = takers < (uint32_t)workers ? (uint32_t)block - takers : (uint32_t)block;   // which of the others; takers have none where that wraps
-          if (k < others) {
-            rest_at = min(s0 + share * k, all);
+          if ((uint32_t)block >= takers && (uint32_t)block < workers) {
+            rest_at = min(s0 + share * ((uint32_t)block - takers), all);
             rest_end = min(rest_at + share, all);
           }
         }
         chunk = kWhole;
-        at = (uint32_t)block < takers ? min((uint32_t)block * each, dealt) : dealt;
-        end = min(at + each, dealt);
+        const uint32_t of_each = many ? each : 1;
+        at = (uint32_t)block < takers ? min((uint32_t)block * of_each, dealt) : dealt;
+        end = min(at + of_each, dealt);
         begin();
         return;
       }
@@ -140,7 +148,7 @@ struct Line {
     if (counted && chunk == 1) {
       chunk = kWhole;
       all = last_lane(wave_scan(all_triples));
-      share = (all + workers - 1) / (uint32_t)workers;
+      share = (all + workers - 1) / workers;
     }
     if (chunk == 1 && share > 1 && a.p.B <= kWave) {
       // A second piece costs a worker some steps (rows anew, its first keys, another result): each has one, if parts an eighth longer do.
@@ -148,7 +156,7 @@ struct Line {
       for (uint32_t more = 0; more < 3; ++more) {
         chunk = share + (more < 2 ? more : 1 + share / 8);
         const uint32_t items = last_lane(wave_scan(items_of(n, len)));
-        if (items <= (uint32_t)workers) {
+        if (items <= workers) {
           all = items;
           share = 1;
           break;
@@ -157,8 +165,8 @@ struct Line {
       }
     }
     // workers that follow each other read the same keys for other columns: where all take part, neighbours run on one XCD and share its L2
-    if (workers % 8 == 0 && share * (uint32_t)(workers - 1) < all) *worker = block % 8 * (workers / 8) + block / 8;
-    at = min(share * (uint32_t)*worker, all);
+    if (workers % 8 == 0 && share * (workers - 1) < all && (uint32_t)block < workers) *worker = block % 8 * ((int)workers / 8) + block / 8;
+    at = (uint32_t)block < workers ? min(share * (uint32_t)*worker, all) : all;
     end = min(at + share, all);
     begin();
   }
@@ -244,7 +252,7 @@ __device__ __forceinline__ float weight(const Args &a, float m, float ref) { ret
 // Where a key lies, from the table entries in LDS; *none: on no page (page 0 is read).
 __device__ __forceinline__ int page_of(const Args &a, int key) { return (int)(__umulhi((uint32_t)(key >> 3) << 1, a.div_mul) >> a.div_shift); }
 
-// Table entries of keys k0 .. k1 - 1 into LDS, -1 for what is no page; *s_bad (zero before) becomes one if there is such.
+// Table entries of keys k0 .. k1 - 1 into LDS, -1 for what is no page; *s_bad (zero before, if given) becomes one if there is such.
 __device__ __forceinline__ void load_pages(const Args &a, int b, int k0, int k1, int first_page, int32_t *s_pages, int32_t *s_bad) {
   const int n = k1 > k0 ? page_of(a, k1 - 1) - first_page + 1 : 0;
   const int32_t *row = a.p.table + (int64_t)b * a.p.table_stride + first_page;
@@ -253,7 +261,7 @@ __device__ __forceinline__ void load_pages(const Args &a, int b, int k0, int k1,
     if (first_page + i < a.p.width) id = row[i];
     const bool there = (uint32_t)id < (uint32_t)a.p.n_pages;
     s_pages[i] = there ? id : -1;
-    if (!there) *s_bad = 1;
+    if (s_bad && !there) *s_bad = 1;
   }
 }
 // Every wave's LDS accesses so far are done; loads from global memory stay on their way.
@@ -296,7 +304,7 @@ page_attention_join_kernel(Args a) {
   __shared__ alignas(16) floatx4 s_part[kJoinThreads];
   const int tid = threadIdx.x;
   const int32_t *j = a.joins + (int64_t)blockIdx.x * kJoinInts;
-  const int n = j[0];
+  const int n = min(j[0], (int)(gridDim.x + 1 - blockIdx.x));    // (more only if lengths have changed under the call)
   if (n == 0) return;
   const int row0 = j[1], rows = j[2], len = j[3], head = j[4], tile = j[5], col0 = blockIdx.y * kCols;
   const int cols = min(kCols, rows * a.group - tile * QT - col0);
@@ -369,21 +377,26 @@ page_attention_join_kernel(Args a) {
 }
 
 // ---- host side -----------------------------------------------------------------------------------
-struct Plan { int workers; bool whole; };
+struct Plan { int workers, grid; bool whole; };
 template <class I>
 constexpr int64_t kPartialBytes = 2 * I::kSlotFloats * (int64_t)sizeof(float) + kJoinInts * (int64_t)sizeof(int32_t);   // a worker's
 
-// Workers of a call: as many as the chip holds at once, or fewer where there is no more to do; whole triples where no request is long.
+// Workers of a call: as many as the chip holds at once, or fewer where there is no more to do.  Triples stay whole, which saves the second launch, where
+// none can be long: up to kWholeSteps steps, or twice that where they fill half the chip.  (What a table has room for counts, lengths are on the device.)
+//   bf16, one column, 128 keys a step: 8 triples of 4 steps 10.4 us whole, 10.5 divided, of 6 steps 12.6 and 10.7; 128 triples of 8 steps 16.8 and 21.6
+//   f32, 64 keys a step: 8 triples of 4 steps 13.2 and 11.9, of 2 steps 9.8 and 11.6; 128 triples of 8 steps 22.5 and 24.1, of 12 steps 29.9 and 28.6
+//   bf16, 128 columns, 64 keys a step: 8 triples of 8 steps 20.4 and 22.8, of 12 steps 27.0 and 18.9; 128 triples of 16 steps 34.8 and 38.9
 template <class I>
 Plan plan(int B, int M, int Hkv, int group, int width, int page_size) {
   const int64_t tiles = (int64_t)M * group / I::QT + (B < M ? B : M), triples = tiles * Hkv;
   const int64_t steps = ((int64_t)width * page_size + I::kStep - 1) / I::kStep;
   // what fits the chip, and PVF_PAGE_WORKSPACE: a number that 8 divides, for the order of workers on the XCDs
-  constexpr int64_t kRoom = PVF_PAGE_WORKSPACE / kPartialBytes<I> / 8 * 8, most = kCus * I::kPerCu < kRoom ? kCus * I::kPerCu : kRoom;
+  constexpr int64_t kRoom = PVF_PAGE_WORKSPACE / kPartialBytes<I> / 8 * 8, most = kCus * I::kPerCu < kRoom ? kCus * I::kPerCu : kRoom, kGrid = 4 * kCus * I::kPerCu;
+  const int64_t grid = triples < kGrid ? triples : kGrid;
   Plan p;
-  p.whole = steps <= I::kWholeSteps;
-  const int64_t want = p.whole ? triples : triples * steps;
-  p.workers = (int)(want < (p.whole ? 4 * most : most) ? want : (p.whole ? 4 * most : most));
+  p.whole = steps <= (triples < kCus / 2 ? 1 : 2) * I::kWholeSteps;
+  p.workers = (int)(p.whole ? grid : triples * steps < most ? triples * steps : most);
+  p.grid = I::kAsTheyCome && grid > p.workers ? (int)grid : p.workers;
   return p;
 }
 template <class I>
@@ -397,13 +410,14 @@ template <class I>
 Plan prepare(Args &a) {
   const Plan p = plan<I>(a.p.B, a.p.M, a.p.Hkv, a.group, a.p.width, a.p.page_size);
   a.whole = p.whole || p.workers == 1;
+  a.workers = p.workers;
   a.joins = a.whole ? nullptr : (int32_t *)(a.p.ws + (int64_t)p.workers * 2 * I::kSlotFloats);
   const int64_t chunk = (int64_t)(kPageSlots - 2) * a.p.page_size / I::kStep;
   a.chunk_steps = (int)(chunk < 1 << 20 ? chunk : 1 << 20);
   return p;
 }
 
-// more than 32 columns a tile, bf16 and d_head up to 128 (paged_attention_wide.hip)
+// many columns, bf16 and d_head up to 128 (paged_attention_wide.hip)
 pvf_status launch_wide(hipStream_t s, Args &a, int64_t pairs);
 int64_t wide_workspace(int B, int M, int Hkv, int group, int dh, int width, int page_size, int64_t pairs);
 

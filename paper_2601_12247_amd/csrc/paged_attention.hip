@@ -27,7 +27,8 @@ struct Inst {
   static constexpr int VE = kBf16 && DH >= 128 ? 8 : 4;
   static constexpr int NB = DH / (16 * VE), NT = DH / 16;
   static constexpr int kStep = 4 * KT;                  // keys a workgroup takes at once
-  static constexpr int QT = 16 * NQ, kDh = DH, kSplit = 0, kWholeSteps = 4;
+  static constexpr int QT = 16 * NQ, kDh = DH, kSplit = 4, kWholeSteps = kBf16 ? 4 : 3;
+  static constexpr bool kAsTheyCome = false;
   static constexpr int kOPad = DH + 4;
   static constexpr int kSlotFloats = QT * (DH + 2);     // a partial result: m[QT], l[QT], O[QT][DH]
   static constexpr int kRegs = (NT + KJ + 2) * 4 * NQ + NU * KJ * 4 + NU * 4 * NB * VE * (int)sizeof(T) / 4 + 64;   // about
@@ -269,10 +270,9 @@ page_attention_kernel(Args a) {
   __shared__ float s_m[4][I::QT], s_l[4][I::QT];
   __shared__ alignas(16) float s_o[4][16][I::kOPad];
   const int tid = threadIdx.x, wid = __builtin_amdgcn_readfirstlane(tid >> 6);
-  __shared__ int32_t s_bad;
   int worker;
   Line<I> line(a, blockIdx.x, gridDim.x, &worker);
-  if (!a.whole && tid == 0) a.joins[(int64_t)worker * kJoinInts] = 0;
+  if (!a.whole && worker < a.workers && tid == 0) a.joins[(int64_t)worker * kJoinInts] = 0;
   Request r;
   Piece piece;
   Pass<T, DH, NQ, kWhole> pass(a, s_pages);
@@ -310,7 +310,7 @@ page_attention_kernel(Args a) {
       const int k0 = s0 * I::kStep, k1 = (int)min((int64_t)r.len, (int64_t)s1 * I::kStep);
       meet();                             // the last chunk's pages, or the last piece's results, have been read
       pass.first_page = page_of(a, k0);
-      load_pages(a, line.b, k0, k1, pass.first_page, s_pages, &s_bad);
+      load_pages(a, line.b, k0, k1, pass.first_page, s_pages, nullptr);
       meet();
       int kb = k0 + wid * I::KT;
       if (kb < k1) {
@@ -377,27 +377,33 @@ page_attention_kernel(Args a) {
 }
 
 // ---- choice of an instance -----------------------------------------------------------------------
-// Columns of a tile by the mean number of (row, head) pairs that share a key head.
+// Columns of a tile by the mean number of (row, head) pairs that share a key head: two blocks, which leave one workgroup a CU, where one would read every
+// key twice.  64 requests of 2048 keys, 8 key heads, us with 16 and 32 columns:
+//   16 pairs: bf16 44.7 and 46.6 (d_head 64), 103 and 117 (128), 197 and 259 (256); f32 103 and 109 (64), 195 and 233 (128)
+//   24 pairs: bf16 80.5 and 46.8,             189 and 118,       367 and 264;       f32 190 and 109,      377 and 236
+// Many pairs in bf16 with d_head up to 128 are the wide kernel's; there, with 64 columns: 24 pairs 50.1 (d_head 64), 107 (128), 40 pairs 49.6 and 108
+// (32 columns: 83 and 209).
 template <class F>
 auto with_instance(int dtype, int64_t pairs, int dh, F f) {
+  const bool one = pairs <= 16;
   if (dtype == PVF_BF16) {
-    if (dh <= 64) return pairs <= 16 ? f(Inst<bf16_t, 64, 1>{}) : f(Inst<bf16_t, 64, 2>{});
-    if (dh <= 128) return pairs <= 16 ? f(Inst<bf16_t, 128, 1>{}) : f(Inst<bf16_t, 128, 2>{});
-    return pairs <= 16 ? f(Inst<bf16_t, 256, 1>{}) : f(Inst<bf16_t, 256, 2>{});
+    if (dh <= 64) return one ? f(Inst<bf16_t, 64, 1>{}) : f(Inst<bf16_t, 64, 2>{});
+    if (dh <= 128) return f(Inst<bf16_t, 128, 1>{});
+    return one ? f(Inst<bf16_t, 256, 1>{}) : f(Inst<bf16_t, 256, 2>{});
   }
-  if (dh <= 64) return pairs <= 16 ? f(Inst<float, 64, 1>{}) : f(Inst<float, 64, 2>{});
-  if (dh <= 128) return pairs <= 16 ? f(Inst<float, 128, 1>{}) : f(Inst<float, 128, 2>{});
+  if (dh <= 64) return one ? f(Inst<float, 64, 1>{}) : f(Inst<float, 64, 2>{});
+  if (dh <= 128) return one ? f(Inst<float, 128, 1>{}) : f(Inst<float, 128, 2>{});
   return f(Inst<float, 256, 1>{});
 }
 int64_t mean_pairs(int M, int B, int group) { return ((int64_t)M + B - 1) / B * group; }
-bool is_wide(int dtype, int64_t pairs, int dh) { return dtype == PVF_BF16 && dh <= 128 && pairs > 32; }
+bool is_wide(int dtype, int64_t pairs, int dh) { return dtype == PVF_BF16 && dh <= 128 && pairs > (dh <= 64 ? 32 : 16); }
 
 template <typename T, int DH, int NQ>
 pvf_status launch(Inst<T, DH, NQ>, hipStream_t s, Args &a) {
   typedef Inst<T, DH, NQ> I;
   const Plan p = prepare<I>(a);
-  if (a.p.dh == DH) page_attention_kernel<T, DH, NQ, true><<<p.workers, 256, 0, s>>>(a);
-  else page_attention_kernel<T, DH, NQ, false><<<p.workers, 256, 0, s>>>(a);
+  if (a.p.dh == DH) page_attention_kernel<T, DH, NQ, true><<<p.grid, 256, 0, s>>>(a);
+  else page_attention_kernel<T, DH, NQ, false><<<p.grid, 256, 0, s>>>(a);
   PVF_LAUNCH_CHECK(nullptr, "page_attention");
   if (!a.whole) {
     page_attention_join_kernel<T, I><<<dim3(p.workers - 1, I::QT / kJoinCols<I>), kJoinThreads, 0, s>>>(a);

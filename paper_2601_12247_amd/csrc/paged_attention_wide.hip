@@ -1,4 +1,4 @@
-// Attention over pages for many rows a request (paged_attention.h): bf16, more than 32 (row, head) pairs a key head.
+// Attention over pages for many rows a request (paged_attention.h): bf16, more (row, head) pairs a key head than 16 (d_head up to 128) or 32 (up to 64).
 //
 // One workgroup = 128 columns of one (request, key head), 32 a wave, or 64, with the waves in two pairs that take alternate halves of the keys.
 // 64 keys and their values at a time go from the pages into LDS (no detour over registers), one buffer ahead; S^T = K Q^T and O^T = V^T P^T on
@@ -35,7 +35,8 @@ __device__ __forceinline__ void wait_and_meet() {
 // CW: waves beside each other over columns; the 4 / CW groups of them share out the keys of a step.
 template <int DH, int CW>
 struct WideInst {
-  static constexpr int kDh = DH, QT = 32 * CW, KW = 4 / CW, kStep = 64, kSubs = 2 / KW, kSplit = 8, kWholeSteps = 16, kPerCu = 2;
+  static constexpr int kDh = DH, QT = 32 * CW, KW = 4 / CW, kStep = 64, kSubs = 2 / KW, kSplit = 8, kWholeSteps = 8, kPerCu = 2;
+  static constexpr bool kAsTheyCome = true;
   static constexpr int NT = DH / 32, KJ = DH / 16;
   static constexpr int kRow = DH * 2, kChunks = DH / 8, kTile = kStep * kRow;   // bytes of a key, its chunks, bytes of 64 keys
   static constexpr int kLoads = kTile / 4096, kKeys = 1024 / kRow;             // loads of 1 KB a wave and tile, keys of one
@@ -54,7 +55,7 @@ page_attention_wide_kernel(Args a) {
   __shared__ int32_t s_bad;
   int worker;
   Line<I> line(a, blockIdx.x, gridDim.x, &worker);
-  if (!a.whole && tid == 0) a.joins[(int64_t)worker * kJoinInts] = 0;
+  if (!a.whole && worker < a.workers && tid == 0) a.joins[(int64_t)worker * kJoinInts] = 0;
   Request r;
   Piece piece;
 
@@ -383,6 +384,8 @@ page_attention_wide_kernel(Args a) {
   }
 }
 
+// 128 columns where 64 would read every key twice.  64 requests of 2048 keys, 8 key heads, us with 64 and 128 columns: 64 pairs 50.0 and 68.0 (d_head 64),
+// 110 and 133 (128); 72 pairs 88.6 and 68.2, 202 and 134; 128 pairs 90.3 and 71.9, 207 and 141.
 template <class F>
 auto with_wide(int64_t pairs, int dh, F f) {
   if (dh <= 64) return pairs <= 64 ? f(WideInst<64, 2>{}) : f(WideInst<64, 4>{});
@@ -393,8 +396,8 @@ template <int DH, int CW>
 pvf_status launch(WideInst<DH, CW>, hipStream_t s, Args &a) {
   typedef WideInst<DH, CW> I;
   const Plan p = prepare<I>(a);
-  if (a.p.dh == DH) page_attention_wide_kernel<DH, CW, true><<<p.workers, 256, 0, s>>>(a);
-  else page_attention_wide_kernel<DH, CW, false><<<p.workers, 256, 0, s>>>(a);
+  if (a.p.dh == DH) page_attention_wide_kernel<DH, CW, true><<<p.grid, 256, 0, s>>>(a);
+  else page_attention_wide_kernel<DH, CW, false><<<p.grid, 256, 0, s>>>(a);
   PVF_LAUNCH_CHECK(nullptr, "page_attention_wide");
   if (!a.whole) {
     page_attention_join_kernel<bf16_t, I><<<dim3(p.workers - 1, I::QT / kJoinCols<I>), kJoinThreads, 0, s>>>(a);
