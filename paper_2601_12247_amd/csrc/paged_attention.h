@@ -292,6 +292,8 @@ __device__ __forceinline__ uint32_t lower_parts(float x, float y) {
 }
 
 // ---- the join: block w joins the triple that worker w begins, if others end it ----------------------
+// A wait for the notes, one for the maxima and results, one sum over LDS: latency.  8 triples of 64 results of 4 columns 5.8 us, 68 of up to 8 results of 15
+// columns 4.8, the 32 divided ones of 9 x 32 windows 8.2.
 constexpr int kJoinThreads = 1024;
 template <class I>
 constexpr int kJoinCols = I::QT < 32 ? I::QT : 32;   // columns of a block
@@ -417,7 +419,7 @@ Plan prepare(Args &a) {
   return p;
 }
 
-// many columns, bf16 and d_head up to 128 (paged_attention_wide.hip)
+// many columns, bf16 (paged_attention_wide.hip)
 pvf_status launch_wide(hipStream_t s, Args &a, int64_t pairs);
 int64_t wide_workspace(int B, int M, int Hkv, int group, int dh, int width, int page_size, int64_t pairs);
 

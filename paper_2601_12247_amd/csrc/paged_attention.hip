@@ -8,6 +8,10 @@
 //
 // P enters the bf16 instruction as two bf16 parts (16 bits of it): the second instruction costs nothing beside the memory, and the result is
 // rounded once, to its own type.
+//
+// Bound by reading keys and values.  bf16, 64 requests of up to 8192 tokens, 8 key heads, groups of 4: 184 us for 1.05 GB (5.7 TB/s; a copy, which writes
+// as well, reaches 4.9), and 7 to join.  One request of 32768: 27.4 us for 134 MB (4.9 TB/s), and 6 to join.  Where there is little to read it is latency:
+// f32, one request of 128 tokens, 6.4 us; 17 of up to 1411 with 5 rows, 17.2 us and 4.8 to join for 21 MB, of which the first keys take 6.
 #include "paged_attention.h"
 
 #include <cmath>
@@ -378,25 +382,24 @@ page_attention_kernel(Args a) {
 
 // ---- choice of an instance -----------------------------------------------------------------------
 // Columns of a tile by the mean number of (row, head) pairs that share a key head: two blocks, which leave one workgroup a CU, where one would read every
-// key twice.  64 requests of 2048 keys, 8 key heads, us with 16 and 32 columns:
-//   16 pairs: bf16 44.7 and 46.6 (d_head 64), 103 and 117 (128), 197 and 259 (256); f32 103 and 109 (64), 195 and 233 (128)
-//   24 pairs: bf16 80.5 and 46.8,             189 and 118,       367 and 264;       f32 190 and 109,      377 and 236
-// Many pairs in bf16 with d_head up to 128 are the wide kernel's; there, with 64 columns: 24 pairs 50.1 (d_head 64), 107 (128), 40 pairs 49.6 and 108
-// (32 columns: 83 and 209).
+// key twice; in bf16 the wide kernel's.  64 requests of 2048 keys, 8 key heads, us:
+//   f32, 16 and 32 columns: 16 pairs 103 and 109 (d_head 64), 195 and 233 (128); 24 pairs 190 and 109, 377 and 236
+//   bf16, 16, 32 and the wide kernel's 64: 16 pairs 44.7, 46.6, 51.0 (64), 103, 117, 107 (128), 191, 259, - (256)
+//                                          24 pairs 80.5, 46.8, 50.1,      189, 118, 107,       367, 264, 203;   40 pairs of d_head 64 116, 83.2, 49.6
 template <class F>
 auto with_instance(int dtype, int64_t pairs, int dh, F f) {
   const bool one = pairs <= 16;
   if (dtype == PVF_BF16) {
     if (dh <= 64) return one ? f(Inst<bf16_t, 64, 1>{}) : f(Inst<bf16_t, 64, 2>{});
     if (dh <= 128) return f(Inst<bf16_t, 128, 1>{});
-    return one ? f(Inst<bf16_t, 256, 1>{}) : f(Inst<bf16_t, 256, 2>{});
+    return f(Inst<bf16_t, 256, 1>{});
   }
   if (dh <= 64) return one ? f(Inst<float, 64, 1>{}) : f(Inst<float, 64, 2>{});
   if (dh <= 128) return one ? f(Inst<float, 128, 1>{}) : f(Inst<float, 128, 2>{});
   return f(Inst<float, 256, 1>{});
 }
 int64_t mean_pairs(int M, int B, int group) { return ((int64_t)M + B - 1) / B * group; }
-bool is_wide(int dtype, int64_t pairs, int dh) { return dtype == PVF_BF16 && dh <= 128 && pairs > (dh <= 64 ? 32 : 16); }
+bool is_wide(int dtype, int64_t pairs, int dh) { return dtype == PVF_BF16 && pairs > (dh <= 64 ? 32 : 16); }
 
 template <typename T, int DH, int NQ>
 pvf_status launch(Inst<T, DH, NQ>, hipStream_t s, Args &a) {

@@ -1,9 +1,15 @@
-// Attention over pages for many rows a request (paged_attention.h): bf16, more (row, head) pairs a key head than 16 (d_head up to 128) or 32 (up to 64).
+// Attention over pages for many rows a request (paged_attention.h): bf16, more (row, head) pairs a key head than 16, or 32 where
+// d_head is at most 64.
 //
 // One workgroup = 128 columns of one (request, key head), 32 a wave, or 64, with the waves in two pairs that take alternate halves of the keys.
 // 64 keys and their values at a time go from the pages into LDS (no detour over registers), one buffer ahead; S^T = K Q^T and O^T = V^T P^T on
 // 32 x 32 x 16 matrix instructions.  A lane of S^T holds one column and keys 8 (e / 4) + 4 (lane / 32) + e % 4; P^T is multiplied as it is held, with V^T's
 // keys in that order: transposing reads give a lane four keys of one dimension.
+//
+// Bound by what a step takes in turn: 64 keys of 128 columns are 3400 cycles, 1545 of the matrix unit and about 1800 of the vector unit, which overlap in
+// part, and with the loads behind them.  bf16, 9 windows of 128 rows over up to 1280 tokens, 32 heads of 128: 58 us for 24 GFLOP (36 with P's second
+// part: 0.62 PFLOP/s) and 200 MB (3.6 TB/s), and 8 to join.  Without the products 50 us, without the loads 54.  Eight waves a workgroup took 85 us, two
+// workgroups of 64 columns 81.
 //
 // LDS rows are keys, in 16-byte chunks; chunk x of a key lies at x ^ turn(key), so that equal chunks of 8 keys (the operand K) and pairs of chunks of 4 keys
 // (V^T) fall on different banks.
@@ -35,7 +41,7 @@ __device__ __forceinline__ void wait_and_meet() {
 // CW: waves beside each other over columns; the 4 / CW groups of them share out the keys of a step.
 template <int DH, int CW>
 struct WideInst {
-  static constexpr int kDh = DH, QT = 32 * CW, KW = 4 / CW, kStep = 64, kSubs = 2 / KW, kSplit = 8, kWholeSteps = 8, kPerCu = 2;
+  static constexpr int kDh = DH, QT = 32 * CW, KW = 4 / CW, kStep = 64, kSubs = 2 / KW, kSplit = 8, kWholeSteps = 8, kPerCu = DH <= 128 ? 2 : 1;
   static constexpr bool kAsTheyCome = true;
   static constexpr int NT = DH / 32, KJ = DH / 16;
   static constexpr int kRow = DH * 2, kChunks = DH / 8, kTile = kStep * kRow;   // bytes of a key, its chunks, bytes of 64 keys
@@ -45,7 +51,7 @@ struct WideInst {
 };
 
 template <int DH, int CW, bool kWhole>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(WideInst<DH, CW>::kPerCu, WideInst<DH, CW>::kPerCu)))
 page_attention_wide_kernel(Args a) {
   typedef WideInst<DH, CW> I;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[4 * I::kTile];   // keys, values; twice
@@ -154,25 +160,27 @@ page_attention_wide_kernel(Args a) {
         for (int u = 0; u < I::kSubs; ++u)
 #pragma unroll
           for (int e = 0; e < 16; ++e) s[u][e] = 0.f;
-        // operands of half a row are read while the other half is multiplied
-        constexpr int kHalf = I::KJ / 2;
-        bf16x8 kf[2][kHalf][I::kSubs];
-        auto read_keys = [&](int half) {
+        // operands of one part of a row are read while another is multiplied
+        constexpr int kPart = I::KJ / 2 < 4 ? I::KJ / 2 : 4, kParts = I::KJ / kPart;
+        bf16x8 kf[2][kPart][I::kSubs];
+        auto read_keys = [&](int part) {
 #pragma unroll
-          for (int j = 0; j < kHalf; ++j)
+          for (int j = 0; j < kPart; ++j)
 #pragma unroll
-            for (int u = 0; u < I::kSubs; ++u) kf[half][j][u] = *(const bf16x8 *)(ks + (u * I::KW + kw) * 32 * I::kRow + k_rd[half * kHalf + j]);
+            for (int u = 0; u < I::kSubs; ++u) kf[part % 2][j][u] = *(const bf16x8 *)(ks + (u * I::KW + kw) * 32 * I::kRow + k_rd[part * kPart + j]);
           __builtin_amdgcn_sched_barrier(0);
         };
         read_keys(0);
         read_keys(1);
         find(kb + 2 * I::kStep);                               // beside the products
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
+        for (int part = 0; part < kParts; ++part) {
 #pragma unroll
-          for (int j = 0; j < kHalf; ++j)
+          for (int j = 0; j < kPart; ++j)
 #pragma unroll
-            for (int u = 0; u < I::kSubs; ++u) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[half][j][u], q[half * kHalf + j], s[u], 0, 0, 0);
+            for (int u = 0; u < I::kSubs; ++u) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[part % 2][j][u], q[part * kPart + j], s[u], 0, 0, 0);
+          if (part + 2 < kParts) read_keys(part + 2);
+        }
         if (more) wait_and_meet<2 * I::kLoads>(); else wait_and_meet<0>();     // its values are there, its keys have been read
         if (more) load_keys(kBuf);
         bool odd = false;
@@ -277,14 +285,14 @@ page_attention_wide_kernel(Args a) {
         for (int k = 0; k < kBlocks; ++k) {
           const bool more_blocks = k + 1 < kBlocks;
           if (more_blocks) read_values(k + 1);
-          constexpr int kProducts = 2 * I::NT, kEach = 8 / kProducts;   // probabilities beside a product
+          constexpr int kProducts = 2 * I::NT;
 #pragma unroll
           for (int i = 0; i < kProducts; ++i) {
             const int t = i % I::NT;
             o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt[k % 2][t], __builtin_bit_cast(bf16x8, i < I::NT ? hi[k % 2] : lo[k % 2]), o[t], 0, 0, 0);
             if (more_blocks) {
 #pragma unroll
-              for (int x = kEach * i; x < kEach * (i + 1); ++x) {
+              for (int x = 8 * i / kProducts; x < 8 * (i + 1) / kProducts; ++x) {   // probabilities beside a product
                 exponential(k + 1, x);
                 if (x > 0) take(k + 1, x - 1);
               }
@@ -385,11 +393,12 @@ page_attention_wide_kernel(Args a) {
 }
 
 // 128 columns where 64 would read every key twice.  64 requests of 2048 keys, 8 key heads, us with 64 and 128 columns: 64 pairs 50.0 and 68.0 (d_head 64),
-// 110 and 133 (128); 72 pairs 88.6 and 68.2, 202 and 134; 128 pairs 90.3 and 71.9, 207 and 141.
+// 110 and 133 (128); 72 pairs 88.6 and 68.2, 202 and 126; 128 pairs 90.3 and 71.9, 207 and 128.  d_head 256: 64 pairs 214, 128 pairs 277 (one workgroup a CU).
 template <class F>
 auto with_wide(int64_t pairs, int dh, F f) {
   if (dh <= 64) return pairs <= 64 ? f(WideInst<64, 2>{}) : f(WideInst<64, 4>{});
-  return pairs <= 64 ? f(WideInst<128, 2>{}) : f(WideInst<128, 4>{});
+  if (dh <= 128) return pairs <= 64 ? f(WideInst<128, 2>{}) : f(WideInst<128, 4>{});
+  return pairs <= 64 ? f(WideInst<256, 2>{}) : f(WideInst<256, 4>{});
 }
 
 template <int DH, int CW>

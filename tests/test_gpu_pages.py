@@ -291,7 +291,8 @@ def test_many_requests():
 @pytest.mark.parametrize("nreq,Hkv,n,dh,longest,causal", [
     (10, 30, 128, 128, 0, False), (10, 30, 128, 64, 0, True), (47, 10, 128, 64, 0, False), (75, 8, 128, 128, 0, True), (110, 10, 128, 64, 0, False), (70, 8, 50, 128, 0, True),
     (40, 7, 50, 64, 0, False), (130, 1, 128, 128, 0, True), (65, 4, 33, 72, 0, False), (9, 4, 128, 128, 9000, True), (70, 4, 128, 128, 9000, False), (66, 2, 64, 64, 5000, True),
-    (1, 1, 128, 128, 30000, False), (1, 2, 50, 128, 20000, True), (3, 5, 300, 96, 3000, True)])
+    (1, 1, 128, 128, 30000, False), (1, 2, 50, 128, 20000, True), (3, 5, 300, 96, 3000, True), (40, 8, 100, 256, 0, False),
+    (12, 8, 40, 256, 0, True), (6, 5, 128, 200, 4000, True), (3, 4, 33, 136, 5000, False), (300, 1, 20, 256, 0, True)])
 def test_windows_dealt_to_workers(nreq, Hkv, n, dh, longest, causal):
     lens = [130 + (97 * b) % 331 for b in range(nreq)]
     rows = [n - (b % 5 == 3) * (b % 17) for b in range(nreq)]
