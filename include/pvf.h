@@ -389,7 +389,7 @@ pvf_status pvf_page_trim(void *stream, const int32_t *seq_len, const int32_t *ke
 /* Fresh rows enter the cache: qkv [M, (H + 2 Hkv) * d_head] (q | k | v, rows qkv_stride apart) holds the projections of rows at positions pos [M];
  * q_out [M, H * d_head] (rows q_stride apart) = rotated q, and slot[m] of the caches = rotated k and v of row m.  Rotary embedding as in pvf_model_cfg, its
  * angles in float64, at any position.  A row whose slot lies outside the cache is padding: nothing is written for it.  Slots of a call have to differ
- * (of rows with one slot, any one's elements may stay).  q_out may be the q part of qkv itself. */
+ * (of rows with one slot, any one's elements may stay).  q_out may be the q part of qkv itself; nothing else may overlap. */
 pvf_status pvf_page_store(void *stream, int32_t dtype, const void *qkv, int64_t qkv_stride, const int32_t *pos, const int32_t *slot, int32_t M,
                           int32_t H, int32_t Hkv, int32_t d_head, float rope_theta, void *q_out, int64_t q_stride, void *k_cache, void *v_cache,
                           int32_t n_pages, int32_t page_size, int64_t k_page_stride, int64_t v_page_stride);
@@ -402,7 +402,8 @@ pvf_status pvf_page_store(void *stream, int32_t dtype, const void *qkv, int64_t 
  * Scores, statistics and sums are float32 (probabilities enter the bf16 matrix instruction in two parts, 16 bits), rounded once at the end; the order of
  * sums goes by the lengths of all requests in the call, so last bits may differ between batches, not between calls.
  * Long caches are divided over the chip and joined by a second launch: workspace of pvf_page_attention_workspace bytes (0 where nothing is divided;
- * PVF_PAGE_WORKSPACE suffices for every call; a negative status where the sizes are refused).  Calls that overlap need workspaces of their own. */
+ * PVF_PAGE_WORKSPACE suffices for every call; a negative status where the sizes are refused).  Calls that overlap need workspaces of their own.
+ * out may be q itself; nothing else that is read may overlap what is written. */
 #define PVF_PAGE_WORKSPACE ((int64_t)1 << 26)
 int64_t pvf_page_attention_workspace(int32_t dtype, int32_t B, int32_t M, int32_t H, int32_t Hkv, int32_t d_head, int32_t width, int32_t page_size);
 pvf_status pvf_page_attention(void *stream, int32_t dtype, const void *q, int64_t q_stride, const void *k_cache, const void *v_cache,

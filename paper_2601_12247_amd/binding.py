@@ -710,7 +710,7 @@ def page_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor
                    workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """softmax(scale * q k^T) v of rows q [M, H, d_head] against the seq_len[b] tokens of their request: rows cu_rows[b] .. cu_rows[b + 1] - 1 are request b's
     (None: one row each).  causal: a request's rows are its last tokens and see no later ones.  scale: d_head^-0.5 by default.  q and out may be strided
-    by rows.  workspace: uint8, for callers who keep one (PAGE_WORKSPACE bytes); calls that overlap need one each."""
+    by rows, out may be q.  workspace: uint8, for callers who keep one (PAGE_WORKSPACE bytes); calls that overlap need one each."""
     dev, (M, H, dh), dtype, B, i32, shape = q.get_device(), q.shape, q.dtype, seq_len.numel(), _i32_t, k_cache.shape
     assert len(shape) == 4 and shape[3] == dh, "caches are [n_pages, Hkv, page_size, d_head], d_head that of q"
     n_pages, Hkv, P, _ = shape

@@ -312,6 +312,25 @@ def test_keys_divided_between_workers(nreq, H, Hkv, n, dh):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nreq,H,Hkv,n,dh", [(18, 8, 8, 1, 64), (40, 8, 8, 1, 64), (70, 8, 4, 1, 80), (130, 3, 3, 2, 64), (64, 8, 8, 1, 32), (30, 20, 10, 5, 128)])
+def test_requests_of_like_lengths(dtype, nreq, H, Hkv, n, dh):
+    """Whole triples, one a CU, and the others divided: 144 of them, 320, 280 of more than 64 requests, 390; 512, all divided; 300 of ten columns."""
+    lens = [1100 - 7 * (b % 9) for b in range(nreq)]
+    Pool(lens, H, Hkv, dh, 24, dtype, seed=nreq, width=100).rows([n] * nreq).check(causal=nreq % 4 == 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,n,width", [([300, 17, 90], 1, 20), ([5000, 17, 900], 1, 400), ([2000, 700, 5000], 40, 400)])
+def test_results_in_place_of_the_queries(dtype, lens, n, width):
+    pool = Pool(lens, 8, 2, 128, 16, dtype, seed=n, width=width).rows([n] * len(lens))
+    want = pool.run()
+    q, dev = pool.q.cuda(), pool.pool.cuda()
+    k, v = (dev[:, i].view(dev.shape[0], 2, 16, 128) for i in (0, 1))
+    B.page_attention(q, k, v, pool.table.cuda(), i32(lens), cu_rows=i32(pool.cu), out=q)
+    assert torch.equal(q.cpu(), want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_scales(dtype):
     for scale in (0.0, 0.7, -0.2, 3.0):
         Pool([300, 77], 4, 2, 64, 16, dtype, seed=6).rows([2, 1]).check(scale=scale)
