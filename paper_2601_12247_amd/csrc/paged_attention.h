@@ -109,10 +109,11 @@ struct Line {
     *worker = block;
     base = rest_at = rest_end = 0;
     const bool counted = chunk != 1 || all >> 31;
-    if (!counted) {
+    auto longer = [&](uint32_t cus) { return __builtin_amdgcn_ballot_w64((uint32_t)longest > all / cus + I::kSplit) != 0; };
+    if (!counted && !longer(kCus)) {
       const uint32_t t = last_lane(wave_scan(all_triples));
       const bool many = t >= workers - workers / 8;
-      if ((I::kAsTheyCome || (t >= kCus / 2 && !many)) && __builtin_amdgcn_ballot_w64((uint32_t)longest > all / (many ? 2 * kCus : kCus) + I::kSplit) == 0) {
+      if (many ? I::kAsTheyCome && !longer(2 * kCus) : I::kAsTheyCome || t >= kCus / 2) {
         const uint32_t takers = many ? (uint32_t)grid : min(workers, (uint32_t)kCus), each = (t + takers - 1) / takers, dealt = many ? t : min(t, takers);
         if (dealt < t) {                  // steps of the triples that are dealt out lie in front of the others'
           if (a.p.B > kWave) load(0);
@@ -293,7 +294,7 @@ __device__ __forceinline__ uint32_t lower_parts(float x, float y) {
 
 // ---- the join: block w joins the triple that worker w begins, if others end it ----------------------
 // A wait for the notes, one for the maxima and results, one sum over LDS: latency.  8 triples of 64 results of 4 columns 5.8 us, 68 of up to 8 results of 15
-// columns 4.8, the 32 divided ones of 9 x 32 windows 8.2.
+// columns 4.8, the 32 divided ones of 9 x 32 windows 8.2.  Sixteen or eight columns of a wide tile to a workgroup took 5 and 12 us more.
 constexpr int kJoinThreads = 1024;
 template <class I>
 constexpr int kJoinCols = I::QT < 32 ? I::QT : 32;   // columns of a block
