@@ -252,13 +252,15 @@ page_trim_pages_kernel(PageTrim a) {
 
 // ---- store -------------------------------------------------------------------------------------
 // One pass over the rows, bound by HBM.  A workgroup takes kRows rows; a thread takes units of 2 x VEC elements, i .. i + VEC - 1 of a head
-// and their partners i + dh / 2 .., so that a rotation needs no other thread.  Angles are products in float64, brought to one turn there
+// and their partners i + dh / 2 .., so that a rotation needs no other thread.  Heads of at most 128 bytes (kNarrow) would be written in pieces of half a
+// line or less: there a unit is VEC elements and its partners are read as well (32 + 2 x 8 heads of 64 in bf16, 12000 rows: 27.4 us, 36.7 with pairs; of
+// 256, 3000 rows: 33.4 and 27.3).  The lanes of a head are then in one wave, which has read all of it before it writes any: q_out may be qkv.  Angles are products in float64, brought to one turn there
 // (position 2^31 is as exact as position 1), their sine and cosine in float32, once for each row and pair.
 // 11520 rows of 32 + 2 x 32 heads of 128, bf16: 117 us for 566 MB read and written (4.84 TB/s, a copy's 4.94).
 template <typename T, int VEC>
 struct alignas(sizeof(T) * VEC) Pack { T v[VEC]; };
 
-template <typename T, int VEC, int kRows>
+template <typename T, int VEC, int kRows, bool kNarrow>
 __global__ void __launch_bounds__(256)
 page_store_kernel(PageStore a) {
   __shared__ float2 s_cs[kRows * 128];
@@ -279,7 +281,7 @@ page_store_kernel(PageStore a) {
     s_cs[i] = make_float2(cs, sn);
   }
   __syncthreads();
-  const int per_head = half / VEC, heads = a.H + 2 * a.Hkv, units = rows * heads * per_head;
+  const int per_head = (kNarrow ? a.dh : half) / VEC, heads = a.H + 2 * a.Hkv, units = rows * heads * per_head;
   const int64_t head_stride = (int64_t)a.page_size * a.dh;
   const T *qkv = (const T *)a.qkv;
   constexpr int kHeld = 4;                                     // units a thread has on the way (q_out may be the rows' own q part, so loads are not moved over stores)
@@ -294,17 +296,19 @@ page_store_kernel(PageStore a) {
       head[i] = x - row[i] * heads;
       const T *src = qkv + (int64_t)(m0 + row[i]) * a.qkv_stride + (int64_t)head[i] * a.dh + c[i];
       lo[i] = *(const V *)src;
-      hi[i] = *(const V *)(src + half);
+      hi[i] = *(const V *)(kNarrow && c[i] >= half ? src - half : src + half);
     }
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
       if (u0 + i * 256 >= units || s_k[row[i]] < 0) continue;
       if (head[i] < a.H + a.Hkv) {
+        const bool upper = kNarrow && c[i] >= half;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-          const float2 cs = s_cs[row[i] * half + c[i] + e];
-          const float2 t = rotate_pair(to_float(lo[i].v[e]), to_float(hi[i].v[e]), cs.x, cs.y);
-          lo[i].v[e] = from_float<T>(t.x);
+          const float2 cs = s_cs[row[i] * half + (upper ? c[i] - half : c[i]) + e];
+          const float x = to_float(lo[i].v[e]), y = to_float(hi[i].v[e]);
+          const float2 t = rotate_pair(upper ? y : x, upper ? x : y, cs.x, cs.y);
+          lo[i].v[e] = from_float<T>(upper ? t.y : t.x);
           hi[i].v[e] = from_float<T>(t.y);
         }
       }
@@ -312,17 +316,17 @@ page_store_kernel(PageStore a) {
                : head[i] < a.H + a.Hkv ? (T *)a.k_cache + s_k[row[i]] + (head[i] - a.H) * head_stride
                                        : (T *)a.v_cache + s_v[row[i]] + (head[i] - a.H - a.Hkv) * head_stride;
       *(V *)(dst + c[i]) = lo[i];
-      *(V *)(dst + c[i] + half) = hi[i];
+      if (!kNarrow) *(V *)(dst + c[i] + half) = hi[i];
     }
   }
 }
 
 // Four rows a workgroup keep more loads on the way, one spreads few rows over the chip: 512 rows of 32 + 2 x 8 heads of 128, bf16, 6.1 us with one and 8.3
 // with four, 1024 8.7 and 9.1, 2048 14.0 and 13.1, 4096 22.3 and 19.3.
-template <typename T, int VEC>
+template <typename T, int VEC, bool kNarrow>
 void store_rows(hipStream_t s, const PageStore &a) {
-  if (a.M <= 1024) page_store_kernel<T, VEC, 1><<<a.M, 256, 0, s>>>(a);
-  else page_store_kernel<T, VEC, 4><<<(a.M + 3) / 4, 256, 0, s>>>(a);
+  if (a.M <= 1024) page_store_kernel<T, VEC, 1, kNarrow><<<a.M, 256, 0, s>>>(a);
+  else page_store_kernel<T, VEC, 4, kNarrow><<<(a.M + 3) / 4, 256, 0, s>>>(a);
 }
 
 }  // namespace
@@ -358,9 +362,13 @@ pvf_status launch_page_trim(hipStream_t s, const PageTrim &a) {
 }
 
 pvf_status launch_page_store(hipStream_t s, int dtype, const PageStore &a) {
-  if (dtype == PVF_F32) store_rows<float, 4>(s, a);
-  else if (a.dh % 16 == 0) store_rows<bf16_t, 8>(s, a);
-  else store_rows<bf16_t, 4>(s, a);
+  const int size = dtype == PVF_F32 ? 4 : 2, lanes = a.dh * size / 16;
+  const bool narrow = a.dh * size % 32 == 0 && lanes <= 8 && (lanes & (lanes - 1)) == 0;      // whole heads in a wave
+  if (dtype == PVF_F32 && narrow) store_rows<float, 4, true>(s, a);
+  else if (dtype == PVF_F32) store_rows<float, 4, false>(s, a);
+  else if (narrow) store_rows<bf16_t, 8, true>(s, a);
+  else if (a.dh % 16 == 0) store_rows<bf16_t, 8, false>(s, a);
+  else store_rows<bf16_t, 4, false>(s, a);
   PVF_LAUNCH_CHECK(nullptr, "page_store");
   return PVF_OK;
 }

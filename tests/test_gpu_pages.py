@@ -179,7 +179,8 @@ def check_store(M, H, Hkv, dh, P, dtype, theta=1e4, apart=0, page_apart=0, in_pl
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("M,H,Hkv,dh,P", [(1, 1, 1, 8, 8), (1, 32, 8, 128, 16), (2, 4, 4, 64, 16), (7, 12, 3, 80, 24), (33, 3, 3, 72, 8), (64, 32, 32, 128, 64), (513, 5, 1, 96, 40),
-                                          (514, 2, 2, 256, 16), (1021, 7, 7, 24, 8), (600, 1, 2, 16, 8), (515, 0, 2, 64, 16)])
+                                          (514, 2, 2, 256, 16), (1021, 7, 7, 24, 8), (600, 1, 2, 16, 8), (515, 0, 2, 64, 16),
+                                          (1025, 3, 3, 64, 16), (1030, 4, 2, 128, 24), (1027, 2, 1, 80, 8), (1026, 5, 1, 32, 8), (1029, 1, 1, 8, 16)])
 def test_stored_rows_are_the_reference_s(dtype, M, H, Hkv, dh, P):
     check_store(M, H, Hkv, dh, P, dtype)
     check_store(M, H, Hkv, dh, P, dtype, apart=16, page_apart=48, in_place=H > 0, theta=5e5, seed=1)
@@ -190,6 +191,7 @@ def test_stored_rows_at_far_positions(dtype):
     """Angles of the last positions that 31 bits hold: float32 would be off by whole turns."""
     check_store(40, 4, 2, 128, 16, dtype, theta=1e4, top=2 ** 31 - 1)
     check_store(600, 2, 1, 64, 16, dtype, theta=1.5, top=2 ** 31 - 1)
+    check_store(1400, 2, 1, 128, 16, dtype, theta=1e6, top=2 ** 31 - 1)
 
 
 # ---------------------------------------------------------------- attention
