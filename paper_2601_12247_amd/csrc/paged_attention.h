@@ -59,6 +59,7 @@ struct Line {
   uint32_t left;                          // items of the last piece's triple behind it
 
   static constexpr int kOver = 1 << 30;
+  static constexpr int kTogether = 4;     // times 64 requests on their way at once, where there are more than 64 (4096 of 16 keys: 84.3 -> 69.6 us)
   static constexpr uint32_t kWhole = 1u << 30;                 // more steps than a triple has
 
   __device__ __forceinline__ static int steps_of(int len) { return max((len + I::kStep - 1) / I::kStep, 1); }
@@ -67,42 +68,58 @@ struct Line {
   __device__ __forceinline__ uint32_t chunks_of(int keys) const { return chunk == 1 ? (uint32_t)steps_of(keys) : ((uint32_t)steps_of(keys) + chunk - 1) / chunk; }
   __device__ __forceinline__ uint32_t items_of(int rows, int keys) const { return triples_of(rows) * chunks_of(keys); }
 
-  __device__ __forceinline__ void load(int from) {
-    b0 = from;
+  struct Raw { int len, r0, r1; };
+  __device__ __forceinline__ Raw fetch(int from) const {
     const int i = from + (threadIdx.x & 63);
-    row0 = n = len = 0;
+    Raw w = {0, 0, 0};
     if (i < a.p.B) {
-      const int raw = a.p.seq_len[i], most = a.p.width * a.p.page_size;
-      int r0 = i, r1 = i + 1;
+      w = {a.p.seq_len[i], i, i + 1};
       if (a.p.cu_rows) {
-        r0 = a.p.cu_rows[i];
-        r1 = a.p.cu_rows[i + 1];
+        w.r0 = a.p.cu_rows[i];
+        w.r1 = a.p.cu_rows[i + 1];
       }
-      row0 = min(max(r0, 0), a.p.M);
-      n = max(min(r1, a.p.M) - row0, 0);
-      len = min(max(raw, 0), most);
-      if (raw > most) row0 |= kOver;
     }
+    return w;
   }
+  __device__ __forceinline__ void take(int from, const Raw &w) {
+    const int most = a.p.width * a.p.page_size;
+    b0 = from;
+    row0 = min(max(w.r0, 0), a.p.M);
+    n = max(min(w.r1, a.p.M) - row0, 0);
+    len = min(max(w.len, 0), most);
+    if (w.len > most) row0 |= kOver;
+  }
+  __device__ __forceinline__ void load(int from) { take(from, fetch(from)); }
 
   // Triples stay whole where the host says so.  Else, unless one is longer than its share of all steps by more than kSplit (what dividing costs, in steps):
   // where they are fewer than workers, each CU takes one and the rest is divided between the workers that have none; where they are more, instances with
   // large partial results leave them whole, for the grid's workgroups as they come (a longest one at the end then costs less than dividing).  On the others
   // a few triples (half the CUs) are divided, too.
   //   bf16, 9 x 32 triples of 128 columns, 1280 keys: 65.4 us; 70.6 if none is divided, 81 with equal shares of all steps
-  //   bf16, 20 x 32 of them: 121 us (90 with lengths from half of that on); 154 (124) with equal shares
+  //   bf16, 20 x 32 of them: 126 us (94 with lengths from half of that on); 154 (124) with equal shares
   //   bf16, 32 x 8 triples of one column, 2048 keys: 45.8 us; 49.8 with equal shares
   __device__ __forceinline__ Line(const Args &args, int block, int grid, int *worker) : a(args) {
     const uint32_t workers = (uint32_t)a.workers;
     chunk = a.whole ? kWhole : 1;
     uint32_t sum = 0, all_triples = 0;
     int longest = 0;
-    for (int from = 0; from < a.p.B; from += kWave) {
-      load(from);
+    auto add = [&](int from, const Raw &w) {
+      take(from, w);
       const uint32_t mine = items_of(n, len);
       sum = __builtin_elementwise_add_sat(sum, chunk == 1 && __umulhi(triples_of(n), (uint32_t)steps_of(len)) ? 0xffffffffu : mine);
       longest = max(longest, n > 0 ? steps_of(len) : 0);
       all_triples += triples_of(n);
+    };
+    if (a.p.B <= kWave) {
+      add(0, fetch(0));
+    } else {
+      for (int from = 0; from < a.p.B; from += kTogether * kWave) {
+        Raw w[kTogether];
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) w[k] = fetch(from + k * kWave);
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) add(from + k * kWave, w[k]);
+      }
     }
     uint32_t all = last_lane(wave_scan(sum));
     share = (all + workers - 1) / workers;
@@ -188,12 +205,21 @@ struct Line {
       chunk = 1;
       begin();
     }
-    uint64_t beyond;
-    while (beyond = __builtin_amdgcn_ballot_w64(upto > at), beyond == 0) {
-      base = last_lane(upto);
-      if (b0 + kWave >= a.p.B) return false;
-      load(b0 + kWave);
-      upto = base + wave_scan(items_of(n, len));
+    uint64_t beyond = __builtin_amdgcn_ballot_w64(upto > at);
+    while (beyond == 0) {
+      const int from = b0 + kWave;
+      if (from >= a.p.B) return false;
+      Raw w[kTogether];
+#pragma unroll
+      for (int k = 0; k < kTogether; ++k) w[k] = fetch(from + k * kWave);
+#pragma unroll
+      for (int k = 0; k < kTogether; ++k)
+        if (beyond == 0) {
+          base = last_lane(upto);
+          take(from + k * kWave, w[k]);
+          upto = base + wave_scan(items_of(n, len));
+          beyond = __builtin_amdgcn_ballot_w64(upto > at);
+        }
     }
     const int l = __builtin_ctzll(beyond);
     auto of = [&](int x) { return __builtin_amdgcn_readlane(x, l); };
@@ -398,7 +424,9 @@ Plan plan(int B, int M, int Hkv, int group, int width, int page_size) {
   const int64_t grid = triples < kGrid ? triples : kGrid;
   Plan p;
   p.whole = steps <= (triples < kCus / 2 ? 1 : 2) * I::kWholeSteps;
-  p.workers = (int)(p.whole ? grid : triples * steps < most ? triples * steps : most);
+  if (p.whole) p.workers = (int)(I::kAsTheyCome || grid < most ? grid : most);           // every workgroup looks at all lengths: 256 x 8
+                                                                                              // triples of 16 keys 20.6 us, 31.5 on four times as many
+  else p.workers = (int)(triples * steps < most ? triples * steps : most);
   p.grid = I::kAsTheyCome && grid > p.workers ? (int)grid : p.workers;
   return p;
 }
