@@ -424,8 +424,8 @@ Plan plan(int B, int M, int Hkv, int group, int width, int page_size) {
   const int64_t grid = triples < kGrid ? triples : kGrid;
   Plan p;
   p.whole = steps <= (triples < kCus / 2 ? 1 : 2) * I::kWholeSteps;
-  if (p.whole) p.workers = (int)(I::kAsTheyCome || grid < most ? grid : most);           // every workgroup looks at all lengths: 256 x 8
-                                                                                              // triples of 16 keys 20.6 us, 31.5 on four times as many
+  // (every workgroup looks at all lengths: 256 x 8 triples of one column and 16 keys 20.6 us, 31.5 on four times as many)
+  if (p.whole) p.workers = (int)(I::kAsTheyCome || grid < most ? grid : most);
   else p.workers = (int)(triples * steps < most ? triples * steps : most);
   p.grid = I::kAsTheyCome && grid > p.workers ? (int)grid : p.workers;
   return p;

@@ -23,11 +23,14 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void lptr_t;
 typedef __attribute__((address_space(3))) short4v *trptr_t;
 
-// 16 bytes a lane from global memory to LDS, lane after lane from `at` on, counted by vmcnt alone: written out because the compiler, which cannot
-// tell the tile on its way from the one that is read, waits for the builtin's loads before the next read of LDS.  There is no register that a load
-// writes.  Every wait for them stands below.
-__device__ __forceinline__ void load_to_lds(const void *src, uint32_t lane_bytes, uint32_t at) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(lane_bytes), "s"(src) : "memory", "m0");
+// Twice 16 bytes a lane from global memory to LDS, lane after lane from `at` and from 4096 bytes behind it on, counted by vmcnt alone: written out
+// because the compiler, which cannot tell the tile on its way from the one that is read, waits for the builtin's loads before the next read of LDS.  There is
+// no register that a load writes.  Every wait for them stands below.  The compiler does not count wait states into an asm block: addresses come from
+// v_readlane, and a load may read a scalar register five states after a vector instruction wrote it (s_mov, s_nop 3), m0 one after.
+__device__ __forceinline__ void load_to_lds(const void *src0, const void *src1, uint32_t lane_bytes, uint32_t at) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2\n\t"
+      "s_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3" ::"s"(at), "v"(lane_bytes), "s"(src0), "s"(src1) : "memory", "m0", "scc");
 }
 // at most N of this wave's loads are on the way; its LDS reads are done; then every wave's
 template <int N>
@@ -47,7 +50,7 @@ struct WideInst {
   static constexpr int kRow = DH * 2, kChunks = DH / 8, kTile = kStep * kRow;   // bytes of a key, its chunks, bytes of 64 keys
   static constexpr int kLoads = kTile / 4096, kKeys = 1024 / kRow;             // loads of 1 KB a wave and tile, keys of one
   static constexpr int kSlotFloats = QT * (DH + 2);
-  static_assert(CW * KW == 4 && kSubs * KW == 2, "four waves, two groups of 32 keys");
+  static_assert(CW * KW == 4 && kSubs * KW == 2 && kLoads % 2 == 0, "four waves, two groups of 32 keys, loads by two");
 };
 
 template <int DH, int CW, bool kWhole>
@@ -133,9 +136,13 @@ page_attention_wide_kernel(Args a) {
       int64_t values_at = 0;
       auto load = [&](int64_t at, uint32_t dst) {
 #pragma unroll
-        for (int i = 0; i < I::kLoads; ++i) {
-          const uint32_t lo = __builtin_amdgcn_readlane((int)at, i), hi = __builtin_amdgcn_readlane((int)(at >> 32), i);
-          if (kWhole || lane_chunk * 8 < a.p.dh) load_to_lds((const void *)((uint64_t)hi << 32 | lo), lane_bytes, dst + i * 4096);
+        for (int i = 0; i < I::kLoads; i += 2) {
+          auto from = [&](int l) {
+            const uint32_t lo = __builtin_amdgcn_readlane((int)at, l), hi = __builtin_amdgcn_readlane((int)(at >> 32), l);
+            return (const void *)((uint64_t)hi << 32 | lo);
+          };
+          const void *src0 = from(i), *src1 = from(i + 1);       // by all lanes: one that loads nothing may hold an address
+          if (kWhole || lane_chunk * 8 < a.p.dh) load_to_lds(src0, src1, lane_bytes, dst + i * 4096);
         }
       };
       int64_t keys_at = 0;
