@@ -26,11 +26,12 @@ typedef __attribute__((address_space(3))) short4v *trptr_t;
 // Twice 16 bytes a lane from global memory to LDS, lane after lane from `at` and from 4096 bytes behind it on, counted by vmcnt alone: written out
 // because the compiler, which cannot tell the tile on its way from the one that is read, waits for the builtin's loads before the next read of LDS.  There is
 // no register that a load writes.  Every wait for them stands below.  The compiler does not count wait states into an asm block: addresses come from
-// v_readlane, and a load may read a scalar register five states after a vector instruction wrote it (s_mov, s_nop 3), m0 one after.
+// v_readlane, and a load may read a scalar register five states after a vector instruction wrote it (s_mov, s_nop 3), m0 one after.  m0, which the
+// compiler reserves, is set by nothing else here.
 __device__ __forceinline__ void load_to_lds(const void *src0, const void *src1, uint32_t lane_bytes, uint32_t at) {
   asm volatile(
       "s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2\n\t"
-      "s_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3" ::"s"(at), "v"(lane_bytes), "s"(src0), "s"(src1) : "memory", "m0", "scc");
+      "s_add_u32 m0, m0, 0x1000\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3" ::"s"(at), "v"(lane_bytes), "s"(src0), "s"(src1) : "memory", "scc");
 }
 // at most N of this wave's loads are on the way; its LDS reads are done; then every wave's
 template <int N>

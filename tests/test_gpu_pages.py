@@ -451,6 +451,8 @@ def test_caches_past_32_bits():
     got = B.page_attention(q, k, v, table, i32([40]), cu_rows=i32([0, 40]), causal=True)
     want, slack = R.attention(q.cpu(), k.cpu(), v.cpu(), table.cpu(), [40], [0, 40], True, dh ** -0.5)
     assert R.close(got, want, slack)
+    last = B.page_attention(q[39:], k, v, table, i32([40]))
+    assert R.close(last, want[39:], slack[39:])
 
 
 def test_same_bits_every_time():
