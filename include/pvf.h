@@ -357,7 +357,7 @@ pvf_status pvf_gemm_mx_instance(int32_t call, int32_t w_fmt, int32_t dtype, int3
 /* ---- keys and values in pages -------------------------------------------------------------
  * A cache that B requests of different lengths share: pages of page_size tokens in one pool, [n_pages, Hkv, page_size, d_head] each for
  * keys and values in dtype.  What is in a page is contiguous; pages may lie further apart (page strides, in elements), as in a pool that holds
- * keys and values, or layers, side by side.  Row b of the table, int32 [B, width] (rows table_stride apart), names the pages of request b in
+ * keys and values, or layers, side by side.  Row b of the table, int32 [B, width] (rows table_stride >= width apart), names the pages of request b in
  * order: the token at position p lies on page table[b][p / page_size], and its slot is that page * page_size + p % page_size.
  * All arrays here are dev, int32 ones among them; lengths and counts stay on the GPU.  The calls allocate nothing and may be captured into a graph;
  * what they keep between their launches is in their outputs or the workspace, so calls on different streams may overlap if those differ.

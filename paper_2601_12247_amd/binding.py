@@ -567,7 +567,8 @@ def gemm_mx_instance(call: int, M: int, N: int, K: int, w_fmt: int = MX_E4M3, dt
 
 # ---- keys and values in pages --------------------------------------------------------------
 # A cache is a pair of tensors [n_pages, Hkv, page_size, d_head], pages contiguous but for the distance between them (stride(0)); a table is
-# int32 [B, width]; lengths, counts, positions and slots are int32.  These calls may stand in a loop of single tokens, where what a check costs counts:
+# int32 [B, width], its rows apart by stride(0): the library refuses a table whose rows overlap, as an expanded one's do (one row for all requests: copy it).
+# Lengths, counts, positions and slots are int32.  These calls may stand in a loop of single tokens, where what a check costs counts:
 # conditions are written out in one expression, and what does not fit is looked at again to say what it was.
 _i32_t = torch.int32
 
@@ -637,7 +638,7 @@ def page_extend(seq_len: torch.Tensor, n_rows: torch.Tensor, table: torch.Tensor
     if start is not None and not (start.dtype is i32 and start.numel() == B and start.is_contiguous() and start.get_device() == dev):
         _misfit(dev, (("start", start, B),))
     _page_call(lib().pvf_page_extend, dev, (
-        seq_len.data_ptr(), None if start is None else start.data_ptr(), n_rows.data_ptr(), B, table.data_ptr(), width, stride if stride > width else width, page_size,
+        seq_len.data_ptr(), None if start is None else start.data_ptr(), n_rows.data_ptr(), B, table.data_ptr(), width, stride, page_size,
         free_pages.data_ptr(), cap, n_free.data_ptr(), M, len_out.data_ptr(), free_out.data_ptr(), cu.data_ptr(), admitted.data_ptr(), place.data_ptr(),
         pos.data_ptr(), slot.data_ptr()))
     return out
@@ -662,7 +663,7 @@ def page_trim(seq_len: torch.Tensor, keep: torch.Tensor, table: torch.Tensor, fr
         _misfit(dev, (("seq_len", seq_len, B), ("keep", keep, B), ("seq_len of out", len_out, B), ("place", place, B + 1), ("n_free", n_free, 1),
                       ("n_free of out", free_out, 1), ("free_pages", free_pages, cap)))
     _page_call(lib().pvf_page_trim, dev, (
-        seq_len.data_ptr(), keep.data_ptr(), B, table.data_ptr(), width, stride if stride > width else width, page_size, free_pages.data_ptr(), cap,
+        seq_len.data_ptr(), keep.data_ptr(), B, table.data_ptr(), width, stride, page_size, free_pages.data_ptr(), cap,
         n_free.data_ptr(), len_out.data_ptr(), free_out.data_ptr(), place.data_ptr()))
     return out
 
@@ -737,7 +738,7 @@ def page_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor
     one, few = M <= 1, n_pages <= 1
     _page_call(lib().pvf_page_attention, dev, (
         _dtype_code(dtype), q.data_ptr(), 0 if one else q0, k_cache.data_ptr(), v_cache.data_ptr(), n_pages, P, 0 if few else k0, 0 if few else v0,
-        table.data_ptr(), width, stride if stride > width else width, seq_len.data_ptr(), None if cu_rows is None else cu_rows.data_ptr(), B, M, H, Hkv, dh,
+        table.data_ptr(), width, stride, seq_len.data_ptr(), None if cu_rows is None else cu_rows.data_ptr(), B, M, H, Hkv, dh,
         1 if causal else 0, dh ** -0.5 if scale is None else scale, out.data_ptr(), 0 if one else o0, workspace.data_ptr(), workspace.numel()))
     return out
 
