@@ -398,7 +398,8 @@ pvf_status pvf_page_store(void *stream, int32_t dtype, const void *qkv, int64_t 
  * h * H / Hkv .. of the rows share key head h.  Rows cu_rows[b] .. cu_rows[b + 1] - 1 belong to request b (cu_rows NULL: one row each, M = B); rows outside of
  * all stay as they are.  A row sees all seq_len[b] tokens (causal = 0), or with causal = 1 those up to its own place, the rows of a request being its
  * last tokens: seq_len[b] - n_rows + i + 1 for row i.  A row that sees no token is zeros; what lies behind the tokens a row sees has no part in it, whatever it
- * is.  A row that sees a token whose page is outside the cache or whose request is longer than its table is NaN.
+ * is.  A row that sees a token whose page is outside the cache is NaN, and so is each row that sees any token of a request longer than its table; what it
+ * sees goes by seq_len as given.
  * Scores, statistics and sums are float32 (probabilities enter the bf16 matrix instruction in two parts, 16 bits), rounded once at the end; the order of
  * sums goes by the lengths of all requests in the call, so last bits may differ between batches, not between calls.
  * Long caches are divided over the chip and joined by a second launch: workspace of pvf_page_attention_workspace bytes (0 where nothing is divided;

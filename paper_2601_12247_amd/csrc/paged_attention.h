@@ -28,15 +28,16 @@ struct Args {
   int32_t workers;                        // workgroups between which triples may be divided: the grid's first
   int32_t *joins;                         // [workers][kJoinInts]: the triple that worker w begins and others end
 };
-constexpr int kJoinInts = 8;              // workers that took it (0: none), its first row, rows, length, key head, tile
+constexpr int kJoinInts = 8;              // workers that took it (0: none), its first row, rows, length as told, key head, tile
 
 struct Request {
-  int row0, n, len, steps, tiles;         // its rows, visible keys, steps of keys and tiles of columns
-  bool over;                              // longer than its table
+  int row0, n, len, steps, tiles;         // its rows, keys in its table, steps of keys and tiles of columns
+  int told;                               // its length, by which rows see: more than len if it is
+  bool over;                              // longer than its table: keys are NaN, so every row is that sees one
 };
 
-// Keys that row `row` of a request sees.
-__device__ __forceinline__ int limit_of(const Args &a, int len, int n, int row) { return a.p.causal ? len - n + row + 1 : len; }
+// Keys that row `row` of a request sees whose length is `told`.
+__device__ __forceinline__ int limit_of(const Args &a, int told, int n, int row) { return a.p.causal ? told - n + row + 1 : told; }
 
 // The part of a triple that a worker takes next.
 struct Piece {
@@ -227,7 +228,8 @@ struct Line {
     r.row0 = of(row0) & ~kOver;
     r.over = (of(row0) & kOver) != 0;
     r.n = of(n);
-    r.len = of(len);
+    r.len = r.told = of(len);
+    if (r.over) r.told = max(a.p.seq_len[b], r.len);
     r.steps = steps_of(r.len);
     r.tiles = tiles_of(r.n);
     const uint32_t rel = at - ((uint32_t)of((int)upto) - items_of(r.n, r.len)), chunks = chunks_of(r.len), triple = chunks == 1 ? rel : rel / chunks;
@@ -248,7 +250,7 @@ struct Line {
   __device__ __forceinline__ void note_join(int worker, const Request &r, const Piece &p) const {
     int32_t *j = a.joins + (int64_t)worker * kJoinInts;
     *(int4 *)(j + 4) = make_int4(p.head, p.tile, 0, 0);
-    *(int4 *)j = make_int4((int)((left + share - 1) / share) + 1, r.row0, r.n, r.len);
+    *(int4 *)j = make_int4((int)((left + share - 1) / share) + 1, r.row0, r.n, r.told);
   }
 };
 
@@ -335,7 +337,7 @@ page_attention_join_kernel(Args a) {
   const int32_t *j = a.joins + (int64_t)blockIdx.x * kJoinInts;
   const int n = min(j[0], (int)(gridDim.x + 1 - blockIdx.x));    // (more only if lengths have changed under the call)
   if (n == 0) return;
-  const int row0 = j[1], rows = j[2], len = j[3], head = j[4], tile = j[5], col0 = blockIdx.y * kCols;
+  const int row0 = j[1], rows = j[2], told = j[3], head = j[4], tile = j[5], col0 = blockIdx.y * kCols;
   const int cols = min(kCols, rows * a.group - tile * QT - col0);
   if (cols <= 0) return;
   const float *first = partial<I>(a, blockIdx.x, true) + col0;
@@ -400,7 +402,7 @@ page_attention_join_kernel(Args a) {
     if (live && part == 0) {
       int row;
       const int64_t to = row_place(a, row0, head, tile * QT + col0 + col, a.p.out_stride, &row);
-      store4((T *)a.p.out + to + e % per_col * 4, sum, 1.0f / s_total[col], limit_of(a, len, rows, row) <= 0);
+      store4((T *)a.p.out + to + e % per_col * 4, sum, 1.0f / s_total[col], limit_of(a, told, rows, row) <= 0);
     }
   }
 }

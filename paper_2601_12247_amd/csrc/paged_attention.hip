@@ -292,7 +292,7 @@ page_attention_kernel(Args a) {
       const int col = 16 * nq + pass.c;
       int row;
       const T *src = (const T *)a.p.q + row_place(a, r.row0, piece.head, piece.tile * I::QT + col, a.p.q_stride, &row) + I::KE * pass.g;
-      pass.limit[nq] = col < cols ? limit_of(a, r.len, r.n, row) : INT32_MAX;
+      pass.limit[nq] = col < cols ? limit_of(a, r.told, r.n, row) : INT32_MAX;
       pass.least = min(pass.least, pass.limit[nq]);
 #pragma unroll
       for (int j = 0; j < I::KJ; ++j) {
@@ -366,7 +366,7 @@ page_attention_kernel(Args a) {
         if (piece.done) {
           int row;
           const int64_t at = row_place(a, r.row0, piece.head, piece.tile * I::QT + col, a.p.out_stride, &row);
-          store4((T *)a.p.out + at + d, sum, 1.0f / total, limit_of(a, r.len, r.n, row) <= 0);
+          store4((T *)a.p.out + at + d, sum, 1.0f / total, limit_of(a, r.told, r.n, row) <= 0);
         } else {
           *(floatx4 *)(slot + 2 * I::QT + col * DH + d) = sum;
           if (d == 0) {

@@ -93,8 +93,8 @@ page_attention_wide_kernel(Args a) {
     const bf16_t *vbase = (const bf16_t *)a.p.v_cache + (int64_t)piece.head * a.p.page_size * a.p.dh;
     int row;
     const int64_t q_at = row_place(a, r.row0, piece.head, piece.tile * I::QT + col, a.p.q_stride, &row);
-    const int limit = col < cols ? limit_of(a, len, r.n, row) : INT32_MAX;
-    const int least = limit_of(a, len, r.n, (int)((uint32_t)(piece.tile * I::QT) / (uint32_t)a.group));      // of the tile's columns: the first row's
+    const int limit = col < cols ? limit_of(a, r.told, r.n, row) : INT32_MAX;
+    const int least = limit_of(a, r.told, r.n, (int)((uint32_t)(piece.tile * I::QT) / (uint32_t)a.group));      // of the tile's columns: the first row's
     bf16x8 q[I::KJ];
 #pragma unroll
     for (int j = 0; j < I::KJ; ++j) {
