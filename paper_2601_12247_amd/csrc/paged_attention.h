@@ -86,7 +86,7 @@ struct Line {
     const int most = a.p.width * a.p.page_size;
     b0 = from;
     row0 = min(max(w.r0, 0), a.p.M);
-    n = max(min(w.r1, a.p.M) - row0, 0);
+    n = max(min(max(w.r1, 0), a.p.M) - row0, 0);   // (an offset far below zero less row0 would wrap)
     len = min(max(w.len, 0), most);
     if (w.len > most) row0 |= kOver;
   }

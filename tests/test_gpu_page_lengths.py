@@ -1,8 +1,9 @@
-"""Attention over pages of requests that are longer than their table: every row that sees a token is NaN, by the length as it was told, and rows that see none
-are zeros.  Every other row against tests/page_reference.py, with the slack that it derives."""
+"""Attention over pages where lengths and row offsets are not what a table or M has room for.  Requests longer than their table: every row that sees a token is
+NaN, by the length as it was told, and rows that see none are zeros.  Every other row against tests/page_reference.py, with the slack that it derives."""
 import pytest
 import torch
 
+from paper_2601_12247_amd import binding as B
 from tests import page_reference as R
 from tests.test_gpu_pages import Pool
 
@@ -51,3 +52,24 @@ def test_divided_and_joined(dtype, width, n):
     held = [width * 16 if x > 1 else 100 + 7 * b for b, x in enumerate(n)]
     told = [width * 16 + 40 if x > 1 else y for x, y in zip(n, held)]
     check(held, n, told, 1, 1, 64, dtype, width, True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [2, 70])
+def test_row_offsets_at_the_ends_of_their_type(dtype, n):
+    """Offsets of -2^31 and 2^31 - 1 behind sound ones: the requests that they end or begin have no rows, or those up to M, and nothing else is touched."""
+    least, most = -2 ** 31, 2 ** 31 - 1
+    p = Pool([100, 90, 80], 4, 2, 64, 16, dtype, seed=n).rows([n, n, n])
+    want, slack = R.attention(p.q, p.k, p.v, p.table, p.lens, p.cu, False, 64 ** -0.5)
+    q, k, v, table, lens = p.q.cuda(), p.k.cuda(), p.v.cuda(), p.table.cuda(), torch.tensor(p.lens, dtype=torch.int32, device="cuda")
+    for cu, written in (([0, n, least, least + 1], 1), ([0, n, least + n, least], 1), ([least, n, 2 * n, most], 3), ([0, n, most, least], 2), ([most, least, -1, 0], 0)):
+        buf = torch.full((3 * n + 8, 4, 64), 7.0, dtype=p.dtype, device="cuda")
+        B.page_attention(q, k, v, table, lens, cu_rows=torch.tensor(cu, dtype=torch.int32, device="cuda"), out=buf[4: 4 + 3 * n])
+        got, own = buf[4: 4 + 3 * n].cpu(), n if written == 2 else n * written      # with `most` behind n, request 1 has all rows from n on
+        assert R.close(got[:own], want[:own], slack[:own])
+        if written == 2:
+            again, off = R.attention(p.q, p.k, p.v, p.table, p.lens, [0, n, 3 * n, 3 * n], False, 64 ** -0.5)
+            assert R.close(got, again, off)
+        else:
+            assert bool((got[own:] == 7.0).all())
+        assert bool((buf[:4] == 7.0).all() and (buf[4 + 3 * n:] == 7.0).all())
