@@ -380,7 +380,8 @@ pvf_status pvf_page_extend(void *stream, const int32_t *seq_len, const int32_t *
 
 /* Request b keeps its first keep[b] tokens (seq_len_out[b] = min(max(keep[b], 0), seq_len[b]): rejected drafts, or all of an ended request);
  * the pages behind them go to free_pages[*n_free ..), in order of requests and pages: those of request b to place[b] .. place[b + 1] - 1.
- * The table stays as it is.  free_pages holds free_cap pages; what would lie behind them is dropped.
+ * The table stays as it is.  free_pages holds free_cap pages; what would lie behind them is dropped.  A page that several requests share comes back once
+ * for each that gives it up: keep those of a shared canvas with one of them.
  * seq_len_out may be seq_len or keep, n_free_out may be n_free; nothing else may overlap. */
 pvf_status pvf_page_trim(void *stream, const int32_t *seq_len, const int32_t *keep, int32_t B, const int32_t *table, int32_t width,
                          int64_t table_stride, int32_t page_size, int32_t *free_pages, int32_t free_cap, const int32_t *n_free,

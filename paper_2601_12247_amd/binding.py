@@ -568,7 +568,7 @@ def gemm_mx_instance(call: int, M: int, N: int, K: int, w_fmt: int = MX_E4M3, dt
 # ---- keys and values in pages --------------------------------------------------------------
 # A cache is a pair of tensors [n_pages, Hkv, page_size, d_head], pages contiguous but for the distance between them (stride(0)); a table is
 # int32 [B, width], its rows apart by stride(0): the library refuses a table whose rows overlap, as an expanded one's do (one row for all requests: copy it).
-# Lengths, counts, positions and slots are int32.  These calls may stand in a loop of single tokens, where what a check costs counts:
+# Lengths, counts, positions and slots are int32.  Tables may be of pages of any size, page_store and page_attention take multiples of 8.  These calls may stand in a loop of single tokens, where what a check costs counts:
 # conditions are written out in one expression, and what does not fit is looked at again to say what it was.
 _i32_t = torch.int32
 

@@ -311,8 +311,8 @@ __device__ __forceinline__ uint32_t bf16s_finite(uint32_t w) {   // what is not 
 // y (float32 bits) where it is not finite, else zero: what a key adds whose probability is not zero
 __device__ __forceinline__ float odd_part(uint32_t y) { return (y & 0x7f800000u) == 0x7f800000u ? __uint_as_float(y) : 0.f; }
 
-// Two probabilities as bf16 in two parts: the upper halves, and the rest of 16 bits.  The rest is never zero beside p > 0 (2^-23 of p is added): zero
-// times an infinite value would make NaN of infinity.
+// Two probabilities as bf16 in two parts: the upper halves, and the rest of 16 bits.  The rest is never zero beside p > 2^-110 (2^-23 of p is added, and
+// bf16 ends at 2^-133): zero times an infinite value would make NaN of infinity.
 __device__ __forceinline__ uint32_t upper_parts(float x, float y) { return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302); }
 __device__ __forceinline__ uint32_t lower_parts(float x, float y) {
   auto low = [](float p) { return (bf16_t)__builtin_fmaf(p, 1.0f + 0x1p-23f, -__uint_as_float(__float_as_uint(p) & 0xffff0000u)); };

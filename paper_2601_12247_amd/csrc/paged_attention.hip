@@ -7,11 +7,12 @@
 // lane c holds dimensions VE c .. of four neighbouring keys, and operand j of the matrix instruction is made of dimension VE c + j of those.
 //
 // P enters the bf16 instruction as two bf16 parts (16 bits of it): the second instruction costs nothing beside the memory, and the result is
-// rounded once, to its own type.
+// rounded once, to its own type.  Beside probabilities of 32 bits that moves 0.4 % of results to the neighbouring bf16 (32768 keys: 0.42 and 0.46 % differ from 64 bits
+// rounded once, 0.17 and 0.10 % with float32 arithmetic, on two inputs); the error against 64 bits is that of the one rounding, to four digits.
 //
-// Bound by reading keys and values.  bf16, 64 requests of up to 8192 tokens, 8 key heads, groups of 4: 184 us for 1.05 GB (5.7 TB/s; a copy, which writes
-// as well, reaches 4.9), and 7 to join.  One request of 32768: 27.4 us for 134 MB (4.9 TB/s), and 6 to join.  Where there is little to read it is latency:
-// f32, one request of 128 tokens, 6.4 us; 17 of up to 1411 with 5 rows, 17.2 us and 4.8 to join for 21 MB, of which the first keys take 6.
+// Bound by reading keys and values.  bf16, 64 requests of up to 8192 tokens, 8 key heads, groups of 4: 191 us for 1.05 GB (5.5 TB/s; a copy, which writes
+// as well, reaches 4.9), and 8 to join.  One request of 32768: 28.2 us for 134 MB (4.8 TB/s), and 6 to join.  Where there is little to read it is latency:
+// f32, one request of 128 tokens, 6.5 us; 17 of up to 1411 with 5 rows, 16.9 us and 4.8 to join for 21 MB, of which the first keys take 6.
 #include "paged_attention.h"
 
 #include <cmath>

@@ -7,8 +7,8 @@
 // keys in that order: transposing reads give a lane four keys of one dimension.
 //
 // Bound by what a step takes in turn: 64 keys of 128 columns are 3400 cycles, 1545 of the matrix unit and about 1800 of the vector unit, which overlap in
-// part, and with the loads behind them.  bf16, 9 windows of 128 rows over up to 1280 tokens, 32 heads of 128: 58 us for 24 GFLOP (36 with P's second
-// part: 0.62 PFLOP/s) and 200 MB (3.6 TB/s), and 8 to join.  Without the products 50 us, without the loads 54.  Eight waves a workgroup took 85 us, two
+// part, and with the loads behind them.  bf16, 9 windows of 128 rows over up to 1280 tokens, 32 heads of 128: 60 us for 24 GFLOP (36 with P's second
+// part: 0.60 PFLOP/s) and 200 MB (3.4 TB/s), and 9 to join.  Without the products 50 us, without the loads 54.  Eight waves a workgroup took 85 us, two
 // workgroups of 64 columns 81.
 //
 // LDS rows are keys, in 16-byte chunks; chunk x of a key lies at x ^ turn(key), so that equal chunks of 8 keys (the operand K) and pairs of chunks of 4 keys

@@ -56,7 +56,7 @@ def requests(nreq, most_len, most_rows, W, P, seed):
     return lens, rows, table, pages + [-5] * 3, len(pages)
 
 
-# (requests, longest, most rows, width, page size): one launch, and two (more than 8192 rows or 2048 requests)
+# (requests, longest, most rows, width, page size): one launch, and two (more than 2048 rows or 2048 requests)
 SIZES = [(1, 0, 1, 1, 16), (1, 15, 1, 2, 16), (1, 16, 1, 2, 16), (5, 40, 3, 9, 8), (64, 500, 1, 40, 16), (63, 100, 200, 30, 16), (700, 30, 5, 9, 7), (2048, 9, 4, 20, 1),
          (9, 100, 3000, 200, 24), (2049, 20, 1, 9, 8), (1, 3, 20000, 400, 64), (3000, 64, 64, 20, 16), (1025, 10, 2, 4, 8)]
 
